@@ -59,12 +59,18 @@ extern "C" {
 #define BMX_ERR_WORKSPACE (-6)   /* workspace NULL or smaller than bmx_workspace_bytes says (bmx_quant_gemm: see there) */
 #define BMX_ERR_HIP (-7)         /* the HIP runtime reported an error at launch */
 
+/* Element types of the calls that take more than fp32. */
+#define BMX_F32 0
+#define BMX_F16 1
+#define BMX_BF16 2
+
 /* Operation selectors for bmx_workspace_bytes. */
 #define BMX_OP_BINARY_FC 1     /* dims = {batch, in_features, out_features} */
 #define BMX_OP_BINARY_CONV2D 2 /* dims = {N, C, H, W, O, KH, KW, stride, pad} */
 #define BMX_OP_QUANT_GEMM 3    /* dims = {M, N, K, bits_a, bits_w} */
 #define BMX_OP_BINARY_CONV2D_BITS 4 /* dims = {N, C, H, W, O, KH, KW, stride, pad, out_pad} */
 #define BMX_OP_XNOR_GEMM_W32 5 /* dims = {M, N, K} */
+#define BMX_OP_KV_ATTENTION 6 /* dims = {sequences, table_width, heads, q_heads, dim, max_new} */
 
 /* Sign-binarise and bit-pack (Sec. 1: binarisation with the sign function, 64
  * values per word; Sec. 3.1: the per-forward-pass input binarisation step).
@@ -260,6 +266,75 @@ int bmx_binary_conv2d_bits(const uint64_t* xp, int N, int C, int H, int W, const
 int bmx_quant_gemm(const float* a, int64_t lda, int bits_a, const float* w, int64_t ldw,
                    int bits_w, int M, int N, int K, int32_t* out_i32_scaled, float* out_f32,
                    int64_t ldo, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- A decoder layer in few bits: 4-bit weights, a cache of 8 bits, attention over it ----
+ *
+ * Values are of `type` (BMX_F32, BMX_F16 or BMX_BF16) where a pointer is void*; sums, running maxima and scales are fp32, and a
+ * result is rounded to its type once, at the end.
+ *
+ * 4-bit weights with group scales.  Row n of W [N, K] is cut into groups of `group` = 32, 64 or 128 values, each with a scale s and an
+ * offset b in bf16; a weight is w = s * q + b with a level q in 0..15.
+ *   tiles   uint8 [ceil(N/16)][ceil(K/128)][1024], 16-byte aligned: 16 rows x 128 values a tile, in the order of the matrix cores' lanes:
+ *           byte (n%16 + 16*g)*16 + 4*step + p holds, of row n, the values k = 128*tile + 32*step + 8*g + j, four bits each: j = 2*(c%4)
+ *           + c/4 in nibble c = 2*p (low) and 2*p + 1 (high).  Levels of rows >= N and of k >= K do not matter.
+ *   scales  bf16 pairs (s, b) [ceil(N/16)][ceil(K/128)*128/group][16], 16-byte aligned.
+ * bmx_w4_quantize: from fp32 weights [N, ldw].  Over a group's finite values: b = bf16(min), s = bf16(max/15 - min/15),
+ *   q = round((w - b) / s) to the nearest, ties to even, clamped to 0..15 (all 0 where s < 2^-126); NaN is level 0.
+ * bmx_w4_dequantize: w = s * q + b in fp32, [N, ldw].
+ * bmx_w4_fc: out[m][n] = sum_k x[m][k] * w[n][k] + bias[n], x [M, ldx] and out [M, ldo] of `type`, bias fp32 [N] or NULL.  Exact weights
+ *   and x against fp32 sums: neither is rounded on the way.  M, N < 2^22. */
+int bmx_w4_quantize(const float* w, int64_t ldw, int N, int K, int group, uint8_t* tiles, uint16_t* scales, void* stream);
+int bmx_w4_dequantize(const uint8_t* tiles, const uint16_t* scales, int N, int K, int group, float* w, int64_t ldw, void* stream);
+int bmx_w4_fc(const void* x, int type, int64_t ldx, const uint8_t* tiles, const uint16_t* scales, int group, const float* bias,
+              int M, int N, int K, void* out, int64_t ldo, void* stream);
+
+/* A paged cache of keys and values in 8 bits.  A page holds 64 tokens of a sequence; a block of 16, 32 or 64 tokens of a page has, for
+ * each head, one scale for its keys and one for its values: a value is q * scale with a level q in -127..127.
+ *   pages   int8 [num_pages][heads][2][64*row], 16-byte aligned, row = dim rounded up to 32; keys (0), then values (1).  Token t, value d:
+ *           keys at    t/16*16*row + d/64*1024 + d%64/16*256 + t%16*16 + d%16, in a last 32 values of a row that is no multiple of 64
+ *                      t/16*16*row + d/64*1024 + d%32/8*128 + t%16*8 + d%8;
+ *           values at  d/16*1024 + t%16/4*256 + d%16*16 + t/16*4 + t%4.
+ *           (In the order of the matrix cores' lanes.)  What lies between dim and row does not matter.
+ *   scales  fp32 [num_pages][heads][2][64/block].
+ *   table   int32 [sequences][table_ld], table_width pages of each sequence in order, each a page number.  What tokens do not reach is not read.
+ *           A page that new tokens go to belongs to one sequence.
+ *   lengths int32 [sequences]: tokens of each sequence, those of the call in hand included.
+ *   starts  int32 [sequences + 1] or NULL: the call's rows starts[i] .. starts[i+1] are sequence i's, its last tokens; NULL: as many
+ *           rows for each.
+ * The four arrays of integers are device memory, which the host does not look at.  Kernels stay inside the buffers whatever they
+ * hold: tokens past 64 * table_width, on page numbers outside 0 .. num_pages - 1 or at positions below 0 are not there. */
+typedef struct bmx_kv_cache {
+  int8_t* pages;
+  float* scales;
+  const int32_t* table;
+  int64_t table_ld;
+  const int32_t* lengths;
+  const int32_t* starts;
+  int sequences, table_width, num_pages, heads, dim, block; /* dim in 1..256 */
+} bmx_kv_cache;
+
+/* Calls on the cache.  k, v and q, out are `rows` rows of heads, element d of head h of row r at r*X_row + h*X_head + d.  max_new: no
+ * sequence has more rows in this call (0: not known; rows beyond it are not looked at); with starts NULL it follows from rows, a
+ * multiple of sequences.
+ * bmx_kv_write: quantises the rows into the cache, at each sequence's last positions.  A block's scale is max |x| / 127 over its tokens; one
+ *   that holds older tokens keeps its scale s_old unless a new value is past 127 * s_old, and then the older levels become
+ *   round(q * (s_old / s)).  New levels are round(x * (1 / s)) (all 0 where s < 2^-126), to the nearest, ties to even.  Scales are taken over
+ *   finite values; an infinity is level +-127, NaN is level 0.
+ * bmx_kv_read: the rows' values q * scale; rows of tokens that are not there are zeros.
+ * bmx_kv_attention: out = softmax(scale * q k^T) v with q_heads heads of queries, a multiple of cache->heads: head h reads head
+ *   h / (q_heads / heads) of the cache.  A row at position p sees the tokens t < its sequence's length, with causal those t <= p, with
+ *   window > 0 those t > p - window.  A row that sees nothing is zeros.  lse fp32 [rows][q_heads] or NULL: the logarithm of the
+ *   softmax's sum (-infinity where nothing is seen).
+ *   workspace >= bmx_workspace_bytes(BMX_OP_KV_ATTENTION, {sequences, table_width, heads, q_heads, dim, max_new}, 6), 16-byte aligned, all
+ *   zeros before the first call that uses it; every call leaves it ready for the next on its stream, whatever that one's sizes.  NULL
+ *   where that is 0. */
+int bmx_kv_write(const bmx_kv_cache* cache, const void* k, const void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row,
+                 int64_t v_head, int64_t rows, int max_new, void* stream);
+int bmx_kv_read(const bmx_kv_cache* cache, void* k, void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head,
+                int64_t rows, int max_new, void* stream);
+int bmx_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
+                     int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                     void* workspace, size_t workspace_bytes, void* stream);
 
 /* alpha[r] = mean_j |w[r][j]| over cols entries per row (the XNOR-Net weight scale the
  * abstract refers to), accumulated in fp64 and rounded once to fp32.

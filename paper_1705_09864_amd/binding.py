@@ -20,15 +20,24 @@ _lib = None
 _native = None
 
 OP_BINARY_FC, OP_BINARY_CONV2D, OP_QUANT_GEMM, OP_BINARY_CONV2D_BITS, OP_XNOR_GEMM_W32 = 1, 2, 3, 4, 5
+OP_KV_ATTENTION = 6
+PAGE = 64  # tokens of a page of a cache
 EXPORTS = ["bmx_binarize_pack", "bmx_xnor_gemm", "bmx_binary_fc", "bmx_pack_conv_weights",
            "bmx_binary_conv2d", "bmx_quant_gemm", "bmx_alpha_mean_abs", "bmx_pack_nchw",
            "bmx_binary_conv2d_packed", "bmx_workspace_bytes", "bmx_status_string", "bmx_version",
            "bmx_conv_weight_row_words", "bmx_binary_fc_packed", "bmx_tune_set",
            "bmx_binary_conv2d_bits", "bmx_xnor_gemm_count", "bmx_unpack_pm1", "bmx_widen_words32",
            "bmx_xnor_gemm_w32", "bmx_binary_fc_static", "bmx_last_kernel",
-           "bmx_probe_valu"]
+           "bmx_probe_valu", "bmx_w4_quantize", "bmx_w4_dequantize", "bmx_w4_fc", "bmx_kv_write", "bmx_kv_read",
+           "bmx_kv_attention"]
 
 _i64, _int, _p, _sz = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
+
+
+class KvCache(ctypes.Structure):
+    """bmx_kv_cache of include/bmx.h, for calls of the C functions themselves."""
+    _fields_ = [("pages", _p), ("scales", _p), ("table", _p), ("table_ld", _i64), ("lengths", _p), ("starts", _p), ("sequences", _int),
+                ("table_width", _int), ("num_pages", _int), ("heads", _int), ("dim", _int), ("block", _int)]
 
 
 class BmxError(RuntimeError):
@@ -85,6 +94,16 @@ def lib():
         L.bmx_probe_valu.restype = _int
         L.bmx_tune_set.argtypes = [_int, _int]
         L.bmx_tune_set.restype = _int
+        _kv = ctypes.POINTER(KvCache)
+        L.bmx_w4_quantize.argtypes = [_p, _i64, _int, _int, _int, _p, _p, _p]
+        L.bmx_w4_dequantize.argtypes = [_p, _p, _int, _int, _int, _p, _i64, _p]
+        L.bmx_w4_fc.argtypes = [_p, _int, _i64, _p, _p, _int, _p, _int, _int, _int, _p, _i64, _p]
+        L.bmx_kv_write.argtypes = [_kv, _p, _p, _int, _i64, _i64, _i64, _i64, _i64, _int, _p]
+        L.bmx_kv_read.argtypes = L.bmx_kv_write.argtypes
+        L.bmx_kv_attention.argtypes = [_kv, _p, _int, _i64, _i64, _int, _i64, _int, ctypes.c_float, _int, _int, _p, _i64, _i64,
+                                       _p, _p, _sz, _p]
+        for name in EXPORTS[-6:]:
+            getattr(L, name).restype = _int
         for name in EXPORTS[:9]:
             getattr(L, name).restype = _int
         _lib = L
@@ -257,3 +276,48 @@ def quant_gemm(a, w, bits_a, bits_w=1, want_int=True, want_float=True, out_int=N
 
 def alpha_mean_abs(w, stream=None):
     return (_native or _host()).alpha_mean_abs(w, stream)
+
+
+def w4_quantize(w, group=128, stream=None):
+    """w: fp32 [N, K] -> (tiles, scales): 4-bit levels, and a bf16 scale and offset for each `group` (32, 64 or 128) values of a row."""
+    return (_native or _host()).w4_quantize(w, group, stream)
+
+
+def w4_dequantize(tiles, scales, N, K, out=None, stream=None):
+    """The fp32 weights [N, K] that the tiles stand for."""
+    return (_native or _host()).w4_dequantize(tiles, scales, N, K, out, stream)
+
+
+def w4_fc(x, tiles, scales, N, bias=None, out=None, stream=None):
+    """x: [M, K] of float32, float16 or bfloat16 -> [M, N] of the same type: x w^T + bias."""
+    return (_native or _host()).w4_fc(x, tiles, scales, N, bias, out, stream)
+
+
+def kv_cache(num_pages, heads, dim, block=16, device="cuda"):
+    """New memory of a cache, (pages, scales): num_pages pages of 64 tokens, a scale for each `block` (16, 32 or 64) of them and head."""
+    if block not in (16, 32, 64):
+        raise ValueError("kv_cache: block must be 16, 32 or 64 (got %r)" % (block,))
+    row = (dim + 31) // 32 * 32
+    return (torch.zeros((num_pages, heads, 2, PAGE * row), dtype=torch.int8, device=device),
+            torch.zeros((num_pages, heads, 2, PAGE // block), dtype=torch.float32, device=device))
+
+
+def kv_write(k, v, pages, scales, table, lengths, starts=None, max_new=0, stream=None):
+    """Quantises k, v [rows, heads, dim] into the cache, at each sequence's last positions.  table: int32 [sequences, pages of one];
+    lengths: int32 [sequences], the new tokens included; starts: int32 [sequences + 1], each sequence's first row (None: as many for
+    each); max_new: no sequence has more new rows (0: not known)."""
+    return (_native or _host()).kv_write(k, v, pages, scales, table, lengths, starts, max_new, stream)
+
+
+def kv_read(pages, scales, table, lengths, dim, dtype, rows, starts=None, max_new=0, out_k=None, out_v=None, stream=None):
+    """The last tokens of each sequence, `rows` in all, as kv_write takes them: (k, v), each [rows, heads, dim] of `dtype`."""
+    return (_native or _host()).kv_read(pages, scales, table, lengths, dim, dtype, rows, starts, max_new, out_k, out_v, stream)
+
+
+def kv_attention(q, pages, scales, table, lengths, starts=None, max_new=0, scale=None, causal=True, window=0, lse=False, out=None,
+                 workspace=None, stream=None):
+    """Attention of each sequence's last tokens, q [rows, q_heads, dim], over its part of the cache; scale: 1 / sqrt(dim) if None.
+    lse: returns (out, log of the softmax's sum, fp32 [rows, q_heads]).  workspace: a tensor of kv_attention_workspace bytes or
+    more, zeros before its first use and kept from call to call on one stream; None: made and cleared in the call."""
+    return (_native or _host()).kv_attention(q, pages, scales, table, lengths, starts, max_new, scale, causal, window, lse, out,
+                                             workspace, stream)

@@ -73,6 +73,44 @@ QuantWs quant_ws(int64_t M, int64_t N, int64_t K, int bits_a, int bits_w) {
   return q;
 }
 
+inline bool is_type(int type) { return type == BMX_F32 || type == BMX_F16 || type == BMX_BF16; }
+
+int w4_check(int N, int K, int group) {
+  if (N < 0 || N >= (1 << 22) || K <= 0 || K >= kMaxK) return BMX_ERR_SHAPE;
+  if (group != 32 && group != 64 && group != 128) return BMX_ERR_UNSUPPORTED;
+  if (bmx::ceil_div(N, 16) * bmx::ceil_div(K, 128) >= ((int64_t)1 << 31)) return BMX_ERR_SHAPE;
+  return BMX_OK;
+}
+
+// The description of a cache and the number of a call's rows; *max_new becomes what it stands for.
+int kv_check(const bmx_kv_cache* c, int type, int64_t rows, int* max_new) {
+  if (!c) return BMX_ERR_NULL;
+  if (c->sequences < 0 || c->sequences > 65535 || c->table_width < 0 || c->num_pages < 0 || c->heads <= 0 || c->heads > 32767 ||
+      c->dim <= 0 || c->dim > 256 || rows < 0 || rows >= ((int64_t)1 << 31) || *max_new < 0)
+    return BMX_ERR_SHAPE;
+  if (!is_type(type) || (c->block != 16 && c->block != 32 && c->block != 64)) return BMX_ERR_UNSUPPORTED;
+  if (rows > 0 && c->sequences == 0) return BMX_ERR_SHAPE;
+  if (!c->starts && rows > 0 && rows % c->sequences) return BMX_ERR_SHAPE;
+  if (!c->starts) *max_new = rows > 0 ? (int)(rows / c->sequences) : 0;
+  else if (*max_new == 0 || *max_new > rows) *max_new = (int)rows;
+  if (c->sequences * ((int64_t)*max_new / 64 + 2) >= ((int64_t)1 << 31)) return BMX_ERR_SHAPE;  // (workgroups of a launch)
+  if (rows == 0) return BMX_OK;
+  if (!c->pages || !c->scales || !c->lengths || (!c->table && c->table_width > 0)) return BMX_ERR_NULL;
+  if (c->table_ld < c->table_width) return BMX_ERR_LD;
+  if (misaligned(c->pages, 16) || misaligned(c->scales, 4) || misaligned(c->table, 4) || misaligned(c->lengths, 4) ||
+      misaligned(c->starts, 4))
+    return BMX_ERR_ALIGN;
+  return BMX_OK;
+}
+
+// Rows of heads in memory.
+int kv_rows_check(const void* p, int type, int64_t row, int64_t head, int64_t rows, int heads, int dim) {
+  if (!p) return BMX_ERR_NULL;
+  if ((rows > 1 && row < dim) || (heads > 1 && head < dim)) return BMX_ERR_LD;
+  if (misaligned(p, type == BMX_F32 ? 4 : 2)) return BMX_ERR_ALIGN;
+  return BMX_OK;
+}
+
 }  // namespace
 
 namespace bmx {
@@ -189,6 +227,7 @@ size_t bmx_workspace_bytes(int op, const int64_t* dims, int ndims) {
                       (int)dims[4])
           .total;
     }
+    case BMX_OP_KV_ATTENTION: return 0;
     default: return 0;
   }
 }
@@ -675,6 +714,87 @@ int bmx_alpha_mean_abs(const float* w, int64_t rows, int64_t cols, int64_t ldw, 
   if (ldw < cols) return BMX_ERR_LD;
   if (misaligned(w, 4) || misaligned(alpha, 4)) return BMX_ERR_ALIGN;
   return hip_status(bmx::launch_alpha_mean_abs(w, rows, cols, ldw, alpha, (hipStream_t)stream));
+}
+
+int bmx_w4_quantize(const float* w, int64_t ldw, int N, int K, int group, uint8_t* tiles, uint16_t* scales, void* stream) {
+  const int st = w4_check(N, K, group);
+  if (st != BMX_OK || N == 0) return st;
+  if (!w || !tiles || !scales) return BMX_ERR_NULL;
+  if (ldw < K) return BMX_ERR_LD;
+  if (misaligned(w, 4) || misaligned(tiles, 16) || misaligned(scales, 16)) return BMX_ERR_ALIGN;
+  return hip_status(bmx::launch_w4_quantize(w, ldw, N, K, group, tiles, scales, (hipStream_t)stream));
+}
+
+int bmx_w4_dequantize(const uint8_t* tiles, const uint16_t* scales, int N, int K, int group, float* w, int64_t ldw, void* stream) {
+  const int st = w4_check(N, K, group);
+  if (st != BMX_OK || N == 0) return st;
+  if (!w || !tiles || !scales) return BMX_ERR_NULL;
+  if (ldw < K) return BMX_ERR_LD;
+  if (misaligned(w, 4) || misaligned(tiles, 16) || misaligned(scales, 16)) return BMX_ERR_ALIGN;
+  return hip_status(bmx::launch_w4_dequantize(tiles, scales, N, K, group, w, ldw, (hipStream_t)stream));
+}
+
+int bmx_w4_fc(const void* x, int type, int64_t ldx, const uint8_t* tiles, const uint16_t* scales, int group, const float* bias,
+              int M, int N, int K, void* out, int64_t ldo, void* stream) {
+  const int st = w4_check(N, K, group);
+  if (st != BMX_OK) return st;
+  if (M < 0 || M >= (1 << 22)) return BMX_ERR_SHAPE;
+  if (!is_type(type)) return BMX_ERR_UNSUPPORTED;
+  if (M == 0 || N == 0) return BMX_OK;
+  if (!x || !tiles || !scales || !out) return BMX_ERR_NULL;
+  if (ldx < K || ldo < N) return BMX_ERR_LD;
+  const size_t size = type == BMX_F32 ? 4 : 2;
+  if (misaligned(x, size) || misaligned(out, size) || misaligned(tiles, 16) || misaligned(scales, 16) || misaligned(bias, 4))
+    return BMX_ERR_ALIGN;
+  return hip_status(bmx::launch_w4_fc(x, type, ldx, tiles, scales, group, bias, M, N, K, out, ldo, (hipStream_t)stream));
+}
+
+int bmx_kv_write(const bmx_kv_cache* cache, const void* k, const void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row,
+                 int64_t v_head, int64_t rows, int max_new, void* stream) {
+  int st = kv_check(cache, type, rows, &max_new);
+  if (st != BMX_OK || rows == 0) return st;
+  if ((st = kv_rows_check(k, type, k_row, k_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
+  if ((st = kv_rows_check(v, type, v_row, v_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
+  return hip_status(bmx::launch_kv_write(*cache, k, v, type, k_row, k_head, v_row, v_head, (int)rows, max_new, (hipStream_t)stream));
+}
+
+int bmx_kv_read(const bmx_kv_cache* cache, void* k, void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head,
+                int64_t rows, int max_new, void* stream) {
+  int st = kv_check(cache, type, rows, &max_new);
+  if (st != BMX_OK || rows == 0) return st;
+  if ((st = kv_rows_check(k, type, k_row, k_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
+  if ((st = kv_rows_check(v, type, v_row, v_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
+  return hip_status(bmx::launch_kv_read(*cache, k, v, type, k_row, k_head, v_row, v_head, (int)rows, max_new, (hipStream_t)stream));
+}
+
+static int kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
+                        int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                        void* workspace, size_t workspace_bytes, void* stream, bool lazy) {
+  int st = kv_check(cache, type, rows, &max_new);
+  if (st != BMX_OK) return st;
+  if (q_heads <= 0 || q_heads % cache->heads || q_heads > 65535 || window < 0) return BMX_ERR_SHAPE;
+  if ((int64_t)max_new * (q_heads / cache->heads) > 65535 * 16) return BMX_ERR_SHAPE;
+  if (rows == 0) return BMX_OK;
+  if ((st = kv_rows_check(q, type, q_row, q_head, rows, q_heads, cache->dim)) != BMX_OK) return st;
+  if ((st = kv_rows_check(out, type, out_row, out_head, rows, q_heads, cache->dim)) != BMX_OK) return st;
+  if (misaligned(lse, 4)) return BMX_ERR_ALIGN;
+  (void)workspace, (void)workspace_bytes, (void)lazy;
+  return hip_status(bmx::launch_kv_attention(*cache, q, type, q_row, q_head, q_heads, (int)rows, max_new, scale, causal != 0, window, out,
+                                             out_row, out_head, lse, (hipStream_t)stream));
+}
+
+int bmx_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
+                     int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  return kv_attention(cache, q, type, q_row, q_head, q_heads, rows, max_new, scale, causal, window, out, out_row, out_head, lse,
+                      workspace, workspace_bytes, stream, false);
+}
+
+int bmx_lazy_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
+                          int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  return kv_attention(cache, q, type, q_row, q_head, q_heads, rows, max_new, scale, causal, window, out, out_row, out_head, lse,
+                      workspace, workspace_bytes, stream, true);
 }
 
 }  // extern "C"

@@ -10,6 +10,7 @@
 #include <tuple>
 #include <type_traits>
 
+#include "../../include/bmx.h"
 #include "lds_limit.h"
 
 namespace bmx {
@@ -246,6 +247,20 @@ bool launch_quant_i8(const float* a, int64_t lda, int bits_a, const float* w, in
 // would take the product (what it is weighed against; else the plane kernels are).
 bool launch_quant_small(const float* a, int64_t lda, int bits_a, const float* w, int64_t ldw, int bits_w, int M, int N,
                         int K, int32_t* S_out, float* out_f32, int64_t ldo, bool pair, hipStream_t s, hipError_t* err);
+
+// w4.hip: products with 4-bit weights, and the weights' way into their tiles and back.
+hipError_t launch_w4_fc(const void* x, int type, int64_t ldx, const void* tiles, const void* scales, int group, const float* bias, int M,
+                        int N, int K, void* out, int64_t ldo, hipStream_t s);
+hipError_t launch_w4_quantize(const float* w, int64_t ldw, int N, int K, int group, void* tiles, void* scales, hipStream_t s);
+hipError_t launch_w4_dequantize(const void* tiles, const void* scales, int N, int K, int group, float* w, int64_t ldw, hipStream_t s);
+// kv_cache.hip, kv_attention.hip: the cache of 8 bits and the attention over it.
+hipError_t launch_kv_write(const bmx_kv_cache& c, const void* k, const void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row,
+                           int64_t v_head, int rows, int max_new, hipStream_t s);
+hipError_t launch_kv_read(const bmx_kv_cache& c, void* k, void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head,
+                          int rows, int max_new, hipStream_t s);
+hipError_t launch_kv_attention(const bmx_kv_cache& c, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int rows,
+                               int max_new, float scale, bool causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                               hipStream_t s);
 
 // The same convolution on the GEMM kernel (filters = A rows streamed through SGPRs, im2col
 // rows gathered per chunk): for K that does not fit the stationary kernel or grids with too

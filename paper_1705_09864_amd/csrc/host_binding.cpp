@@ -12,10 +12,12 @@
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <initializer_list>
 #include <optional>
@@ -452,6 +454,168 @@ FUNCTION(alpha_mean_abs, 2) {  // w, stream
   return out.result();
 }
 
+// ---- a decoder layer in few bits ----
+
+int type_of(at::ScalarType t) { return t == at::kFloat ? BMX_F32 : t == at::kHalf ? BMX_F16 : t == at::kBFloat16 ? BMX_BF16 : -1; }
+
+// A tensor of one of the three types of values (or of the one given).
+T values(PyObject* o, int dims, const char* what, const at::ScalarType* type = nullptr) {
+  if (!THPVariable_Check(o)) raise_value("%s: expected a torch tensor, got %s", what, Py_TYPE(o)->tp_name);
+  const at::ScalarType t = THPVariable_Unpack(o).scalar_type();
+  if (type_of(t) < 0) raise_value("%s: dtype %s, expected Float, Half or BFloat16%s", what, c10::toString(t));
+  if (type && t != *type) raise_value("%s: dtype %s, expected %s", what, c10::toString(t), c10::toString(*type));
+  T v = &THPVariable_Unpack(o);
+  if (!v->is_cuda()) raise_value("%s: tensor must live on the GPU (device is %s)", what, v->device().str().c_str());
+  if (v->dim() != dims)
+    raise_value("%s: expected %s dimensions, got %s", what, std::to_string(dims).c_str(), std::to_string(v->dim()).c_str());
+  if (v->numel() > 0 && v->size(-1) > 1 && v->stride(-1) != 1)
+    raise_value("%s: last dimension must have stride 1 (got %s)", what, std::to_string(v->stride(-1)).c_str());
+  return v;
+}
+
+void shape(T t, at::IntArrayRef want, const char* what) {
+  if (t->sizes() == want) return;
+  std::string s;
+  for (int64_t n : want) s += (s.empty() ? "" : ", ") + std::to_string(n);
+  raise_value("%s: expected the shape [%s]%s", what, s.c_str());
+}
+
+FUNCTION(w4_quantize, 3) {  // w, group, stream -> (tiles, scales)
+  T w = required(a[0], kF32, 2, "w4_quantize w");
+  const int N = as_int(w->size(0)), K = as_int(w->size(1)), group = small(a[1]);
+  if (group != 32 && group != 64 && group != 128) check_status(BMX_ERR_UNSUPPORTED, "bmx_w4_quantize");
+  const int64_t nt = (N + 15ll) / 16, kt = (K + 127ll) / 128;
+  Out tiles(Py_None, at::kByte, {nt, kt, 1024}, w, ""), scales(Py_None, at::kBFloat16, {nt, kt * (128 / group), 16, 2}, w, "");
+  const hipStream_t s = stream_of(a[2]);
+  call("bmx_w4_quantize", bmx_w4_quantize, ptr<float>(w), ld(w), N, K, group, ptr<uint8_t>(tiles.t), ptr<uint16_t>(scales.t), s);
+  return Py_BuildValue("NN", tiles.result(), scales.result());
+}
+
+// The tiles and scales of weights [N, K]; returns the group.
+int w4_weights(PyObject* t, PyObject* s, int64_t N, int64_t K, const char* what, T* tiles, T* scales) {
+  *tiles = required(t, at::kByte, 3, what, true);
+  *scales = required(s, at::kBFloat16, 4, what, true);
+  const int64_t nt = (N + 15) / 16, kt = (K + 127) / 128, groups = (*scales)->size(1);
+  const int64_t group = groups > 0 ? kt * 128 / groups : 0;
+  if (group != 32 && group != 64 && group != 128) check_status(BMX_ERR_UNSUPPORTED, what);
+  shape(*tiles, {nt, kt, 1024}, what);
+  shape(*scales, {nt, kt * (128 / group), 16, 2}, what);
+  return (int)group;
+}
+
+FUNCTION(w4_dequantize, 6) {  // tiles, scales, N, K, out, stream
+  const int N = small(a[2]), K = small(a[3]);
+  T tiles, scales;
+  const int group = w4_weights(a[0], a[1], N, K, "w4_dequantize weights", &tiles, &scales);
+  Out out(a[4], kF32, {std::max(N, 0), std::max(K, 0)}, tiles, "w4_dequantize out");
+  if (a[4] != Py_None) shape(out.t, {N, K}, "w4_dequantize out");
+  const hipStream_t s = stream_of(a[5]);
+  call("bmx_w4_dequantize", bmx_w4_dequantize, ptr<uint8_t>(tiles), ptr<uint16_t>(scales), N, K, group, ptr<float>(out.t), ld(out.t), s);
+  return out.result();
+}
+
+FUNCTION(w4_fc, 7) {  // x, tiles, scales, N, bias, out, stream
+  T x = values(a[0], 2, "w4_fc x");
+  const int N = small(a[3]), M = as_int(x->size(0)), K = as_int(x->size(1));
+  T tiles, scales, bias = tensor(a[4], kF32, "w4_fc bias", true);
+  const int group = w4_weights(a[1], a[2], N, K, "w4_fc weights", &tiles, &scales);
+  if (bias) shape(bias, {N}, "w4_fc bias");
+  Out out(a[5], x->scalar_type(), {M, std::max(N, 0)}, x, "w4_fc out");
+  if (a[5] != Py_None) shape(out.t, {M, N}, "w4_fc out");
+  const hipStream_t s = stream_of(a[6]);
+  call("bmx_w4_fc", bmx_w4_fc, x->data_ptr(), type_of(x->scalar_type()), ld(x), ptr<uint8_t>(tiles), ptr<uint16_t>(scales), group,
+       ptr<float>(bias), M, N, K, out.t->data_ptr(), ld(out.t), s);
+  return out.result();
+}
+
+// pages, scales, table, lengths, starts of a cache whose heads have `dim` values
+bmx_kv_cache cache_of(PyObject* p, PyObject* s, PyObject* t, PyObject* n, PyObject* at_, int64_t dim) {
+  T pages = required(p, at::kChar, 4, "cache pages", true), scales = required(s, kF32, 4, "cache scales", true);
+  T table = required(t, kI32, 2, "cache table"), lengths = required(n, kI32, 1, "cache lengths", true);
+  T starts = tensor(at_, kI32, "cache starts", true);
+  const int64_t blocks = scales->size(3), seqs = lengths->size(0);
+  if (blocks != 1 && blocks != 2 && blocks != 4) check_status(BMX_ERR_UNSUPPORTED, "cache scales");
+  if (dim <= 0 || dim > 256) check_status(BMX_ERR_SHAPE, "cache");
+  shape(pages, {pages->size(0), pages->size(1), 2, 64 * ((dim + 31) / 32 * 32)}, "cache pages");
+  shape(scales, {pages->size(0), pages->size(1), 2, blocks}, "cache scales");
+  shape(table, {seqs, table->size(1)}, "cache table");
+  if (starts) shape(starts, {seqs + 1}, "cache starts");
+  return {ptr<int8_t>(pages), ptr<float>(scales), ptr<int32_t>(table), ld(table), ptr<int32_t>(lengths), ptr<int32_t>(starts),
+          as_int(seqs), as_int(table->size(1)), as_int(pages->size(0)), as_int(pages->size(1)), as_int(dim), (int)(64 / blocks)};
+}
+
+FUNCTION(kv_write, 9) {  // k, v, pages, scales, table, lengths, starts, max_new, stream
+  T k = values(a[0], 3, "kv_write k");
+  const at::ScalarType type = k->scalar_type();
+  T v = values(a[1], 3, "kv_write v", &type);
+  const bmx_kv_cache c = cache_of(a[2], a[3], a[4], a[5], a[6], k->size(2));
+  shape(k, {k->size(0), c.heads, c.dim}, "kv_write k");
+  shape(v, {k->size(0), c.heads, c.dim}, "kv_write v");
+  const int max_new = small(a[7]);
+  const hipStream_t s = stream_of(a[8]);
+  call("bmx_kv_write", bmx_kv_write, &c, k->data_ptr(), v->data_ptr(), type_of(type), k->stride(0), k->stride(1), v->stride(0),
+       v->stride(1), k->size(0), max_new, s);
+  Py_RETURN_NONE;
+}
+
+// pages, scales, table, lengths, dim, dtype, rows, starts, max_new, out_k, out_v, stream -> (k, v)
+FUNCTION(kv_read, 12) {
+  const bmx_kv_cache c = cache_of(a[0], a[1], a[2], a[3], a[7], integer(a[4]));
+  if (!THPDtype_Check(a[5])) raise_value("%s: expected a torch.dtype, got %s", "kv_read dtype", Py_TYPE(a[5])->tp_name);
+  const at::ScalarType type = reinterpret_cast<THPDtype*>(a[5])->scalar_type;
+  if (type_of(type) < 0) raise_value("%s: %s, expected Float, Half or BFloat16", "kv_read dtype", c10::toString(type));
+  const int64_t rows = integer(a[6]);
+  if (rows < 0) check_status(BMX_ERR_SHAPE, "bmx_kv_read");
+  T pages = &THPVariable_Unpack(a[0]), k, v;
+  std::optional<Out> ok, ov;
+  if (a[9] == Py_None) k = ok.emplace(Py_None, type, at::IntArrayRef({rows, c.heads, c.dim}), pages, "").t;
+  else k = values(a[9], 3, "kv_read out_k", &type);
+  if (a[10] == Py_None) v = ov.emplace(Py_None, type, at::IntArrayRef({rows, c.heads, c.dim}), pages, "").t;
+  else v = values(a[10], 3, "kv_read out_v", &type);
+  shape(k, {rows, c.heads, c.dim}, "kv_read out_k");
+  shape(v, {rows, c.heads, c.dim}, "kv_read out_v");
+  const int max_new = small(a[8]);
+  const hipStream_t s = stream_of(a[11]);
+  call("bmx_kv_read", bmx_kv_read, &c, k->data_ptr(), v->data_ptr(), type_of(type), k->stride(0), k->stride(1), v->stride(0), v->stride(1),
+       rows, max_new, s);
+  PyObject* r = PyTuple_New(2);
+  if (!r) throw python_error();
+  for (int i = 0; i < 2; ++i) {
+    std::optional<Out>& o = i ? ov : ok;
+    PyObject* x = o ? o->result() : a[9 + i];
+    if (!o) Py_INCREF(x);
+    PyTuple_SET_ITEM(r, i, x);
+  }
+  return r;
+}
+
+// q, pages, scales, table, lengths, starts, max_new, scale, causal, window, lse, out, workspace, stream -> out or (out, lse)
+FUNCTION(kv_attention, 14) {
+  T q = values(a[0], 3, "kv_attention q");
+  const at::ScalarType type = q->scalar_type();
+  const bmx_kv_cache c = cache_of(a[1], a[2], a[3], a[4], a[5], q->size(2));
+  const int64_t rows = q->size(0);
+  const int heads = as_int(q->size(1)), window = small(a[9]);
+  int max_new = small(a[6]);
+  const double scale = a[7] == Py_None ? 1.0 / std::sqrt((double)c.dim) : PyFloat_AsDouble(a[7]);
+  if (scale == -1.0 && PyErr_Occurred()) throw python_error();
+  std::optional<Out> made, lse;
+  T out;
+  if (a[11] == Py_None) out = made.emplace(Py_None, type, q->sizes(), q, "").t;
+  else out = values(a[11], 3, "kv_attention out", &type);
+  shape(out, q->sizes(), "kv_attention out");
+  if (truth(a[10])) lse.emplace(Py_None, kF32, at::IntArrayRef({rows, heads}), q, "");
+  const hipStream_t s = stream_of(a[13]);
+  lazily("bmx_kv_attention", a[12], BMX_OP_KV_ATTENTION,
+         {c.sequences, c.table_width, c.heads, heads, c.dim, c.starts ? max_new ? max_new : rows : rows / std::max(c.sequences, 1)}, q, s,
+         bmx_lazy_kv_attention, &c, q->data_ptr(), type_of(type), q->stride(0), q->stride(1), heads, rows, max_new, (float)scale,
+         (int)truth(a[8]), window, out->data_ptr(), out->stride(0), out->stride(1), lse ? ptr<float>(lse->t) : nullptr);
+  PyObject* o;
+  if (made) o = made->result();
+  else Py_INCREF(o = a[11]);
+  return lse ? Py_BuildValue("NN", o, lse->result()) : o;
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
   Py_INCREF(cls);
   Py_XDECREF(bmx_error);
@@ -464,6 +628,8 @@ PyMethodDef methods[] = {ENTRY(binarize_pack), ENTRY(unpack_pm1), ENTRY(xnor_gem
                          ENTRY(xnor_gemm_w32), ENTRY(binary_fc), ENTRY(binary_fc_static), ENTRY(binary_fc_packed),
                          ENTRY(pack_conv_weights), ENTRY(binary_conv2d), ENTRY(pack_nchw), ENTRY(binary_conv2d_packed),
                          ENTRY(binary_conv2d_bits), ENTRY(quant_gemm), ENTRY(alpha_mean_abs),
+                         ENTRY(w4_quantize), ENTRY(w4_dequantize), ENTRY(w4_fc), ENTRY(kv_write), ENTRY(kv_read),
+                         ENTRY(kv_attention),
                          {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bmx_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
