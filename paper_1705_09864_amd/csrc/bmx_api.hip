@@ -227,7 +227,13 @@ size_t bmx_workspace_bytes(int op, const int64_t* dims, int ndims) {
                       (int)dims[4])
           .total;
     }
-    case BMX_OP_KV_ATTENTION: return 0;
+    case BMX_OP_KV_ATTENTION: {
+      if (ndims != 6) return 0;
+      for (int i = 0; i < 6; ++i)
+        if (dims[i] < (i == 2 || i == 3 || i == 4) || dims[i] >= ((int64_t)1 << 31)) return 0;
+      if (dims[3] % dims[2] || dims[4] > 256) return 0;
+      return round256(bmx::kv_attention_workspace(dims[0], dims[1], dims[2], dims[3], dims[4], dims[5]));
+    }
     default: return 0;
   }
 }
@@ -769,7 +775,7 @@ int bmx_kv_read(const bmx_kv_cache* cache, void* k, void* v, int type, int64_t k
 
 static int kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
                         int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
-                        void* workspace, size_t workspace_bytes, void* stream, bool lazy) {
+                        void* workspace, size_t workspace_bytes, void* stream, bool fresh) {
   int st = kv_check(cache, type, rows, &max_new);
   if (st != BMX_OK) return st;
   if (q_heads <= 0 || q_heads % cache->heads || q_heads > 65535 || window < 0) return BMX_ERR_SHAPE;
@@ -778,9 +784,12 @@ static int kv_attention(const bmx_kv_cache* cache, const void* q, int type, int6
   if ((st = kv_rows_check(q, type, q_row, q_head, rows, q_heads, cache->dim)) != BMX_OK) return st;
   if ((st = kv_rows_check(out, type, out_row, out_head, rows, q_heads, cache->dim)) != BMX_OK) return st;
   if (misaligned(lse, 4)) return BMX_ERR_ALIGN;
-  (void)workspace, (void)workspace_bytes, (void)lazy;
+  const int64_t dims[6] = {cache->sequences, cache->table_width, cache->heads, q_heads, cache->dim, max_new};
+  const size_t need = bmx_workspace_bytes(BMX_OP_KV_ATTENTION, dims, 6);
+  if (need && (!workspace || workspace_bytes < need)) return BMX_ERR_WORKSPACE;
+  if (need && misaligned(workspace, 16)) return BMX_ERR_ALIGN;
   return hip_status(bmx::launch_kv_attention(*cache, q, type, q_row, q_head, q_heads, (int)rows, max_new, scale, causal != 0, window, out,
-                                             out_row, out_head, lse, (hipStream_t)stream));
+                                             out_row, out_head, lse, workspace, fresh, (hipStream_t)stream));
 }
 
 int bmx_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
@@ -790,9 +799,9 @@ int bmx_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t
                       workspace, workspace_bytes, stream, false);
 }
 
-int bmx_lazy_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
-                          int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
-                          void* workspace, size_t workspace_bytes, void* stream) {
+int bmx_fresh_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
+                           int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream) {
   return kv_attention(cache, q, type, q_row, q_head, q_heads, rows, max_new, scale, causal, window, out, out_row, out_head, lse,
                       workspace, workspace_bytes, stream, true);
 }

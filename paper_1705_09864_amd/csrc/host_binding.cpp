@@ -606,10 +606,13 @@ FUNCTION(kv_attention, 14) {
   shape(out, q->sizes(), "kv_attention out");
   if (truth(a[10])) lse.emplace(Py_None, kF32, at::IntArrayRef({rows, heads}), q, "");
   const hipStream_t s = stream_of(a[13]);
-  lazily("bmx_kv_attention", a[12], BMX_OP_KV_ATTENTION,
-         {c.sequences, c.table_width, c.heads, heads, c.dim, c.starts ? max_new ? max_new : rows : rows / std::max(c.sequences, 1)}, q, s,
-         bmx_lazy_kv_attention, &c, q->data_ptr(), type_of(type), q->stride(0), q->stride(1), heads, rows, max_new, (float)scale,
-         (int)truth(a[8]), window, out->data_ptr(), out->stride(0), out->stride(1), lse ? ptr<float>(lse->t) : nullptr);
+  const int64_t most = c.starts ? max_new ? std::min<int64_t>(max_new, rows) : rows : rows / std::max(c.sequences, 1);
+  Workspace ws;
+  const bool fresh = !ws.given(a[12]);
+  if (fresh) ws.allocate(BMX_OP_KV_ATTENTION, {c.sequences, c.table_width, c.heads, heads, c.dim, most}, q, s);
+  call("bmx_kv_attention", fresh ? bmx_fresh_kv_attention : bmx_kv_attention, &c, q->data_ptr(), type_of(type), q->stride(0),
+       q->stride(1), heads, rows, max_new, (float)scale, (int)truth(a[8]), window, out->data_ptr(), out->stride(0), out->stride(1),
+       lse ? ptr<float>(lse->t) : nullptr, ws.p, ws.bytes, s);
   PyObject* o;
   if (made) o = made->result();
   else Py_INCREF(o = a[11]);

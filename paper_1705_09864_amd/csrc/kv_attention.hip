@@ -10,13 +10,24 @@
 //   p goes in as p * (c_b / C) * 2^14 with C the largest c_b so far: at most 2^14, and with all of f16's 11 bits down to 2^-28 of that.
 // For f32 results they are bf16's, q and p * c_b in three parts of 8 bits each, which together are all of them whatever the range; levels
 // are exact in bf16 too.
+//
+// Bound by the cache's bytes: a wave goes over pages of its own (16 KB at 128 values a head) with its queries, running maxima, sums and
+// results in registers, and requests the next page's keys as soon as this one's are used up, its values as soon as these are.  A workgroup's
+// four waves join their parts through LDS.  Where rows x heads are few, a sequence's pages are split over workgroups too: each leaves
+// its rows' sums in the workspace, and the last of them to arrive (a counter there, back at 0 behind the call) joins them, in their order, so
+// the result does not depend on which that was.
+//   Measured (bf16, 32 heads on 8 of 128 values): one token over 131072, 268 MB: 57 us, 4.7 TB/s (a large copy moves 4.8); one token each
+// over 64 sequences of up to 4096, 269 MB: 60 us; over 4096: 10.7 us, of which the join takes 3.  Two pages on their way a wave, or eight
+// waves: no faster where bytes bound it, and 1 us slower on short sequences, where the conversions' instructions do (2 us a page with two
+// waves on a SIMD, 1 with one).
 #include "bmx_internal.h"
 #include "few_bits.h"
+
+#include <algorithm>
 
 namespace bmx {
 namespace {
 
-constexpr int kWaves = 4;
 
 // The upper halves of two dwords.
 __device__ inline uint32_t upper_halves(float a, float b) {
@@ -64,36 +75,106 @@ __device__ inline void pair(float a, float b, uint32_t (&part)[PARTS]) {
   }
 }
 
+// Numbers that workgroups of other XCDs read, each with an L2 of its own: written through and read past it (relaxed atomics of the device's
+// scope, eight bytes each), so nobody has to write back or throw away a whole L2, as a fence of that scope does: with __threadfence()
+// around plain accesses, 64 sequences in two splits ran for 325 us, 110 in one.
+__device__ inline void put(float* p, float a, float b) {
+  const uint64_t x = __builtin_bit_cast(uint32_t, a) | (uint64_t)__builtin_bit_cast(uint32_t, b) << 32;
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline u32x2 get(const float* p) {
+  return __builtin_bit_cast(u32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+__device__ inline f32x4 get4(const float* p) {
+  const u32x2 a = get(p), b = get(p + 2);
+  return __builtin_bit_cast(f32x4, u32x4{a[0], a[1], b[0], b[1]});
+}
+
 struct Args {
   const void* q;
   int64_t q_row, q_head;
   void* out;
   int64_t out_row, out_head;
   float* lse;
-  int q_heads, share, rows, max_new, window;
+  float* parts;      // [sequence, tile of rows, head][split][part_rows][ROW + 4]: the rows' results, maximum and sum
+  uint32_t* arrived; // [sequence, tile of rows, head]
+  int q_heads, share, rows, max_new, window, splits, part_rows;
   bool causal, aligned;
   float scale;
 };
+
+constexpr int kWaves = 4;
+constexpr int kCounters = 16384;  // of the workspace's head; what needs more than these has rows enough not to be split
+constexpr int kMostSplits = 128;
+
+using Rsrc = __amdgpu_buffer_rsrc_t;
+// A page as a buffer: reads behind its end (all of them, where there is no page) give zeros and cost nothing.
+__device__ inline Rsrc buffer(const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000); }
+__device__ inline u32x4 load16(Rsrc r, int lane_at, int at) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 0)); }
+__device__ inline u32x2 load8(Rsrc r, int lane_at, int at) { return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, lane_at, at, 0)); }
 
 template <int TYPE, int DC>
 __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache c, Args a) {
   constexpr int PARTS = TYPE == BMX_F32 ? 3 : 1, ROW = DC * 32, DT = DC * 2, WIDE = DC / 2;
   constexpr bool F16 = PARTS == 1;
-  __shared__ float red_o[kWaves][16][ROW + 4], red_m[kWaves][16], red_l[kWaves][16];
+  constexpr int LINE = ROW + 4;
+  __shared__ float red[kWaves * 16 * LINE], red_m[kWaves][16], red_l[kWaves][16], factor_of[kMostSplits][16], sum_of[kMostSplits][16];
+  __shared__ uint32_t place;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16;
-  const int head = blockIdx.x, seq = blockIdx.z;
+  const int head = blockIdx.x % c.heads, split = blockIdx.x / c.heads, seq = blockIdx.z;
   const KvSpan s = kv_span(c, seq, a.rows, a.max_new);
   const int r0 = blockIdx.y * 16;
   if (r0 >= s.count * a.share) return;
-  // this lane's row of queries, and what it sees: positions [low, high)
-  const int r = r0 + lane % 16, token = min(r / a.share, s.count - 1), pos = s.first + token;
-  const int high = a.causal ? min(pos + 1, s.length) : s.length;
-  const int low = a.window ? max(pos - a.window + 1, 0) : 0;
-  // what any row of the 16 sees
+  // what any, and what every one of the 16 rows sees: positions [low, high)
   const int tok0 = r0 / a.share, tok1 = min((r0 + 15) / a.share, s.count - 1);
-  const int high_any = a.causal ? min(s.first + tok1 + 1, s.length) : s.length;
-  const int low_any = a.window ? max(s.first + tok0 - a.window + 1, 0) : 0;
+  const int high_any = a.causal ? min(s.first + tok1 + 1, s.length) : s.length, high_all = a.causal ? min(s.first + tok0 + 1, s.length) : s.length;
+  const int low_any = a.window ? max(max(s.first + tok0, 0) - a.window + 1, 0) : 0, low_all = a.window ? max(max(s.first + tok1, 0) - a.window + 1, 0) : 0;
+  // this workgroup's pages
+  const int page0 = low_any / kPage, pages = max((high_any + kPage - 1) / kPage - page0, 0);
+  // (to join parts takes as long as two pages of a wave, so up to three pages each stay in one workgroup: 8 pages 7.8 us, in two 9.3;
+  // 16 pages 10.6, in four 9.3)
+  const int per = pages <= 3 * kWaves ? pages : max((pages + a.splits - 1) / a.splits, kWaves), used = pages > 0 ? (pages + per - 1) / per : 1;
+  if (split >= used) return;
+  const int begin = page0 + split * per, count = max(min(per, pages - split * per) - wave + kWaves - 1, 0) / kWaves;  // (of this wave, kWaves apart)
 
+  const int blocks = kPage / c.block, log_block = 31 - __builtin_clz(c.block);
+  const int64_t page_bytes = (int64_t)c.heads * 2 * kPage * ROW;
+  int ids = -1, next = 0;  // the numbers of 64 pages, a lane each; the place of the next page
+  int page, at;  // the page on its way, and its place
+  u32x4 k[4][WIDE > 0 ? WIDE : 1], v[DT];
+  u32x2 k_tail[4];
+  float scale_of;  // lanes 0 to 3: a page's scales of keys, a unit of 16 tokens each; 4 to 7: of values
+  const int scale_at = (lane / 4 % 2) * blocks + (lane % 4 * 16 >> log_block);
+  // the next of this wave's pages that is there, and its keys
+  const auto load_keys = [&] {
+    page = -1;
+    for (; next < count; ++next) {
+      if (next % 64 == 0) ids = next + lane < count ? kv_page(c, seq, begin + wave + (next + lane) * kWaves) : -1;
+      page = __builtin_amdgcn_readlane(ids, next % 64);
+      if (page >= 0) break;
+    }
+    at = next++;
+    const Rsrc r = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)head * 2 * kPage * ROW, page >= 0 ? kPage * ROW : 0);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int w = 0; w < WIDE; ++w) k[u][w] = load16(r, lane * 16, u * 16 * ROW + w * 1024);
+      if constexpr (DC % 2) k_tail[u] = load8(r, lane * 8, u * 16 * ROW + WIDE * 1024);
+    }
+    const Rsrc rs = buffer(c.scales + ((int64_t)max(page, 0) * c.heads + head) * 2 * blocks, page >= 0 ? 8 * blocks : 0);
+    scale_of = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, scale_at * 4, 0, 0));
+  };
+  const auto load_values = [&] {
+    const Rsrc r = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)(head * 2 + 1) * kPage * ROW, page >= 0 ? kPage * ROW : 0);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) v[dt] = load16(r, lane * 16, dt * 1024);
+  };
+  load_keys();
+  load_values();
+
+  // this lane's row of queries
+  const int r = r0 + lane % 16, token = min(r / a.share, s.count - 1), pos = s.first + token;
+  const int high = a.causal ? min(pos + 1, s.length) : s.length, low = a.window ? max(max(pos, 0) - a.window + 1, 0) : 0;
   u32x4 q[PARTS][DC];
   float factor;
   {
@@ -126,43 +207,54 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
       }
   }
 
-  const int blocks = kPage / c.block, log_block = 31 - __builtin_clz(c.block);
   float m = -INFINITY, l = 0.0f, most = 0.0f;
   f32x4 o[DT] = {};
-  for (int pg = low_any / kPage + wave; pg * kPage < high_any; pg += kWaves) {
-    const int page = kv_page(c, seq, pg);
-    if (page < 0) continue;
-    const int64_t unit = ((int64_t)page * c.heads + head) * 2;
-    const int8_t* keys = c.pages + unit * kPage * ROW;
-    const int8_t* values = keys + kPage * ROW;
-    const float* ks = c.scales + unit * blocks;
-    const float* vs = ks + blocks;
-    float p[4][4], vscale[4], top = -INFINITY, most_new = most;
+  while (page >= 0) {
+    const int t0 = (begin + wave + at * kWaves) * kPage;
+    float p[4][4], key_scale[4], value_scale[4], top = -INFINITY, most_new = most;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      key_scale[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale_of), u));
+      value_scale[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale_of), 4 + u));
+    }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       f32x4 z = {};
 #pragma unroll
       for (int w = 0; w < WIDE; ++w) {
-        const u32x4 k = *reinterpret_cast<const u32x4*>(keys + u * 16 * ROW + w * 1024 + lane * 16);
-        const u32x4 k0 = eight_levels<F16>(k[0], k[1]), k1 = eight_levels<F16>(k[2], k[3]);
+        const u32x4 k0 = eight_levels<F16>(k[u][w][0], k[u][w][1]), k1 = eight_levels<F16>(k[u][w][2], k[u][w][3]);
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) z = mfma<F16>(k1, q[part][2 * w + 1], mfma<F16>(k0, q[part][2 * w], z));
       }
       if constexpr (DC % 2) {
-        const u32x2 k = *reinterpret_cast<const u32x2*>(keys + u * 16 * ROW + WIDE * 1024 + lane * 8);
-        const u32x4 k0 = eight_levels<F16>(k[0], k[1]);
+        const u32x4 k0 = eight_levels<F16>(k_tail[u][0], k_tail[u][1]);
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) z = mfma<F16>(k0, q[part][DC - 1], z);
       }
-      const int at = pg * kPage + 16 * u, b = 16 * u >> log_block;
-      const float f = factor * ks[b];
-      vscale[u] = at < high_any && at + 16 > low_any ? vs[b] : 0.0f;  // (a block that nobody has written has any scale)
-      most_new = fmaxf(most_new, vscale[u]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = at + 4 * g + i;
-        p[u][i] = t < high && t >= low ? z[i] * f : -INFINITY;
-        top = fmaxf(top, p[u][i]);
+      for (int i = 0; i < 4; ++i) p[u][i] = z[i];
+    }
+    load_keys();
+    if (t0 >= low_all && t0 + kPage <= high_all) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float f = factor * key_scale[u];
+        most_new = fmaxf(most_new, value_scale[u]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, p[u][i] *= f);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int t = t0 + 16 * u;
+        const float f = factor * key_scale[u];
+        if (t >= high_any || t + 16 <= low_any) value_scale[u] = 0.0f;  // (a block that nobody has written has any scale)
+        most_new = fmaxf(most_new, value_scale[u]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[u][i] = t + 4 * g + i < high && t + 4 * g + i >= low ? p[u][i] * f : -INFINITY;
+          top = fmaxf(top, p[u][i]);
+        }
       }
     }
     top = fmaxf(top, __shfl_xor(top, 16));
@@ -177,7 +269,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
     u32x4 w[PARTS][2];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const float f = F16 ? vscale[u] * inverse * 0x1p14f : vscale[u];
+      const float f = F16 ? value_scale[u] * inverse * 0x1p14f : value_scale[u];
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
         const float e0 = __builtin_amdgcn_exp2f(p[u][i] - m_at), e1 = __builtin_amdgcn_exp2f(p[u][i + 1] - m_at);
@@ -191,62 +283,165 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
     l = l * shrink + sum;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(values + dt * 1024 + lane * 16);
-      const u32x4 v0 = eight_levels<F16>(v[0], v[1]), v1 = eight_levels<F16>(v[2], v[3]);
+      const u32x4 v0 = eight_levels<F16>(v[dt][0], v[dt][1]), v1 = eight_levels<F16>(v[dt][2], v[dt][3]);
       o[dt] *= shrink_o;
 #pragma unroll
       for (int part = 0; part < PARTS; ++part) o[dt] = mfma<F16>(v1, w[part][1], mfma<F16>(v0, w[part][0], o[dt]));
     }
+    load_values();
   }
 
+  // the four waves' parts
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   if (g == 0) red_m[wave][lane] = m, red_l[wave][lane] = l;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) red_o[wave][lane % 16][dt * 16 + 4 * g + i] = F16 ? o[dt][i] * (most * 0x1p-14f) : o[dt][i];
+    *reinterpret_cast<f32x4*>(&red[(wave * 16 + lane % 16) * LINE + dt * 16 + 4 * g]) = F16 ? o[dt] * (most * 0x1p-14f) : o[dt];
   __syncthreads();
-  for (int e = threadIdx.x; e < 16 * ROW; e += kWaves * 64) {
-    const int i = e / ROW, d = e % ROW, rr = r0 + i;
-    if (rr >= s.count * a.share || d >= c.dim) continue;
-    float top = -INFINITY, sum = 0.0f, v = 0.0f;
+  const int rows = min(s.count * a.share - r0, 16), quads = rows * (ROW / 4);
+  const int64_t unit = ((int64_t)seq * gridDim.y + blockIdx.y) * c.heads + head;
+  float* parts = a.parts + unit * a.splits * a.part_rows * LINE;
+  const auto store = [&](int i, int d, f32x4 x, float top, float sum) {
+    const int64_t t = s.row0 + (r0 + i) / a.share;
+    const int h = head * a.share + (r0 + i) % a.share;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)  // (a row that sees nothing is zeros)
+      if (d + j < c.dim) store_one<TYPE>(a.out, t * a.out_row + h * a.out_head + d + j, sum == 0.0f ? 0.0f : x[j] / sum);
+    if (a.lse && d == 0) a.lse[t * a.q_heads + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  };
+  for (int e = threadIdx.x; e < quads; e += kWaves * 64) {
+    const int i = e / (ROW / 4), d = e % (ROW / 4) * 4;
+    float top = -INFINITY, sum = 0.0f;
+    f32x4 x = {};
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, red_m[w][i]);
-    const float at = top == -INFINITY ? 0.0f : top;
+    const float m_at = top == -INFINITY ? 0.0f : top;
     for (int w = 0; w < kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(red_m[w][i] - at);
+      const float f = __builtin_amdgcn_exp2f(red_m[w][i] - m_at);
       sum += f * red_l[w][i];
-      v += f * red_o[w][i][d];
+      x += f * *reinterpret_cast<const f32x4*>(&red[(w * 16 + i) * LINE + d]);
     }
-    const int64_t t = s.row0 + rr / a.share;
-    const int h = head * a.share + rr % a.share;
-    // (a row that sees nothing is zeros)
-    store_one<TYPE>(a.out, t * a.out_row + h * a.out_head + d, sum == 0.0f ? 0.0f : v / sum);
-    if (a.lse && d == 0) a.lse[t * a.q_heads + h] = sum == 0.0f ? -INFINITY : (at + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+    if (used == 1) {
+      store(i, d, x, m_at, sum);
+    } else {
+      float* line = parts + ((int64_t)split * a.part_rows + i) * LINE;
+      put(line + d, x[0], x[1]), put(line + d + 2, x[2], x[3]);
+      if (d == 0) put(line + ROW, top, sum);
+    }
+  }
+  if (used == 1) return;
+
+  // the workgroups' parts: the last to arrive joins them
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's numbers are there
+  __syncthreads();
+  if (threadIdx.x == 0) place = __hip_atomic_fetch_add(a.arrived + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (place != (uint32_t)used - 1) return;
+  if (threadIdx.x == 0) __hip_atomic_store(a.arrived + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // (every read of a step at once: each is a trip to memory)
+  for (int e = threadIdx.x; e < used * 16; e += kWaves * 64) {
+    const int p = e / 16, i = e % 16;
+    if (i >= rows) continue;
+    const float* line = parts + ((int64_t)p * a.part_rows + i) * LINE;
+    const u32x2 x = get(line + ROW);
+    const uint32_t top = x[0], sum = x[1];
+    factor_of[p][i] = __builtin_bit_cast(float, top), sum_of[p][i] = __builtin_bit_cast(float, sum);
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {  // a row's maximum and sum, four lanes to a row, and what each part counts for
+    const int i = threadIdx.x / 4, sub = threadIdx.x % 4;
+    float top = -INFINITY, sum = 0.0f;
+    for (int p = sub; p < used; p += 4) top = fmaxf(top, factor_of[p][i]);
+    top = fmaxf(top, __shfl_xor(top, 1));
+    top = fmaxf(top, __shfl_xor(top, 2));
+    const float m_at = top == -INFINITY ? 0.0f : top;
+    for (int p = sub; p < used; p += 4) {
+      const float f = __builtin_amdgcn_exp2f(factor_of[p][i] - m_at);
+      factor_of[p][i] = f;
+      sum += f * sum_of[p][i];
+    }
+    sum += __shfl_xor(sum, 1);
+    sum += __shfl_xor(sum, 2);
+    if (sub == 0) red_m[0][i] = m_at, red_l[0][i] = sum;
+  }
+  __syncthreads();
+  // the results, four values to a thread; where they are fewer than threads, the parts are dealt out too
+  const int deal = max(kWaves * 64 / quads, 1);
+  for (int e = threadIdx.x; e < quads * deal; e += kWaves * 64) {
+    const int i = e % quads / (ROW / 4), d = e % quads % (ROW / 4) * 4;
+    f32x4 x = {};
+    for (int p = e / quads; p < used; p += 8 * deal) {
+      f32x4 y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = get4(parts + ((int64_t)min(p + j * deal, used - 1) * a.part_rows + i) * LINE + d);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x += (p + j * deal < used ? factor_of[min(p + j * deal, used - 1)][i] : 0.0f) * y[j];
+    }
+    *reinterpret_cast<f32x4*>(&red[e * 4]) = x;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < quads; e += kWaves * 64) {
+    f32x4 x = {};
+    for (int p = 0; p < deal; ++p) x += *reinterpret_cast<const f32x4*>(&red[(p * quads + e) * 4]);
+    const int i = e / (ROW / 4);
+    store(i, e % (ROW / 4) * 4, x, red_m[0][i], red_l[0][i]);
   }
 }
 
-template <int TYPE>
-void launch_typed(const bmx_kv_cache& c, const Args& a, hipStream_t s) {
-  const dim3 grid(c.heads, (uint32_t)ceil_div((int64_t)a.max_new * a.share, 16), c.sequences);
-  const int dc = kv_row_bytes(c.dim) / 32;
-  const auto kern = dc == 1 ? kv_attention_kernel<TYPE, 1> : dc == 2 ? kv_attention_kernel<TYPE, 2> : dc == 3 ? kv_attention_kernel<TYPE, 3>
-                  : dc == 4 ? kv_attention_kernel<TYPE, 4> : dc == 5 ? kv_attention_kernel<TYPE, 5> : dc == 6 ? kv_attention_kernel<TYPE, 6>
-                  : dc == 7 ? kv_attention_kernel<TYPE, 7> : kv_attention_kernel<TYPE, 8>;
-  launch_kernel(kern, grid, dim3(kWaves * 64), 0, s, c, a);
-  note_kernel("kv_attention_kernel<%d,%d> grid %ux%ux%u block %d", TYPE, dc, grid.x, grid.y, grid.z, kWaves * 64);
+// What a call needs: tiles of rows, splits, and bytes of the workspace.
+struct Plan {
+  int64_t units, tiles;
+  int splits, part_rows;
+  size_t bytes;
+};
+Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new) {
+  Plan p;
+  const int64_t rows = max_new * (q_heads / heads);
+  p.tiles = ceil_div(rows, 16);
+  p.units = sequences * heads * p.tiles;
+  p.part_rows = (int)std::min<int64_t>(rows, 16);
+  // One workgroup for each of the chip's 256 CUs, but four pages of the longest sequence for each at least.  One token over 131072 with 256, 512,
+  // 1024 workgroups: 57, 60, 67 us; over 16384: 17, 23, 23.
+  p.splits = (int)std::max<int64_t>(std::min({ceil_div(256, std::max<int64_t>(p.units, 1)), ceil_div(table_width, 4), (int64_t)kMostSplits}), 1);
+  if (p.units > kCounters) p.splits = 1;
+  p.bytes = p.splits == 1 ? 0 : kCounters * 4 + (size_t)p.units * p.splits * p.part_rows * (kv_row_bytes((int)dim) + 4) * 4;
+  return p;
 }
+
+template <int TYPE, int DC>
+void launch(const bmx_kv_cache& c, const Args& a, int64_t tiles, hipStream_t s) {
+  const dim3 grid(c.heads * a.splits, (uint32_t)tiles, c.sequences), block(kWaves * 64);
+  launch_kernel(kv_attention_kernel<TYPE, DC>, grid, block, 0, s, c, a);
+  note_kernel("kv_attention_kernel<%d,%d> grid %ux%ux%u block %u", TYPE, DC, grid.x, grid.y, grid.z, block.x);
+}
+template <int TYPE>
+void launch_typed(const bmx_kv_cache& c, const Args& a, int64_t tiles, hipStream_t s) {
+  const int dc = kv_row_bytes(c.dim) / 32;
+  const auto f = dc == 1 ? launch<TYPE, 1> : dc == 2 ? launch<TYPE, 2> : dc == 3 ? launch<TYPE, 3> : dc == 4 ? launch<TYPE, 4>
+               : dc == 5 ? launch<TYPE, 5> : dc == 6 ? launch<TYPE, 6> : dc == 7 ? launch<TYPE, 7> : launch<TYPE, 8>;
+  f(c, a, tiles, s);
+}
+
+__global__ void clear_kernel(uint32_t* p) { p[blockIdx.x * 256 + threadIdx.x] = 0; }
 
 }  // namespace
 
+size_t kv_attention_workspace(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new) {
+  return plan(sequences, table_width, heads, q_heads, dim, max_new).bytes;
+}
+
 hipError_t launch_kv_attention(const bmx_kv_cache& c, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int rows,
                                int max_new, float scale, bool causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
-                               hipStream_t s) {
+                               void* workspace, bool fresh, hipStream_t s) {
   const int64_t size = type_bytes(type);
   const bool aligned = (uintptr_t)q % 16 == 0 && q_row * size % 16 == 0 && q_head * size % 16 == 0;
-  const Args a = {q, q_row, q_head, out, out_row, out_head, lse, q_heads, q_heads / c.heads, rows, max_new, window, causal, aligned, scale};
+  const Plan p = plan(c.sequences, c.table_width, c.heads, q_heads, c.dim, max_new);
+  uint32_t* arrived = static_cast<uint32_t*>(workspace);
+  const Args a = {q, q_row, q_head, out, out_row, out_head, lse, reinterpret_cast<float*>(arrived + kCounters), arrived, q_heads,
+                  q_heads / c.heads, rows, max_new, window, p.splits, p.part_rows, causal, aligned, scale};
+  if (fresh && p.splits > 1) launch_kernel(clear_kernel, dim3((uint32_t)ceil_div(p.units, 256)), dim3(256), 0, s, arrived);
   const auto f = type == BMX_F32 ? launch_typed<BMX_F32> : type == BMX_F16 ? launch_typed<BMX_F16> : launch_typed<BMX_BF16>;
-  f(c, a, s);
+  f(c, a, p.tiles, s);
   return launch_error();
 }
 

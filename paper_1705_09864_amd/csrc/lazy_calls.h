@@ -23,7 +23,8 @@ int bmx_lazy_binary_conv2d_bits(const uint64_t* xp, int N, int C, int H, int W, 
 int bmx_lazy_quant_gemm(const float* a, int64_t lda, int bits_a, const float* w, int64_t ldw, int bits_w, int M, int N,
                         int K, int32_t* out_i32_scaled, float* out_f32, int64_t ldo, void* workspace,
                         size_t workspace_bytes, void* stream);
-int bmx_lazy_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
-                          int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
-                          void* workspace, size_t workspace_bytes, void* stream);
+// bmx_kv_attention on a workspace whose memory is just allocated: the call clears what it needs.
+int bmx_fresh_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
+                           int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
 }
