@@ -98,4 +98,19 @@ __device__ static inline int kv_key_at(int row, int t, int d) {
 }
 __device__ static inline int kv_value_at(int t, int d) { return d / 16 * 1024 + t % 16 / 4 * 256 + d % 16 * 16 + t / 16 * 4 + t % 4; }
 
+// Memory as a buffer of so many bytes: a read behind its end gives zeros and moves nothing.
+using Rsrc = __amdgpu_buffer_rsrc_t;
+__device__ inline Rsrc buffer(const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000); }
+// (lane_at differs from lane to lane, at does not)
+__device__ inline u32x4 load16(Rsrc r, int lane_at, int at) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 0)); }
+__device__ inline u32x2 load8(Rsrc r, int lane_at, int at) { return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, lane_at, at, 0)); }
+__device__ inline uint32_t load4(Rsrc r, int lane_at, int at) { return __builtin_amdgcn_raw_buffer_load_b32(r, lane_at, at, 0); }
+
+// The upper halves of two dwords.
+__device__ inline uint32_t upper_halves(float a, float b) {
+  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
+}
+// What the upper half of a value leaves.
+__device__ inline float lower_part(float a) { return a - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, a) & 0xffff0000u); }
+
 }  // namespace bmx

@@ -29,10 +29,6 @@ namespace bmx {
 namespace {
 
 
-// The upper halves of two dwords.
-__device__ inline uint32_t upper_halves(float a, float b) {
-  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
-}
 // Four levels of a dword as pairs of 16-bit floats.
 template <bool F16>
 __device__ inline u32x2 four_levels(uint32_t w) {
@@ -69,8 +65,7 @@ __device__ inline void pair(float a, float b, uint32_t (&part)[PARTS]) {
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
       part[p] = upper_halves(a, b);
-      a -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, a) & 0xffff0000u);
-      b -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, b) & 0xffff0000u);
+      a = lower_part(a), b = lower_part(b);
     }
   }
 }
@@ -106,12 +101,6 @@ struct Args {
 constexpr int kWaves = 4;
 constexpr int kCounters = 16384;  // of the workspace's head; what needs more than these has rows enough not to be split
 constexpr int kMostSplits = 128;
-
-using Rsrc = __amdgpu_buffer_rsrc_t;
-// A page as a buffer: reads behind its end (all of them, where there is no page) give zeros and cost nothing.
-__device__ inline Rsrc buffer(const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000); }
-__device__ inline u32x4 load16(Rsrc r, int lane_at, int at) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 0)); }
-__device__ inline u32x2 load8(Rsrc r, int lane_at, int at) { return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, lane_at, at, 0)); }
 
 template <int TYPE, int DC>
 __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache c, Args a) {
@@ -162,7 +151,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
       if constexpr (DC % 2) k_tail[u] = load8(r, lane * 8, u * 16 * ROW + WIDE * 1024);
     }
     const Rsrc rs = buffer(c.scales + ((int64_t)max(page, 0) * c.heads + head) * 2 * blocks, page >= 0 ? 8 * blocks : 0);
-    scale_of = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, scale_at * 4, 0, 0));
+    scale_of = __builtin_bit_cast(float, load4(rs, scale_at * 4, 0));
   };
   const auto load_values = [&] {
     const Rsrc r = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)(head * 2 + 1) * kPage * ROW, page >= 0 ? kPage * ROW : 0);

@@ -4,26 +4,36 @@
 // nibbles (the four bits are the highest of the mantissa of 16.0), so that with S = sum over g of x (a product with ones)
 //   y += s_g * ((16 + q) . x) + (b_g - 16 s_g) * S,
 // both sums in 32 bits.  x stays what it is: bf16 and f16 have matrix-core products of their own, and an f32 value goes in as
-// three bf16 parts (24 bits together).
+// three bf16 parts (24 bits together), against q - 8.
 #include "bmx_internal.h"
 #include "few_bits.h"
+
+#include <algorithm>
 
 namespace bmx {
 namespace {
 
-constexpr int kWaves = 8;
-
-// The 32 levels of a lane's 16 bytes at step `step` (eight of them), as 16 + q.
+// The bits of 16.0 in both halves, in a register: beside a literal v_and_or_b32 takes no other, and would fall into two instructions.
 template <bool F16>
-__device__ inline u32x4 levels(uint32_t w) {
-  // (field p of the low half and of the high half, onto the mantissa's highest four bits)
-  if constexpr (F16) {
-    constexpr uint32_t m = 0x03C003C0, one = 0x4C004C00;
-    return u32x4{((w << 6) & m) | one, ((w << 2) & m) | one, ((w >> 2) & m) | one, ((w >> 6) & m) | one};
-  } else {
-    constexpr uint32_t m = 0x00780078, one = 0x41804180;
-    return u32x4{((w << 3) & m) | one, ((w >> 1) & m) | one, ((w >> 5) & m) | one, ((w >> 9) & m) | one};
+__device__ inline uint32_t sixteen() {
+  uint32_t x = F16 ? 0x4C004C00 : 0x41804180;
+  asm volatile("" : "+v"(x));
+  return x;
+}
+// A lane's eight levels of a step, as 16 + q: field p of either half onto the mantissa's highest four bits.  For f32 results as q - 8, which
+// costs two instructions a value more and keeps the sums small beside their result (error of 1 x 256 x 512 against 64 bits 7.6e-7, so 0.9e-7).
+template <int TYPE>
+constexpr float kZero = TYPE == BMX_F32 ? 8.0f : -16.0f;  // what q is more than the operand
+template <int TYPE>
+__device__ inline u32x4 levels(uint32_t w, uint32_t one) {
+  constexpr uint32_t m = TYPE == BMX_F16 ? 0x03C003C0 : 0x00780078;
+  if constexpr (TYPE == BMX_F16) return u32x4{((w << 6) & m) | one, ((w << 2) & m) | one, ((w >> 2) & m) | one, ((w >> 6) & m) | one};
+  u32x4 x = {((w << 3) & m) | one, ((w >> 1) & m) | one, ((w >> 5) & m) | one, ((w >> 9) & m) | one};
+  if constexpr (TYPE == BMX_F32) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = upper_halves(__builtin_bit_cast(float, x[j] << 16) - 24.0f, __builtin_bit_cast(float, x[j] & 0xffff0000u) - 24.0f);
   }
+  return x;
 }
 
 template <bool F16>
@@ -34,82 +44,141 @@ __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// Eight values of x as matrix-core operands: one, or three bf16 parts of f32 values.
+// Eight values of x as they lie in memory, and as matrix-core operands: themselves, or three bf16 parts of f32 values, 8 bits each, cut off
+// and not rounded (together they are the value).
 template <int TYPE>
-__device__ inline void operand(const void* x, int64_t at, int left, bool aligned, u32x4 (&part)[TYPE == BMX_F32 ? 3 : 1]) {
-  if constexpr (TYPE != BMX_F32) {
-    if (left >= 8 && aligned) {
-      part[0] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(x) + at);
-    } else {
-      uint32_t h[8];
+struct Eight {
+  static constexpr int kParts = TYPE == BMX_F32 ? 3 : 1;
+  u32x4 raw[TYPE == BMX_F32 ? 2 : 1];
+
+  // (unaligned: the address is one of an element)
+  __device__ void load(const void* x, int64_t at) {
+    struct __attribute__((packed, aligned(TYPE == BMX_F32 ? 4 : 2))) Raw {
+      u32x4 v[TYPE == BMX_F32 ? 2 : 1];
+    };
+    const Raw r = *reinterpret_cast<const Raw*>(static_cast<const char*>(x) + at * (TYPE == BMX_F32 ? 4 : 2));
 #pragma unroll
-      for (int j = 0; j < 8; ++j) h[j] = j < left ? static_cast<const uint16_t*>(x)[at + j] : 0;
+    for (int i = 0; i < (TYPE == BMX_F32 ? 2 : 1); ++i) raw[i] = r.v[i];
+  }
+  // `left` values are there, the others are 0.
+  __device__ void load(const void* x, int64_t at, int left) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) part[0][j] = h[2 * j] | h[2 * j + 1] << 16;
-    }
-  } else {
-    float v[8];
-    load_eight<TYPE>(x, at, left, aligned, v);
-#pragma unroll
-    for (int p = 0; p < 3; ++p) {
-      uint32_t h[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        h[j] = bf16_bits(v[j]);
-        v[j] -= bf16_float(h[j]);
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (TYPE == BMX_F32) {
+        raw[j / 4][j % 4] = j < left ? static_cast<const uint32_t*>(x)[at + j] : 0;
+      } else {
+        const uint32_t h = j < left ? static_cast<const uint16_t*>(x)[at + j] : 0;
+        raw[0][j / 2] = j % 2 ? raw[0][j / 2] | h << 16 : h;
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) part[p][j] = h[2 * j] | h[2 * j + 1] << 16;
     }
   }
-}
+  __device__ void parts(u32x4 (&part)[kParts]) const {
+    if constexpr (TYPE != BMX_F32) {
+      part[0] = raw[0];
+    } else {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t bits = raw[j / 4][j % 4];
+        v[j] = __builtin_bit_cast(float, bits);
+      }
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part[p][j] = upper_halves(v[2 * j], v[2 * j + 1]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = lower_part(v[j]);
+      }
+    }
+  }
+};
 
-// 16 outputs x 16 MT rows per workgroup, K dealt out to its waves in steps of 128 (1 KB of weights, 16 bytes a lane).
+constexpr int kMostWaves = 8;
+
+// 16 outputs x 16 MT rows per workgroup, K dealt out to its waves in steps of 128 (1 KB of weights, 16 bytes a lane).  Each wave has DEPTH
+// steps on their way: a step's registers are loaded for the step DEPTH further on as soon as they are used up.
 template <int TYPE, int MT, int GROUP>
-__global__ __launch_bounds__(kWaves * 64) void w4_rows_kernel(const void* x, int64_t ldx, bool aligned, const u32x4* tiles,
-                                                              const uint32_t* scales, const float* bias, int M, int N, int K,
-                                                              void* out, int64_t ldo) {
+__global__ __launch_bounds__(kMostWaves * 64) void w4_rows_kernel(const void* x, int64_t ldx, const u32x4* tiles, const uint32_t* scales,
+                                                                  const float* bias, int M, int N, int K, void* out, int64_t ldo) {
   constexpr bool F16 = TYPE == BMX_F16;
-  constexpr int PARTS = TYPE == BMX_F32 ? 3 : 1, PER = 128 / GROUP, STEPS = GROUP / 32;
+  constexpr int PARTS = Eight<TYPE>::kParts, PER = 128 / GROUP, STEPS = GROUP / 32, DEPTH = MT == 1 && TYPE != BMX_F32 ? 4 : 2;
   constexpr uint32_t one = F16 ? 0x3C003C00 : 0x3F803F80;
-  __shared__ f32x4 red[kWaves][MT][64];
+  __shared__ f32x4 red[kMostWaves][MT][64];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
-  const int g = lane / 16, nt = blockIdx.x, m0 = blockIdx.y * 16 * MT, kt_all = (K + 127) / 128;
+  const int g = lane / 16, nt = blockIdx.x, m0 = blockIdx.y * 16 * MT, full = K / 128, all = (K + 127) / 128;
   const u32x4 ones = {one, one, one, one};
   int64_t row[MT];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) row[i] = (int64_t)min(m0 + 16 * i + lane % 16, M - 1) * ldx;  // (rows past the last: not stored)
+  for (int i = 0; i < MT; ++i) row[i] = (int64_t)min(m0 + 16 * i + lane % 16, M - 1) * ldx + 8 * g;  // (rows past the last: not stored)
+  const Rsrc tile_rows = buffer(tiles + (int64_t)nt * all * 64, full * 1024), scale_rows = buffer(scales + (int64_t)nt * all * PER * 16, all * PER * 64);
   f32x4 acc[MT] = {};
-  for (int kt = wave; kt < kt_all; kt += waves) {
-    const int64_t tile = (int64_t)nt * kt_all + kt;
-    const u32x4 w = tiles[tile * 64 + lane];
+  const uint32_t sixteens = sixteen<F16>();
+  u32x4 w[DEPTH], sb[DEPTH][PER];
+  Eight<TYPE> xs[DEPTH][MT][4];
+  const auto load = [&](int d, int kt) {
+    w[d] = load16(tile_rows, lane * 16, kt * 1024);
+#pragma unroll
+    for (int gi = 0; gi < PER; ++gi) sb[d][gi] = load16(scale_rows, g * 16, (kt * PER + gi) * 64);
+  };
+  const auto load_x = [&](int d, int kt, int i, int step) { xs[d][i][step].load(x, row[i] + min(kt, full - 1) * 128 + 32 * step); };
+  // a step's products; next: the step to load in its place
+  const auto multiply = [&](int d, int groups, int next) {
 #pragma unroll
     for (int gi = 0; gi < PER; ++gi) {
-      if (kt * 128 + gi * GROUP >= K) break;  // (whatever scales lie there)
-      const u32x4 sb = *reinterpret_cast<const u32x4*>(scales + (tile * PER + gi) * 16 + 4 * g);
+      if (gi >= groups) break;  // (whatever scales lie behind the last group)
       f32x4 dot[MT] = {}, sum[MT] = {};
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) {
-        const int step = gi * STEPS + st, k = kt * 128 + 32 * step + 8 * g;
-        const u32x4 a = levels<F16>(w[step]);
+        const int step = gi * STEPS + st;
+        const u32x4 a = levels<TYPE>(w[d][step], sixteens);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           u32x4 b[PARTS];
-          operand<TYPE>(x, row[i] + k, K - k, aligned, b);
+          xs[d][i][step].parts(b);
 #pragma unroll
           for (int p = 0; p < PARTS; ++p) {
             dot[i] = mfma<F16>(a, b[p], dot[i]);
             sum[i] = mfma<F16>(ones, b[p], sum[i]);
           }
+          if (next >= 0) load_x(d, next, i, step);
         }
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float s = bf16_float(sb[j]), o = __builtin_bit_cast(float, sb[j] & 0xffff0000) - 16.0f * s;
+        const float s = bf16_float(sb[d][gi][j]), o = __builtin_bit_cast(float, sb[d][gi][j] & 0xffff0000) + kZero<TYPE> * s;
 #pragma unroll
         for (int i = 0; i < MT; ++i) acc[i][j] += s * dot[i][j] + o * sum[i][j];
       }
     }
+    if (next >= 0) load(d, next);
+  };
+  if (wave < full) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      const int kt = wave + d * waves;
+      load(d, kt);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int step = 0; step < 4; ++step) load_x(d, kt, i, step);
+    }
+    for (int kt = wave; kt < full;) {
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        if (kt < full) multiply(d, PER, kt + DEPTH * waves);
+        kt += waves;
+      }
+    }
+  }
+  if (full < all && wave == full % waves) {  // the last step, of fewer than 128 values
+    w[0] = tiles[((int64_t)nt * all + full) * 64 + lane];
+#pragma unroll
+    for (int gi = 0; gi < PER; ++gi) sb[0][gi] = load16(scale_rows, g * 16, (full * PER + gi) * 64);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int step = 0; step < 4; ++step) xs[0][i][step].load(x, row[i] + full * 128 + 32 * step, K - (full * 128 + 32 * step + 8 * g));
+    multiply(0, (K - full * 128 + GROUP - 1) / GROUP, -1);
   }
 #pragma unroll
   for (int i = 0; i < MT; ++i) red[wave][i][lane] = acc[i];
@@ -117,7 +186,8 @@ __global__ __launch_bounds__(kWaves * 64) void w4_rows_kernel(const void* x, int
   for (int e = threadIdx.x; e < 256 * MT; e += blockDim.x) {
     const int m = e / 16, n = e % 16;
     float v = 0.0f;
-    for (int w = 0; w < waves; ++w) v += red[w][m / 16][m % 16 + 16 * (n / 4)][n % 4];
+#pragma unroll
+    for (int w = 0; w < kMostWaves; ++w) v += w < waves ? red[w][m / 16][m % 16 + 16 * (n / 4)][n % 4] : 0.0f;
     if (m0 + m < M && nt * 16 + n < N) {
       if (bias) v += bias[nt * 16 + n];
       store_one<TYPE>(out, (int64_t)(m0 + m) * ldo + nt * 16 + n, v);
@@ -126,22 +196,399 @@ __global__ __launch_bounds__(kWaves * 64) void w4_rows_kernel(const void* x, int
 }
 
 template <int TYPE, int MT>
-void launch_rows(const void* x, int64_t ldx, bool aligned, const void* tiles, const void* scales, int group, const float* bias, int M,
-                 int N, int K, void* out, int64_t ldo, hipStream_t s) {
-  const dim3 grid((N + 15) / 16, (M + 16 * MT - 1) / (16 * MT)), block(64 * min(kWaves, (K + 127) / 128));
+void launch_rows(const void* x, int64_t ldx, const void* tiles, const void* scales, int group, const float* bias, int M, int N, int K,
+                 void* out, int64_t ldo, hipStream_t s) {
+  // Four waves; eight where a CU has one workgroup and each wave many steps (1 x 4096 x 9216: 8.2 -> 7.8 us; x 4096: 5.0 -> 5.2).
+  const dim3 grid((N + 15) / 16, (M + 16 * MT - 1) / (16 * MT));
+  const dim3 block(64 * std::min(grid.x * grid.y <= 256 && K >= 8192 ? 8 : 4, (K + 127) / 128));
   auto* t = static_cast<const u32x4*>(tiles);
   auto* sc = static_cast<const uint32_t*>(scales);
   const auto kern = group == 32 ? w4_rows_kernel<TYPE, MT, 32> : group == 64 ? w4_rows_kernel<TYPE, MT, 64> : w4_rows_kernel<TYPE, MT, 128>;
-  launch_kernel(kern, grid, block, 0, s, x, ldx, aligned, t, sc, bias, M, N, K, out, ldo);
+  launch_kernel(kern, grid, block, 0, s, x, ldx, t, sc, bias, M, N, K, out, ldo);
   note_kernel("w4_rows_kernel<%d,%d,%d> grid %dx%d block %d", TYPE, MT, group, (int)grid.x, (int)grid.y, (int)block.x);
 }
 
+// ---- many rows ----
+
+using f32x16 = float __attribute__((ext_vector_type(16)));
+template <bool F16>
+__device__ inline f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+template <int CTRL>
+__device__ inline float add_lane(float x) {  // x plus that of the lane which a row's permutation names
+  const int other = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, false);
+  return x + __builtin_bit_cast(float, other);
+}
+
+// f32: 64 x 128 of y per workgroup of 2 x 2 waves, 32 x 64 each.  x passes through registers, a step of 64 values ahead, into LDS in its three
+// parts; the sums over groups, which the offsets take, are made on that way.
+template <int GROUP>
+__global__ __launch_bounds__(256) void w4_f32_kernel(const void* x, int64_t ldx, const u32x4* tiles, const uint32_t* scales,
+                                                      const float* bias, int M, int N, int K, void* out, int64_t ldo) {
+  constexpr int PARTS = 3, RB = 1, CB = 2, KS = 64, CH = KS / 8, BM = 64 * RB;  // values, and chunks of eight of them, of a step
+  constexpr int G = GROUP < KS ? GROUP : KS, PER = KS / G, PER_TILE = 128 / GROUP, MINE = BM * CH / 256;
+  __shared__ u32x4 xs[2][PARTS][BM * CH];
+  __shared__ float sums[2][PER][BM];
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), h = lane / 32, wm = wave / 2, wn = wave % 2;
+  const int all = (K + 127) / 128, steps = (K + KS - 1) / KS;
+  // Tiles in bands of eight tiles of rows, dealt out so that an XCD (every eighth workgroup) has tiles side by side.
+  const int mt = (M + BM - 1) / BM, ntl = (N + 64 * CB - 1) / (64 * CB), total = mt * ntl, eighth = (total + 7) / 8;
+  const int id = blockIdx.x % 8 * eighth + blockIdx.x / 8;
+  if (id >= total || (int)(blockIdx.x / 8) >= eighth) return;
+  const int band = id / (8 * ntl), in_band = id - band * 8 * ntl, high = min(8, mt - band * 8);
+  const int m0 = (band * 8 + in_band % high) * BM, n0 = in_band / high * 64 * CB;
+
+  int64_t row[MINE];
+#pragma unroll
+  for (int i = 0; i < MINE; ++i) row[i] = (int64_t)min(m0 + (tid + 256 * i) / CH, M - 1) * ldx + tid % CH * 8;
+  int64_t tile[CB];
+  int col[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c) {
+    col[c] = n0 + (wn * CB + c) * 32 + lane % 32;
+    tile[c] = (int64_t)min(col[c] / 16, (N - 1) / 16) * all;
+  }
+  Eight<BMX_F32> in[MINE];
+  constexpr int WIDE = KS / 32;  // dwords of weights a lane has of a step, twice
+  uint32_t w[CB][2][WIDE], sb[CB][PER];
+  const auto load = [&](int t) {
+    const int k0 = t * KS;
+    if (k0 + KS <= K) {
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) in[i].load(x, row[i] + k0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) in[i].load(x, row[i] + k0, K - k0 - tid % CH * 8);
+    }
+  };
+  const auto load_weights = [&](int t) {
+    const int kt = t * KS / 128;
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const u32x2 v = reinterpret_cast<const u32x2*>(tiles + (tile[c] + kt) * 64 + lane % 16 + 16 * (2 * half + h))[t % 2];
+        w[c][half][0] = v[0], w[c][half][1] = v[1];
+      }
+#pragma unroll
+      for (int gi = 0; gi < PER; ++gi) {
+        const int k = t * KS + gi * G;  // (a group behind the last has any scale)
+        sb[c][gi] = k < K ? scales[((tile[c] + kt) * PER_TILE + k % 128 / GROUP) * 16 + lane % 16] : 0;
+      }
+    }
+  };
+  const auto store = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+      const int r = (tid + 256 * i) / CH, c = tid % CH;
+      u32x4 part[PARTS];
+      in[i].parts(part);
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) xs[buf][p][r * CH + (c ^ (r / 2 % 8))] = part[p];
+      float s = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t bits = in[i].raw[j / 4][j % 4];
+        s += __builtin_bit_cast(float, bits);
+      }
+      s = add_lane<0xb1>(s);  // (the four lanes of 32 values, and the eight of 64)
+      s = add_lane<0x4e>(s);
+      if constexpr (G >= 64) s = add_lane<0x141>(s);
+      if (c % (G / 8) == 0) sums[buf][c / (G / 8)][r] = s;
+    }
+  };
+  f32x16 acc[RB][CB] = {};
+  const uint32_t sixteens = sixteen<false>();
+  load(0);
+  load_weights(0);
+  store(0);
+  __syncthreads();
+  for (int t = 0; t < steps; ++t) {
+    const int buf = t % 2;
+    uint32_t v[CB][2][WIDE], sv[CB][PER];
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int j = 0; j < WIDE; ++j) v[c][half][j] = w[c][half][j];
+#pragma unroll
+      for (int gi = 0; gi < PER; ++gi) sv[c][gi] = sb[c][gi];
+    }
+    if (t + 1 < steps) load(t + 1), load_weights(t + 1);
+#pragma unroll
+    for (int gi = 0; gi < PER; ++gi) {
+      f32x16 dot[RB][CB] = {};
+#pragma unroll
+      for (int si = 0; si < G / 16; ++si) {
+        const int s = gi * (G / 16) + si;
+        u32x4 b[CB];
+#pragma unroll
+        for (int c = 0; c < CB; ++c) b[c] = levels<BMX_F32>(v[c][s % 2][s / 2], sixteens);
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+          const int rr = (wm * RB + r) * 32 + lane % 32, at = rr * CH + ((2 * s + h) ^ (rr / 2 % 8));
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) {
+            const u32x4 a = xs[buf][p][at];
+#pragma unroll
+            for (int c = 0; c < CB; ++c) dot[r][c] = mfma32<false>(a, b[c], dot[r][c]);
+          }
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        f32x4 sum[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = *reinterpret_cast<const f32x4*>(&sums[buf][gi][(wm * RB + r) * 32 + 8 * i + 4 * h]);
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+          const float sc = bf16_float(sv[c][gi]), o = __builtin_bit_cast(float, sv[c][gi] & 0xffff0000u) + kZero<BMX_F32> * sc;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[r][c][i] += sc * dot[r][c][i] + o * sum[i / 4][i % 4];
+        }
+      }
+    }
+    if (t + 1 < steps) store(1 - buf);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int c = 0; c < CB; ++c) {
+    if (col[c] >= N) continue;
+    const float add = bias ? bias[col[c]] : 0.0f;
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int m = m0 + (wm * RB + r) * 32 + 8 * (i / 4) + 4 * h + i % 4;
+        if (m < M) store_one<BMX_F32>(out, (int64_t)m * ldo + col[c], acc[r][c][i] + add);
+      }
+  }
+}
+
+// 16-bit types: 64 RB x 64 CB of y per workgroup of 2 x 2 waves, 32 RB x 32 CB each.  x comes into LDS without passing registers, a step ahead.  Sums over the groups of x, which the
+// offsets take, are products with ones on the matrix cores; of two 32-row blocks of a wave each column of waves makes its own, and they
+// meet through LDS a step later.  With SPLIT the workgroup has as many sets of four waves, which take turns at K's steps and join at the end.
+template <int TYPE, int RB, int CB, int GROUP, int SPLIT>
+__global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : SPLIT) void w4_deep_kernel(const uint16_t* x, int64_t ldx, bool async, const u32x4* tiles,
+                                                                 const uint32_t* scales, const float* bias, int M, int N, int K,
+                                                                 void* out, int64_t ldo) {
+  static_assert(TYPE != BMX_F32, "");
+  constexpr bool F16 = TYPE == BMX_F16, SHARE = RB == 2;
+  constexpr int BM = 64 * RB, MINE = BM / 16, PER = 128 / GROUP, STEPS = GROUP / 16;
+  static_assert(!SHARE || (PER == 1 && SPLIT == 1), "");
+  constexpr uint32_t one = F16 ? 0x3C003C00 : 0x3F803F80;
+  constexpr int kX = BM * 16;  // of a step, in 16 bytes
+  __shared__ u32x4 mem[SPLIT * 2 * kX];
+  __shared__ float sums[SHARE ? 2 : 1][SHARE ? BM : 4];
+  const int set = __builtin_amdgcn_readfirstlane(threadIdx.x / 256), tid = threadIdx.x % 256;
+  const int lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), h = lane / 32, wm = wave / 2, wn = wave % 2;
+  const int all = (K + 127) / 128;
+  // Tiles in bands of eight tiles of rows, dealt out so that an XCD (every eighth workgroup) has tiles side by side.
+  const int mt = (M + BM - 1) / BM, ntl = (N + 64 * CB - 1) / (64 * CB), total = mt * ntl, eighth = (total + 7) / 8;
+  const int id = blockIdx.x % 8 * eighth + blockIdx.x / 8;
+  if (id >= total || (int)(blockIdx.x / 8) >= eighth) return;
+  const int band = id / (8 * ntl), in_band = id - band * 8 * ntl, high = min(8, mt - band * 8);
+  const int m0 = (band * 8 + in_band % high) * BM, n0 = in_band / high * 64 * CB;
+
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)mem;
+  const auto at_x = [&](int buf) { return (set * 2 + buf) * kX; };
+  // A row's 16 chunks of eight values lie in 16 places, chunk c in place c ^ (row % 16), so that 16 rows' chunks of one number lie on all banks.
+  const int chunk = tid % 16 ^ tid / 16;
+  uint32_t from[MINE];
+#pragma unroll
+  for (int i = 0; i < MINE; ++i) from[i] = (uint32_t)((min(m0 + tid / 16 + 16 * i, M - 1) - m0) * ldx + chunk * 8) * 2;
+  const char* base = reinterpret_cast<const char*>(x + m0 * ldx);
+  int64_t tile[CB];
+  int col[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c) {
+    col[c] = n0 + (wn * CB + c) * 32 + lane % 32;
+    tile[c] = (int64_t)min(col[c] / 16, (N - 1) / 16) * all;
+  }
+  const auto stage = [&](int t, int buf) {
+    if (async && (t + 1) * 128 <= K) {
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) {
+        const uint32_t to = lds + (at_x(buf) + i * 256 + wave * 64) * 16;
+        const char* b = base + t * 256;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(from[i]), "s"(b) : "memory");
+      }
+    } else {  // rows on odd elements, and the last step of fewer than 128 values
+#pragma unroll 1
+      for (int i = 0; i < MINE; ++i) {
+        Eight<TYPE> in;
+        in.load(x, (int64_t)min(m0 + tid / 16 + 16 * i, M - 1) * ldx + t * 128 + chunk * 8, K - t * 128 - chunk * 8);
+        mem[at_x(buf) + i * 256 + tid] = in.raw[0];
+      }
+    }
+  };
+  u32x4 w[CB][2];
+  uint32_t sb[CB][PER];
+  const auto load_weights = [&](int t) {
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) w[c][half] = tiles[(tile[c] + t) * 64 + lane % 16 + 16 * (2 * half + h)];
+#pragma unroll
+      for (int gi = 0; gi < PER; ++gi)  // (a group behind the last has any scale)
+        sb[c][gi] = t * 128 + gi * GROUP < K ? scales[((tile[c] + t) * PER + gi) * 16 + lane % 16] : 0;
+    }
+  };
+  f32x16 acc[RB][CB] = {};
+  const uint32_t sixteens = sixteen<F16>();
+  float o_before[CB] = {};
+  const auto offsets = [&](int buf) {  // the step before's sums times its offsets
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 sum = *reinterpret_cast<const f32x4*>(&sums[buf][(wm * RB + r) * 32 + 8 * i + 4 * h]);
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[r][c][4 * i + j] += o_before[c] * sum[j];
+      }
+  };
+  if (set < all) {
+    load_weights(set);
+    stage(set, 0);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  for (int i = 0; i * SPLIT < all; ++i) {
+    const int t = i * SPLIT + set, buf = i % 2;
+    if (SPLIT == 1 || t < all) {
+      u32x4 v[CB][2];
+      uint32_t sv[CB][PER];
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        v[c][0] = w[c][0], v[c][1] = w[c][1];
+#pragma unroll
+        for (int gi = 0; gi < PER; ++gi) sv[c][gi] = sb[c][gi];
+      }
+      if (t + SPLIT < all) {
+        stage(t + SPLIT, 1 - buf);
+        load_weights(t + SPLIT);
+      }
+      if constexpr (SHARE)
+        if (t > 0) offsets((t - 1) % 2);
+#pragma unroll
+      for (int gi = 0; gi < PER; ++gi) {
+        if constexpr (PER > 1) __builtin_amdgcn_sched_barrier(0);  // (registers: one group's products at a time)
+        f32x16 dot[RB][CB] = {}, sum = {};
+#pragma unroll
+        for (int si = 0; si < STEPS; ++si) {
+          const int s = gi * STEPS + si;
+          u32x4 b[CB];
+#pragma unroll
+          for (int c = 0; c < CB; ++c) b[c] = levels<TYPE>(v[c][s % 2][s / 2], sixteens);
+          u32x4 xr[RB];
+#pragma unroll
+          for (int r = 0; r < RB; ++r) {
+            const int rr = (wm * RB + r) * 32 + lane % 32;
+            xr[r] = mem[at_x(buf) + rr * 16 + ((2 * s + h) ^ rr % 16)];
+#pragma unroll
+            for (int c = 0; c < CB; ++c) dot[r][c] = mfma32<F16>(xr[r], b[c], dot[r][c]);
+          }
+          sum = mfma32<F16>(SHARE && wn == 1 ? xr[RB - 1] : xr[0], u32x4{one, one, one, one}, sum);
+        }
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+          const float sc = bf16_float(sv[c][gi] & 0xffff), o = __builtin_bit_cast(float, sv[c][gi] & 0xffff0000u) + kZero<TYPE> * sc;
+#pragma unroll
+          for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[r][c][i] += SHARE ? sc * dot[r][c][i] : sc * dot[r][c][i] + o * sum[i];
+          o_before[c] = o;
+        }
+        if constexpr (SHARE) {
+          if (lane % 32 == 0)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<f32x4*>(&sums[t % 2][(wm * RB + wn) * 32 + 8 * i + 4 * h]) = f32x4{sum[4 * i], sum[4 * i + 1], sum[4 * i + 2], sum[4 * i + 3]};
+        }
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next step has come
+    __syncthreads();
+  }
+  if constexpr (SHARE) offsets((all - 1) % 2);
+  if constexpr (SPLIT > 1) {  // the other sets' parts, in their order
+    float* part = reinterpret_cast<float*>(mem);
+    if (set > 0) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) part[(((set - 1) * 4 + wave) * 16 + i) * 64 + lane] = acc[0][0][i];
+    }
+    __syncthreads();
+    if (set > 0) return;
+#pragma unroll
+    for (int p = 0; p < SPLIT - 1; ++p)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[0][0][i] += part[((p * 4 + wave) * 16 + i) * 64 + lane];
+  }
+#pragma unroll
+  for (int c = 0; c < CB; ++c) {
+    if (col[c] >= N) continue;
+    const float add = bias ? bias[col[c]] : 0.0f;
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int m = m0 + (wm * RB + r) * 32 + 8 * (i / 4) + 4 * h + i % 4;
+        if (m < M) store_one<TYPE>(out, (int64_t)m * ldo + col[c], acc[r][c][i] + add);
+      }
+  }
+}
+
+template <int TYPE, int RB, int CB, int SPLIT>
+void launch_deep(const void* x, int64_t ldx, const void* tiles, const void* scales, int group, const float* bias, int M, int N, int K,
+                 void* out, int64_t ldo, hipStream_t s) {
+  const int64_t total = ceil_div(M, 64 * RB) * ceil_div(N, 64 * CB);
+  const dim3 grid((uint32_t)(ceil_div(total, 8) * 8));
+  auto* t = static_cast<const u32x4*>(tiles);
+  auto* sc = static_cast<const uint32_t*>(scales);
+  const bool async = (uintptr_t)x % 4 == 0 && (M == 1 || ldx % 2 == 0);
+  const auto pick = [&] {
+    if constexpr (RB * CB == 1) {
+      if (group == 32) return w4_deep_kernel<TYPE, RB, CB, 32, SPLIT>;
+      if (group == 64) return w4_deep_kernel<TYPE, RB, CB, 64, SPLIT>;
+    }
+    return w4_deep_kernel<TYPE, RB, CB, 128, SPLIT>;
+  };
+  launch_kernel(pick(), grid, dim3(256 * SPLIT), 0, s, static_cast<const uint16_t*>(x), ldx, async, t, sc, bias, M, N, K, out, ldo);
+  note_kernel("w4_deep_kernel<%d,%d,%d,%d,%d> grid %d block %d", TYPE, RB, CB, group, SPLIT, (int)grid.x, 256 * SPLIT);
+}
+
+// Few rows: 16 columns a workgroup, whatever bounds a stream of weights.  More: tiles of 64 x 64, or of 128 x 128 where they fill the chip.
+// bf16, 4096 x 4096, us, rows against tiles in four sets of waves: 16 rows 8.2, 17; 32 rows 12, 18; 64 rows 18 (four tiles of 16 a wave), 18;
+// 256 rows 61, 20.  In four, two, one set: 256 rows 20, 22, 28; 512 rows 37, 35, 36; 2048 rows 145, 127, 120, and 89 in tiles of 128 x 128.
+// f32: 64 rows 38, in tiles 94; 256 rows 152, 94; 2048 rows 1150, 294.
 template <int TYPE>
 void launch_typed(const void* x, int64_t ldx, const void* tiles, const void* scales, int group, const float* bias, int M, int N, int K,
                   void* out, int64_t ldo, hipStream_t s) {
-  const bool aligned = (uintptr_t)x % 16 == 0 && (M == 1 || ldx * type_bytes(TYPE) % 16 == 0);
-  const auto f = M <= 16 ? launch_rows<TYPE, 1> : M <= 32 ? launch_rows<TYPE, 2> : launch_rows<TYPE, 4>;
-  f(x, ldx, aligned, tiles, scales, group, bias, M, N, K, out, ldo, s);
+  const int64_t small = ceil_div(M, 64) * ceil_div(N, 64), large = ceil_div(M, 128) * ceil_div(N, 128);
+  if constexpr (TYPE == BMX_F32) {
+    if (M > 32 && (int64_t)M * N > 160 * 4096) {
+      const dim3 grid((uint32_t)(ceil_div(ceil_div(M, 64) * ceil_div(N, 128), 8) * 8));
+      const auto kern = group == 32 ? w4_f32_kernel<32> : group == 64 ? w4_f32_kernel<64> : w4_f32_kernel<128>;
+      launch_kernel(kern, grid, dim3(256), 0, s, x, ldx, static_cast<const u32x4*>(tiles), static_cast<const uint32_t*>(scales), bias, M, N, K, out, ldo);
+      note_kernel("w4_f32_kernel<%d> grid %d block 256", group, (int)grid.x);
+      return;
+    }
+  } else if ((M > 32 || (M > 16 && N > 6144)) && ldx < (1 << 24)) {  // (offsets within a tile's rows in 32 bits)
+    const auto f = group == 128 && large >= 256 ? launch_deep<TYPE, 2, 2, 1> : small <= 256 ? launch_deep<TYPE, 1, 1, 4>
+                 : small <= 512 ? launch_deep<TYPE, 1, 1, 2> : launch_deep<TYPE, 1, 1, 1>;
+    f(x, ldx, tiles, scales, group, bias, M, N, K, out, ldo, s);
+    return;
+  }
+  const auto f = M <= 16 ? launch_rows<TYPE, 1> : launch_rows<TYPE, 2>;
+  f(x, ldx, tiles, scales, group, bias, M, N, K, out, ldo, s);
 }
 
 // A bf16 that is no infinity: the quantiser's scales and offsets stay finite.

@@ -76,6 +76,26 @@ def test_w4_fc(M, N, K, group, kind):
     assert "w4_" in B.last_kernel()
 
 
+@pytest.mark.parametrize("M,N,K,group,kind,kernel", [
+    (100, 4100, 300, 64, "bf16", "1,1,64,4"), (260, 4100, 300, 32, "f16", "1,1,32,2"), (520, 4200, 700, 64, "bf16", "1,1,64,1"),
+    (577, 4200, 1000, 32, "f16", "1,1,32,1"), (1050, 4250, 300, 128, "bf16", "2,2,128,1"), (2000, 2100, 1024, 128, "f16", "2,2,128,1"),
+    (1050, 4250, 150, 64, "bf16", "1,1,64,1"), (20, 7001, 520, 128, "bf16", "1,1,128,4"), (300, 2500, 300, 32, "f32", "f32_kernel<32>"),
+    (700, 1000, 200, 64, "f32", "f32_kernel<64>"), (260, 4097, 513, 128, "f32", "f32_kernel<128>")])
+def test_w4_fc_many_results(M, N, K, group, kind, kernel):
+    """Sizes that reach the kernels of many tiles, rows on odd elements too; the values in 64 bits made on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    tiles, scales = random_tiles(g, N, K, group)
+    q, s, b = (torch.from_numpy(a).cuda() for a in unpack(tiles, scales, N, K))
+    for shift in (0, 3):
+        x = torch.randn((M, K + 2 * shift), device="cuda", generator=g).to(TYPES[kind][0])[:, shift:shift + K]
+        y = B.w4_fc(x, tiles, scales, N)
+        assert kernel in B.last_kernel()
+        want = x.double() @ (q * s + b).t().contiguous()
+        size = x.double().abs() @ (31 * s.abs() + (b - 16 * s).abs()).t().contiguous()
+        bound = TYPES[kind][1] * want.abs() + (K / 32 + 64) * 2.0**-24 * size + 1e-30
+        assert bool(((y.double() - want).abs() <= bound).all())
+
+
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("M,pad,shift", [(3, 0, 1), (20, 3, 0), (70, 8, 2), (150, 5, 3), (150, 8, 8)])
 def test_w4_fc_strides_and_bias(M, pad, shift, kind):
