@@ -55,6 +55,10 @@ __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
+using f32x16 = float __attribute__((ext_vector_type(16)));
+__device__ inline f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
 // Two values as one pair of f16, or as three pairs of bf16.  The parts' bits are cut off, not rounded: the compiler folds a product into one
 // use of a conversion and not into another, and what is left would then belong to another part than the one in use.
 template <int PARTS>
@@ -94,6 +98,7 @@ struct Args {
   float* parts;      // [sequence, tile of rows, head][split][part_rows][ROW + 4]: the rows' results, maximum and sum
   uint32_t* arrived; // [sequence, tile of rows, head]
   int q_heads, share, rows, max_new, window, splits, part_rows;
+  int few;  // sequences of more rows than this are the other kernel's
   bool causal, aligned;
   float scale;
 };
@@ -113,7 +118,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
   const int head = blockIdx.x % c.heads, split = blockIdx.x / c.heads, seq = blockIdx.z;
   const KvSpan s = kv_span(c, seq, a.rows, a.max_new);
   const int r0 = blockIdx.y * 16;
-  if (r0 >= s.count * a.share) return;
+  if (r0 >= s.count * a.share || s.count * a.share > a.few) return;
   // what any, and what every one of the 16 rows sees: positions [low, high)
   const int tok0 = r0 / a.share, tok1 = min((r0 + 15) / a.share, s.count - 1);
   const int high_any = a.causal ? min(s.first + tok1 + 1, s.length) : s.length, high_all = a.causal ? min(s.first + tok0 + 1, s.length) : s.length;
@@ -377,15 +382,239 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
   }
 }
 
+// Many rows: 128 of one head of the cache per workgroup, 32 a wave, over all pages that any of them sees.  A page comes into LDS once for
+// the four waves, as 16-bit floats in the order of the 32 x 32 x 16 products' operands (a wave brings in a quarter of it, a page ahead, and
+// converts it on its way), and a lane has one row's scores of 16 of 32 tokens, which again are those of its own column of P^T.
+// Bound by the vector ALU: 64 tokens x 32 rows are 32 matrix-core products, 1024 cycles, and 32 exponentials, maxima, conversions a lane.
+// So where all of a page is seen and no scale of its values is far below the largest, the scale goes into the exponent,
+//   p c / C 2^14 = 2^(s + log2(c / C 2^14) - m),
+// and comes out of the sum of p again once for each 16 tokens.
+template <int TYPE, int DC>
+__global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_cache c, Args a) {
+  static_assert(TYPE != BMX_F32, "");
+  constexpr int ROW = DC * 32, WIDE = DC / 2, NS = DC * 2, VN = (DC + 3) / 4;  // NS: steps of 16 values; VN: 32-value tiles of V a wave brings in
+  __shared__ u32x4 lds[2][2][NS * 128];                          // [buffer][keys, values]
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
+  const int head = blockIdx.x, seq = blockIdx.z;
+  const KvSpan s = kv_span(c, seq, a.rows, a.max_new);
+  const int rows = s.count * a.share;
+  const int r0 = ((rows + 127) / 128 - 1 - (int)blockIdx.y) * 128;  // (the last rows, which see most, first)
+  if (r0 < 0 || rows <= a.few) return;
+  const auto first_seen = [&](int token) { return a.window ? max(max(s.first + token, 0) - a.window + 1, 0) : 0; };
+  const auto end_seen = [&](int token) { return a.causal ? min(s.first + token + 1, s.length) : s.length; };
+  const auto token_of = [&](int r) { return min(r, rows - 1) / a.share; };
+  // what any row of the workgroup sees; what any, and every row of this wave does; what this lane's row does
+  const int low_group = first_seen(token_of(r0)), high_group = end_seen(token_of(r0 + 127));
+  const int r_wave = r0 + wave * 32, r = r_wave + lane % 32, token = token_of(r);
+  const int low_any = first_seen(token_of(r_wave)), low_all = first_seen(token_of(r_wave + 31));
+  const int high_all = end_seen(token_of(r_wave)), high_any = r_wave < rows ? end_seen(token_of(r_wave + 31)) : 0;
+  const int low = first_seen(token), high = end_seen(token);
+
+  const int blocks = kPage / c.block, log_block = 31 - __builtin_clz(c.block);
+  const int64_t page_bytes = (int64_t)c.heads * 2 * kPage * ROW;
+  u32x4 kr[WIDE > 0 ? WIDE : 1], vr[VN][2];
+  u32x2 kt;
+  float scale_in = 0.0f;  // lanes 0 to 3: the coming page's scales of keys; 4 to 7: of values
+  const int scale_at = (lane / 4 % 2) * blocks + (lane % 4 * 16 >> log_block);
+  const int last = (high_group + kPage - 1) / kPage;
+  // the first page from `pg` on that is there, on its way into registers
+  const auto fetch = [&](int pg) {
+    int page = -1;
+    for (; pg < last; ++pg) {
+      page = kv_page(c, seq, pg);
+      if (page >= 0) break;
+    }
+    const Rsrc rk = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)head * 2 * kPage * ROW, page >= 0 ? 2 * kPage * ROW : 0);
+    const Rsrc rs = buffer(c.scales + ((int64_t)max(page, 0) * c.heads + head) * 2 * blocks, page >= 0 ? 8 * blocks : 0);
+    scale_in = __builtin_bit_cast(float, load4(rs, scale_at * 4, 0));
+#pragma unroll
+    for (int w = 0; w < WIDE; ++w) kr[w] = load16(rk, lane * 16, wave * 16 * ROW + w * 1024);
+    if constexpr (DC % 2) kt = load8(rk, lane * 8, wave * 16 * ROW + WIDE * 1024);
+#pragma unroll
+    for (int n = 0; n < VN; ++n) {
+      const int q = min(wave + 4 * n, DC - 1);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) vr[n][g] = load16(rk, (lane % 32 / 16) * 1024 + h * 256 + lane % 16 * 16, kPage * ROW + q * 2048 + g * 512);
+    }
+    return pg;
+  };
+  const auto convert = [&](int buf) {
+    // keys: unit `wave`, lane = (16 values, token); values: lane = (column, every other four tokens)
+    u32x4* to = &lds[buf][0][wave / 2 * NS * 64 + wave % 2 * 16 + lane % 16];
+#pragma unroll
+    for (int w = 0; w < WIDE; ++w) {
+      to[(4 * w + lane / 16) * 64] = eight_levels<true>(kr[w][0], kr[w][1]);
+      to[(4 * w + lane / 16) * 64 + 32] = eight_levels<true>(kr[w][2], kr[w][3]);
+    }
+    if constexpr (DC % 2) to[(4 * WIDE + lane / 32) * 64 + lane / 16 % 2 * 32] = eight_levels<true>(kt[0], kt[1]);
+#pragma unroll
+    for (int n = 0; n < VN; ++n) {
+      if (wave + 4 * n >= DC) break;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) lds[buf][1][(u * DC + wave + 4 * n) * 64 + lane] = eight_levels<true>(vr[n][0][u], vr[n][1][u]);
+    }
+  };
+  int pg = fetch(low_group / kPage);
+
+  u32x4 q[NS];
+  float factor;
+  {
+    const int64_t base = (s.row0 + token) * a.q_row + (head * a.share + min(r, rows - 1) % a.share) * a.q_head;
+    float x[NS][8], top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const int d = 16 * i + 8 * h;
+      load_eight<TYPE>(a.q, base + d, c.dim - d, a.aligned, x[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[i][j]));
+    }
+    top = fmaxf(top, __shfl_xor(top, 32));
+    int e = 0;
+    if (top > 0.0f && top < INFINITY) (void)frexpf(top, &e);
+    e -= 8;
+    factor = ldexpf(a.scale * 1.4426950408889634f, e);
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t part[1];
+        pair<1>(ldexpf(x[i][2 * j], -e), ldexpf(x[i][2 * j + 1], -e), part);
+        q[i][j] = part[0];
+      }
+  }
+  if (pg < last) convert(0);
+  float scale_of = scale_in;
+  __syncthreads();
+
+  float m = -INFINITY, l = 0.0f, most = 0.0f;
+  f32x16 o[DC] = {};
+  for (int buf = 0; pg < last; buf ^= 1) {
+    const int next = fetch(pg + 1), t0 = pg * kPage;
+    if (t0 < high_any && t0 + kPage > low_any) {
+      f32x16 z[2] = {};
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) z[t] = mfma32(lds[buf][0][(t * NS + i) * 64 + lane], q[i], z[t]);
+      float key_scale[4], value_scale[4], most_new = most, top = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        key_scale[u] = factor * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale_of), u));
+        value_scale[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale_of), 4 + u));
+        if (t0 + 16 * u >= high_any || t0 + 16 * u + 16 <= low_any) value_scale[u] = 0.0f;  // (a block that nobody has written has any scale)
+        most_new = fmaxf(most_new, value_scale[u]);
+      }
+      // (scales below 2^-126 are those of levels that are all 0)
+      const float inverse = most_new >= 0x1p-126f ? 1.0f / most_new : 0.0f;
+      float f[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) f[u] = value_scale[u] * inverse * 0x1p14f;
+      const bool full = __builtin_amdgcn_readfirstlane(t0 >= low_all && t0 + kPage <= high_all && fminf(fminf(f[0], f[1]), fminf(f[2], f[3])) >= 0x1p-8f);
+      u32x4 w[4];
+      if (full) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          float t = z[u / 2][u % 2 * 8];
+#pragma unroll
+          for (int i = 1; i < 8; ++i) t = fmaxf(t, z[u / 2][u % 2 * 8 + i]);
+          // (of a negative factor the smallest score is the largest)
+          if (a.scale < 0.0f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t = fminf(t, z[u / 2][u % 2 * 8 + i]);
+          }
+          top = fmaxf(top, t * key_scale[u]);
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int t = t0 + 16 * u + i / 4 * 8 + 4 * h + i % 4;
+            const float x = t < high && t >= low ? z[u / 2][u % 2 * 8 + i] * key_scale[u] : -INFINITY;
+            z[u / 2][u % 2 * 8 + i] = x;
+            top = fmaxf(top, x);
+          }
+      }
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m_new = fmaxf(m, top), m_at = m_new == -INFINITY ? 0.0f : m_new;
+      const float shrink = __builtin_amdgcn_exp2f(m - m_at), shrink_o = shrink * (most * inverse);
+      m = m_new;
+      most = most_new;
+      l *= shrink;
+      if (full) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float at = __builtin_amdgcn_logf(f[u]) - m_at;
+          float sum = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float y0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u / 2][u % 2 * 8 + 2 * i], key_scale[u], at));
+            const float y1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u / 2][u % 2 * 8 + 2 * i + 1], key_scale[u], at));
+            sum += y0 + y1;
+            uint32_t part[1];
+            pair<1>(y0, y1, part);
+            w[u][i] = part[0];
+          }
+          l += sum * __builtin_amdgcn_rcpf(f[u]);
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float e0 = __builtin_amdgcn_exp2f(z[u / 2][u % 2 * 8 + 2 * i] - m_at), e1 = __builtin_amdgcn_exp2f(z[u / 2][u % 2 * 8 + 2 * i + 1] - m_at);
+            l += e0 + e1;
+            uint32_t part[1];
+            pair<1>(e0 * f[u], e1 * f[u], part);
+            w[u][i] = part[0];
+          }
+      }
+      if (__any(shrink_o != 1.0f)) {  // (most pages hold no new maximum)
+#pragma unroll
+        for (int n = 0; n < DC; ++n) o[n] *= shrink_o;
+      }
+#pragma unroll
+      for (int n = 0; n < DC; ++n)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) o[n] = mfma32(lds[buf][1][(u * DC + n) * 64 + lane], w[u], o[n]);
+    }
+    if (next < last) convert(buf ^ 1);
+    scale_of = scale_in;
+    pg = next;
+    __syncthreads();
+  }
+  l += __shfl_xor(l, 32);
+  if (r >= rows) return;
+  const int64_t at = (s.row0 + token) * a.out_row + (head * a.share + r % a.share) * a.out_head;
+  // (a row that sees nothing is zeros)
+  const float share_of = l == 0.0f ? 0.0f : most * 0x1p-14f / l;
+#pragma unroll
+  for (int n = 0; n < DC; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int d = n * 32 + i / 4 * 8 + 4 * h + i % 4;
+      if (d < c.dim) store_one<TYPE>(a.out, at + d, l == 0.0f ? 0.0f : o[n][i] * share_of);
+    }
+  if (a.lse && h == 0)
+    a.lse[(s.row0 + token) * a.q_heads + head * a.share + r % a.share] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
 // What a call needs: tiles of rows, splits, and bytes of the workspace.
 struct Plan {
-  int64_t units, tiles;
-  int splits, part_rows;
+  int64_t units, tiles, prompt_tiles;  // prompt_tiles: of 128 rows, 0 where they are too few to fill the chip
+  int splits, part_rows, few;
   size_t bytes;
 };
-Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new) {
+Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new, int type) {
   Plan p;
-  const int64_t rows = max_new * (q_heads / heads);
+  int64_t rows = max_new * (q_heads / heads);
+  p.few = 0x7fffffff;
+  p.prompt_tiles = 0;
+  if (type != BMX_F32 && ceil_div(rows, 128) * heads * sequences >= 128 && rows > 64) {
+    p.prompt_tiles = ceil_div(rows, 128);
+    p.few = 64;
+    rows = 64;
+  }
   p.tiles = ceil_div(rows, 16);
   p.units = sequences * heads * p.tiles;
   p.part_rows = (int)std::min<int64_t>(rows, 16);
@@ -398,17 +627,29 @@ Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads
 }
 
 template <int TYPE, int DC>
-void launch(const bmx_kv_cache& c, const Args& a, int64_t tiles, hipStream_t s) {
-  const dim3 grid(c.heads * a.splits, (uint32_t)tiles, c.sequences), block(kWaves * 64);
-  launch_kernel(kv_attention_kernel<TYPE, DC>, grid, block, 0, s, c, a);
-  note_kernel("kv_attention_kernel<%d,%d> grid %ux%ux%u block %u", TYPE, DC, grid.x, grid.y, grid.z, block.x);
+void launch(const bmx_kv_cache& c, const Args& a, const Plan& p, hipStream_t s) {
+  // (rows of sequences as long as each other are all many or all few)
+  if (!p.prompt_tiles || (c.starts && c.sequences > 1)) {
+    const dim3 grid(c.heads * a.splits, (uint32_t)p.tiles, c.sequences);
+    launch_kernel(kv_attention_kernel<TYPE, DC>, grid, dim3(kWaves * 64), 0, s, c, a);
+    note_kernel("kv_attention_kernel<%d,%d> grid %ux%ux%u block %d", TYPE, DC, grid.x, grid.y, grid.z, kWaves * 64);
+  }
+  if constexpr (TYPE != BMX_F32) {
+    if (p.prompt_tiles) {
+      const dim3 grid(c.heads, (uint32_t)p.prompt_tiles, c.sequences);
+      Args b = a;
+      if (!c.starts || c.sequences == 1) b.few = 0;
+      launch_kernel(kv_prompt_kernel<TYPE, DC>, grid, dim3(256), 0, s, c, b);
+      note_kernel("kv_prompt_kernel<%d,%d> grid %ux%ux%u block 256", TYPE, DC, grid.x, grid.y, grid.z);
+    }
+  }
 }
 template <int TYPE>
-void launch_typed(const bmx_kv_cache& c, const Args& a, int64_t tiles, hipStream_t s) {
+void launch_typed(const bmx_kv_cache& c, const Args& a, const Plan& p, hipStream_t s) {
   const int dc = kv_row_bytes(c.dim) / 32;
   const auto f = dc == 1 ? launch<TYPE, 1> : dc == 2 ? launch<TYPE, 2> : dc == 3 ? launch<TYPE, 3> : dc == 4 ? launch<TYPE, 4>
                : dc == 5 ? launch<TYPE, 5> : dc == 6 ? launch<TYPE, 6> : dc == 7 ? launch<TYPE, 7> : launch<TYPE, 8>;
-  f(c, a, tiles, s);
+  f(c, a, p, s);
 }
 
 __global__ void clear_kernel(uint32_t* p) { p[blockIdx.x * 256 + threadIdx.x] = 0; }
@@ -416,7 +657,9 @@ __global__ void clear_kernel(uint32_t* p) { p[blockIdx.x * 256 + threadIdx.x] = 
 }  // namespace
 
 size_t kv_attention_workspace(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new) {
-  return plan(sequences, table_width, heads, q_heads, dim, max_new).bytes;
+  // (whatever the type)
+  return std::max(plan(sequences, table_width, heads, q_heads, dim, max_new, BMX_F32).bytes,
+                  plan(sequences, table_width, heads, q_heads, dim, max_new, BMX_F16).bytes);
 }
 
 hipError_t launch_kv_attention(const bmx_kv_cache& c, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int rows,
@@ -424,13 +667,13 @@ hipError_t launch_kv_attention(const bmx_kv_cache& c, const void* q, int type, i
                                void* workspace, bool fresh, hipStream_t s) {
   const int64_t size = type_bytes(type);
   const bool aligned = (uintptr_t)q % 16 == 0 && q_row * size % 16 == 0 && q_head * size % 16 == 0;
-  const Plan p = plan(c.sequences, c.table_width, c.heads, q_heads, c.dim, max_new);
+  const Plan p = plan(c.sequences, c.table_width, c.heads, q_heads, c.dim, max_new, type);
   uint32_t* arrived = static_cast<uint32_t*>(workspace);
   const Args a = {q, q_row, q_head, out, out_row, out_head, lse, reinterpret_cast<float*>(arrived + kCounters), arrived, q_heads,
-                  q_heads / c.heads, rows, max_new, window, p.splits, p.part_rows, causal, aligned, scale};
+                  q_heads / c.heads, rows, max_new, window, p.splits, p.part_rows, p.few, causal, aligned, scale};
   if (fresh && p.splits > 1) launch_kernel(clear_kernel, dim3((uint32_t)ceil_div(p.units, 256)), dim3(256), 0, s, arrived);
   const auto f = type == BMX_F32 ? launch_typed<BMX_F32> : type == BMX_F16 ? launch_typed<BMX_F16> : launch_typed<BMX_BF16>;
-  f(c, a, p.tiles, s);
+  f(c, a, p, s);
   return launch_error();
 }
 

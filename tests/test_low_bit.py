@@ -469,6 +469,54 @@ def test_kv_attention(totals, new, q_heads, heads, dim, block, kind):
         assert torch.equal(out, B.kv_attention(q, c.pages, c.scales, c.table, c.lens(), causal=causal, window=window))
 
 
+@pytest.mark.parametrize("seqs,heads,share,dim,block,kind", [
+    (64, 2, 4, 64, 16, "bf16"), (43, 3, 5, 96, 32, "f16"), (128, 1, 7, 128, 64, "bf16"), (16, 8, 3, 40, 16, "f16"), (64, 2, 8, 160, 16, "bf16"),
+    (128, 1, 6, 256, 32, "f16"), (32, 4, 4, 20, 64, "bf16"), (64, 2, 4, 192, 16, "f16"), (128, 1, 9, 224, 16, "bf16")])
+def test_kv_attention_many_rows(seqs, heads, share, dim, block, kind):
+    """Batches of prompts that fill the chip: evenly, and ragged with sequences of few rows, none, and rows of positions below 0."""
+    totals = [(37 * i + 11) % 230 for i in range(seqs)]
+    c = Cache(seqs, 4, heads, dim, block, seqs + dim)
+    g = fill(c, totals, kind, dim)
+    for ragged in (False, True):
+        new = [min(n, (13 * i) % 90) for i, n in enumerate(totals)] if ragged else [30] * seqs
+        q = torch.randn((sum(new), heads * share, dim), device="cuda", generator=g).to(TYPES[kind][0])
+        starts = torch.tensor(np.cumsum([0] + new), dtype=torch.int32, device="cuda") if ragged else None
+        for causal, window in ((True, 0), (False, 0), (True, 40)):
+            out, lse = B.kv_attention(q, c.pages, c.scales, c.table, c.lens(), starts=starts, max_new=max(new) if ragged else 0,
+                                      causal=causal, window=window, lse=True)
+            assert "kv_prompt_kernel" in B.last_kernel()
+            check_attention(out, q, c, new, kind, causal, window, lse=lse)
+
+
+def test_kv_attention_many_rows_large_and_small_values():
+    """As the test below, where many rows share a page: negative and large factors, blocks whose scales differ by 2^20, zeros, NaN in a query."""
+    c = Cache(8, 5, 4, 64, 16, 9)
+    g = torch.Generator(device="cuda").manual_seed(1)
+
+    def change(kv):
+        kv[0] *= 8
+        kv[1, 30:60] *= 2.0**-10
+        kv[1, 100:130] *= 2.0**10
+        kv[1, 160:176] = 0
+        kv[1, 700:900] = 0
+    c.write([300] * 8, "f32", g, change)
+    q = torch.randn((8 * 250, 8, 64), device="cuda", generator=g)
+    q[:, 1] *= 30
+    q[:, 2] = 0
+    q[:, 3] *= 2.0**-13
+    for kind in ("f16", "bf16"):
+        for scale in (0.3, -0.2):
+            x = q.to(TYPES[kind][0])
+            out = B.kv_attention(x, c.pages, c.scales, c.table, c.lens(), scale=scale)
+            assert "kv_prompt_kernel" in B.last_kernel()
+            check_attention(out, x, c, [250] * 8, kind, scale=scale)
+        x[17, 5, 3] = float("nan")
+        got = B.kv_attention(x, c.pages, c.scales, c.table, c.lens(), scale=scale)
+        assert bool(torch.isnan(got[17, 5]).all())
+        got[17, 5] = out[17, 5]
+        assert torch.equal(got, out)
+
+
 @pytest.mark.parametrize("rows", [1, 40, 200])
 @pytest.mark.parametrize("kind", list(TYPES))
 def test_kv_attention_large_and_small_values(kind, rows):
