@@ -208,6 +208,109 @@ void launch_rows(const void* x, int64_t ldx, const void* tiles, const void* scal
   note_kernel("w4_rows_kernel<%d,%d,%d> grid %dx%d block %d", TYPE, MT, group, (int)grid.x, (int)grid.y, (int)block.x);
 }
 
+// 16-bit types, 17 to 64 rows: as w4_rows_kernel, but a wave brings its steps of x into LDS of its own, a step ahead, and takes the operands from
+// there.  (A lane's operand is 16 bytes of a row, and lanes side by side have rows below each other: read from memory so, 16 rows lie
+// on the same banks of the L1, and 64 rows of 4096 took 13 of 18 us to come.)
+template <int TYPE, int MT, int GROUP>
+__global__ __launch_bounds__(1024 / MT) void w4_few_kernel(const uint16_t* x, int64_t ldx, bool async, const u32x4* tiles, const uint32_t* scales,
+                                                           const float* bias, int M, int N, int K, void* out, int64_t ldo) {
+  constexpr bool F16 = TYPE == BMX_F16;
+  constexpr int PER = 128 / GROUP, STEPS = GROUP / 32, WAVES = 16 / MT, MINE = 4 * MT;
+  constexpr uint32_t one = F16 ? 0x3C003C00 : 0x3F803F80;
+  __shared__ u32x4 mem[WAVES][2][MT * 256];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16;
+  const int nt = blockIdx.x, m0 = blockIdx.y * 16 * MT, all = (K + 127) / 128;
+  const u32x4 ones = {one, one, one, one};
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)mem[wave];
+  // chunk c of a row's 16 chunks of eight values lies in place c ^ (row % 16)
+  uint32_t from[MINE];
+#pragma unroll
+  for (int i = 0; i < MINE; ++i) from[i] = (uint32_t)((min(m0 + 4 * i + g, M - 1) - m0) * ldx + ((lane % 16) ^ ((4 * i + g) % 16)) * 8) * 2;
+  const char* base = reinterpret_cast<const char*>(x + m0 * ldx);
+  u32x4 w, sb[PER];
+  const auto load = [&](int kt, int buf) {
+    if (async && (kt + 1) * 128 <= K) {
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) {
+        const uint32_t to = lds + (buf * MT * 256 + i * 64) * 16;
+        const char* b = base + kt * 256;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(from[i]), "s"(b) : "memory");
+      }
+    } else {  // rows on odd elements, and the last step of fewer than 128 values
+#pragma unroll 1
+      for (int i = 0; i < MINE; ++i) {
+        const int chunk = (lane % 16) ^ ((4 * i + g) % 16);
+        Eight<TYPE> in;
+        in.load(x, (int64_t)min(m0 + 4 * i + g, M - 1) * ldx + kt * 128 + chunk * 8, K - kt * 128 - chunk * 8);
+        mem[wave][buf][i * 64 + lane] = in.raw[0];
+      }
+    }
+    const int64_t tile = (int64_t)nt * all + kt;
+    w = tiles[tile * 64 + lane];
+#pragma unroll
+    for (int gi = 0; gi < PER; ++gi) sb[gi] = *reinterpret_cast<const u32x4*>(scales + (tile * PER + gi) * 16 + 4 * g);
+  };
+  f32x4 acc[MT] = {};
+  const uint32_t sixteens = sixteen<F16>();
+  if (wave < all) load(wave, 0);
+  for (int kt = wave, buf = 0; kt < all; kt += WAVES, buf ^= 1) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const u32x4 wv = w;
+    u32x4 sv[PER];
+#pragma unroll
+    for (int gi = 0; gi < PER; ++gi) sv[gi] = sb[gi];
+    if (kt + WAVES < all) load(kt + WAVES, buf ^ 1);
+#pragma unroll
+    for (int gi = 0; gi < PER; ++gi) {
+      if (kt * 128 + gi * GROUP >= K) break;  // (whatever scales lie behind the last group)
+      f32x4 dot[MT] = {}, sum[MT] = {};
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        const int step = gi * STEPS + st;
+        const u32x4 a = levels<TYPE>(wv[step], sixteens);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const u32x4 b = mem[wave][buf][(16 * i + lane % 16) * 16 + ((4 * step + g) ^ (lane % 16))];
+          dot[i] = mfma<F16>(a, b, dot[i]);
+          sum[i] = mfma<F16>(ones, b, sum[i]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float s = bf16_float(sv[gi][j]), o = __builtin_bit_cast(float, sv[gi][j] & 0xffff0000) + kZero<TYPE> * s;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[i][j] += s * dot[i][j] + o * sum[i][j];
+      }
+    }
+  }
+  __syncthreads();
+  f32x4* red = reinterpret_cast<f32x4*>(mem);
+#pragma unroll
+  for (int i = 0; i < MT; ++i) red[(wave * MT + i) * 64 + lane] = acc[i];
+  __syncthreads();
+  for (int e = threadIdx.x; e < 256 * MT; e += 64 * WAVES) {
+    const int m = e / 16, n = e % 16;
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v += red[(w * MT + m / 16) * 64 + m % 16 + 16 * (n / 4)][n % 4];
+    if (m0 + m < M && nt * 16 + n < N) {
+      if (bias) v += bias[nt * 16 + n];
+      store_one<TYPE>(out, (int64_t)(m0 + m) * ldo + nt * 16 + n, v);
+    }
+  }
+}
+
+template <int TYPE, int MT>
+void launch_few(const void* x, int64_t ldx, const void* tiles, const void* scales, int group, const float* bias, int M, int N, int K,
+                void* out, int64_t ldo, hipStream_t s) {
+  const dim3 grid((N + 15) / 16, (M + 16 * MT - 1) / (16 * MT)), block(1024 / MT);
+  const bool async = (uintptr_t)x % 4 == 0 && (M == 1 || ldx % 2 == 0);
+  const auto kern = group == 32 ? w4_few_kernel<TYPE, MT, 32> : group == 64 ? w4_few_kernel<TYPE, MT, 64> : w4_few_kernel<TYPE, MT, 128>;
+  launch_kernel(kern, grid, block, 0, s, static_cast<const uint16_t*>(x), ldx, async, static_cast<const u32x4*>(tiles),
+                static_cast<const uint32_t*>(scales), bias, M, N, K, out, ldo);
+  note_kernel("w4_few_kernel<%d,%d,%d> grid %dx%d block %d", TYPE, MT, group, (int)grid.x, (int)grid.y, (int)block.x);
+}
+
 // ---- many rows ----
 
 using f32x16 = float __attribute__((ext_vector_type(16)));
@@ -565,10 +668,10 @@ void launch_deep(const void* x, int64_t ldx, const void* tiles, const void* scal
   note_kernel("w4_deep_kernel<%d,%d,%d,%d,%d> grid %d block %d", TYPE, RB, CB, group, SPLIT, (int)grid.x, 256 * SPLIT);
 }
 
-// Few rows: 16 columns a workgroup, whatever bounds a stream of weights.  More: tiles of 64 x 64, or of 128 x 128 where they fill the chip.
-// bf16, 4096 x 4096, us, rows against tiles in four sets of waves: 16 rows 8.2, 17; 32 rows 12, 18; 64 rows 18 (four tiles of 16 a wave), 18;
-// 256 rows 61, 20.  In four, two, one set: 256 rows 20, 22, 28; 512 rows 37, 35, 36; 2048 rows 145, 127, 120, and 89 in tiles of 128 x 128.
-// f32: 64 rows 38, in tiles 94; 256 rows 152, 94; 2048 rows 1150, 294.
+// Few rows: 16 columns a workgroup, a stream of weights.  More: tiles of 64 x 64, or of 128 x 128 where they fill the chip.
+// bf16, 4096 columns, K = 4096, us: 16 rows 8.0, through LDS 5.7; 32 rows 11.8, 6.6, in tiles in four sets of waves 18; 64 rows 18, 11.5, 18; of
+// 9216 columns 32 rows 16 through LDS, in tiles 18, 64 rows 30 and 18.  In four, two, one set: 256 rows 20, 22, 28; 512 rows 37, 35, 36;
+// 2048 rows 145, 127, 120, and 89 in tiles of 128 x 128.  f32: 64 rows 38, in tiles 94; 256 rows 152, 94; 2048 rows 1150, 294.
 template <int TYPE>
 void launch_typed(const void* x, int64_t ldx, const void* tiles, const void* scales, int group, const float* bias, int M, int N, int K,
                   void* out, int64_t ldo, hipStream_t s) {
@@ -581,6 +684,10 @@ void launch_typed(const void* x, int64_t ldx, const void* tiles, const void* sca
       note_kernel("w4_f32_kernel<%d> grid %d block 256", group, (int)grid.x);
       return;
     }
+  } else if (M > 8 && M <= 64 && N <= 6144 && ldx < (1 << 24)) {
+    const auto f = M <= 32 ? launch_few<TYPE, 2> : launch_few<TYPE, 4>;
+    f(x, ldx, tiles, scales, group, bias, M, N, K, out, ldo, s);
+    return;
   } else if ((M > 32 || (M > 16 && N > 6144)) && ldx < (1 << 24)) {  // (offsets within a tile's rows in 32 bits)
     const auto f = group == 128 && large >= 256 ? launch_deep<TYPE, 2, 2, 1> : small <= 256 ? launch_deep<TYPE, 1, 1, 4>
                  : small <= 512 ? launch_deep<TYPE, 1, 1, 2> : launch_deep<TYPE, 1, 1, 1>;
