@@ -102,3 +102,17 @@ def test_binding_refusals():
         B.kv_cache(1, 1, 64, block=48, device="cpu")
     pages, scales = B.kv_cache(3, 2, 80, 32, device="cpu")
     assert pages.shape == (3, 2, 2, 64 * 96) and scales.shape == (3, 2, 2, 2)
+
+
+def test_attention_workspace():
+    """What one token over a long sequence needs, and what is refused: none, too little, one on an odd address; sizes that are none."""
+    dims = (4, 80, 2, 4, 96, 2)
+    need = B.workspace_bytes(B.OP_KV_ATTENTION, dims)
+    assert need > 4 * 16384 and need % 256 == 0
+    c = cache(table_width=80, table_ld=80)
+    for ws, size, status in ((None, need, E_WS), (P, need - 1, E_WS), (P + 8, need, E_ALIGN)):
+        assert calls(c, ws=ws, ws_bytes=size)["attention"] == status
+    # rows enough to fill the chip are not split, and need none
+    assert B.workspace_bytes(B.OP_KV_ATTENTION, (64, 80, 8, 32, 128, 1)) == 0
+    for bad in ((4, 80, 2, 3, 96, 2), (-1, 80, 2, 4, 96, 2), (4, 80, 0, 4, 96, 2), (4, 80, 2, 4, 257, 2), (4, 80, 2, 4, 96)):
+        assert B.workspace_bytes(B.OP_KV_ATTENTION, bad) == 0
