@@ -22,9 +22,19 @@
 #include <initializer_list>
 #include <optional>
 #include <string>
+#include <type_traits>
 
 #include "../../include/bmx.h"
 #include "lazy_calls.h"
+
+// (found when they are called, not when the module is loaded: it also loads on a library that has the binary layers alone)
+#pragma weak bmx_w4_quantize
+#pragma weak bmx_w4_dequantize
+#pragma weak bmx_w4_fc
+#pragma weak bmx_kv_write
+#pragma weak bmx_kv_read
+#pragma weak bmx_kv_attention
+#pragma weak bmx_fresh_kv_attention
 
 namespace {
 
@@ -136,6 +146,8 @@ class Unlocked {
 // A call of the library without Python's lock; its arguments are read with it.
 template <class F, class... A>
 void call(const char* what, F f, A... args) {
+  if constexpr (std::is_pointer_v<F>)
+    if (!f) raise_value("%s: the loaded library has no such call%s%s", what);
   int status;
   {
     const Unlocked unlocked;
