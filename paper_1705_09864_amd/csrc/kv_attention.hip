@@ -95,9 +95,9 @@ struct Args {
   void* out;
   int64_t out_row, out_head;
   float* lse;
-  float* parts;      // [sequence, tile of rows, head][split][part_rows][ROW + 4]: the rows' results, maximum and sum
+  float* parts;      // [sequence, tile of rows, head][split][part_rows][ROW + 4]: the rows' results, maximum and sum (of many rows: as their lanes hold them)
   uint32_t* arrived; // [sequence, tile of rows, head]
-  int q_heads, share, rows, max_new, window, splits, part_rows;
+  int q_heads, share, rows, max_new, window, splits, part_rows, prompt_splits;
   int few;  // sequences of more rows than this are the other kernel's
   bool causal, aligned;
   float scale;
@@ -106,6 +106,7 @@ struct Args {
 constexpr int kWaves = 4;
 constexpr int kCounters = 16384;  // of the workspace's head; what needs more than these has rows enough not to be split
 constexpr int kMostSplits = 128;
+constexpr int kLeastPages = 16;   // of a split of many rows
 
 template <int TYPE, int DC>
 __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache c, Args a) {
@@ -393,13 +394,16 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
 // So where all of a page is seen and no scale of its values is far below the largest, the scale goes into the exponent,
 //   p c / C 2^14 = 2^(s + log2(c / C 2^14) - m),
 // and comes out of the sum of p again once for each 16 tokens.
-template <int TYPE, int DC>
+// SPLIT: tiles of rows fewer than the chip holds workgroups at once, whose pages are split and joined as above (a kernel of its own: the
+// splits' arithmetic in the one kernel cost it 1%).  512 new tokens over 4096: 68 us, 120 unsplit; the join is some 15 us of that.
+// Eight waves to a page, which halves the conversions, fill the chip less evenly: 272 us where 289 is, but 163 where 122, 713 where 677.
+template <int TYPE, int DC, bool SPLIT>
 __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_cache c, Args a) {
   static_assert(TYPE != BMX_F32, "");
   constexpr int ROW = DC * 32, WIDE = DC / 2, NS = DC * 2, VN = (DC + 3) / 4;  // NS: steps of 16 values; VN: 32-value tiles of V a wave brings in
   __shared__ u32x4 lds[2][2][NS * 128];                          // [buffer][keys, values]
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
-  const int head = blockIdx.x, seq = blockIdx.z;
+  const int head = SPLIT ? blockIdx.x % c.heads : blockIdx.x, split = SPLIT ? blockIdx.x / c.heads : 0, seq = blockIdx.z;
   const KvSpan s = kv_span(c, seq, a.rows, a.max_new);
   const int rows = s.count * a.share;
   const int r0 = ((rows + 127) / 128 - 1 - (int)blockIdx.y) * 128;  // (the last rows, which see most, first)
@@ -420,7 +424,15 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
   u32x2 kt;
   float scale_in = 0.0f;  // lanes 0 to 3: the coming page's scales of keys; 4 to 7: of values
   const int scale_at = (lane / 4 % 2) * blocks + (lane % 4 * 16 >> log_block);
-  const int last = (high_group + kPage - 1) / kPage;
+  int begin = low_group / kPage, last = (high_group + kPage - 1) / kPage, used = 1;
+  if constexpr (SPLIT) {  // this split's pages: as many for the rows that see few as for those that see most, which then are in fewer splits
+    const int pages = max(last - begin, 0), most_pages = (s.length + kPage - 1) / kPage - first_seen(token_of((rows - 1) / 128 * 128)) / kPage;
+    const int per = max((max(most_pages, pages) + a.prompt_splits - 1) / a.prompt_splits, kLeastPages);
+    used = max((pages + per - 1) / per, 1);
+    if (split >= used) return;
+    last = begin + min(pages, (split + 1) * per);
+    begin += split * per;
+  }
   // the first page from `pg` on that is there, on its way into registers
   const auto fetch = [&](int pg) {
     int page = -1;
@@ -458,7 +470,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
       for (int u = 0; u < 4; ++u) lds[buf][1][(u * DC + wave + 4 * n) * 64 + lane] = eight_levels<true>(vr[n][0][u], vr[n][1][u]);
     }
   };
-  int pg = fetch(low_group / kPage);
+  int pg = fetch(begin);
 
   u32x4 q[NS];
   float factor;
@@ -584,6 +596,48 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
     __syncthreads();
   }
   l += __shfl_xor(l, 32);
+  if (SPLIT && used > 1) {  // the parts: each lane's numbers at the same place in all of them
+    const int64_t unit = ((int64_t)seq * ((a.max_new * a.share + 127) / 128) + r0 / 128) * c.heads + head;
+    constexpr int PART = 64 * (DC * 16 + 2);
+    float* at = a.parts + (unit * a.prompt_splits * 4 + wave) * PART + lane * 2;
+    if (r_wave < rows) {
+      float* to = at + (int64_t)split * 4 * PART;
+      const float unit_of = most * 0x1p-14f;
+#pragma unroll
+      for (int n = 0; n < DC; ++n)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) put(to + (n * 8 + i) * 128, o[n][2 * i] * unit_of, o[n][2 * i + 1] * unit_of);
+      put(to + DC * 1024, m, l);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's numbers are there
+    __shared__ uint32_t place;
+    __syncthreads();
+    if (threadIdx.x == 0) place = __hip_atomic_fetch_add(a.arrived + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (place != (uint32_t)used - 1) return;
+    if (threadIdx.x == 0) __hip_atomic_store(a.arrived + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (r_wave >= rows) return;
+    m = -INFINITY, l = 0.0f, most = 0x1p14f;
+    for (int p = 0; p < used; ++p) {
+      const float* from = at + (int64_t)p * 4 * PART;
+      const u32x2 x = get(from + DC * 1024);
+      u32x2 y[DC * 8];  // (every read at once: each is a trip to memory)
+#pragma unroll
+      for (int i = 0; i < DC * 8; ++i) y[i] = get(from + i * 128);
+      const uint32_t x0 = x[0], x1 = x[1];
+      const float m_part = __builtin_bit_cast(float, x0), m_new = fmaxf(m, m_part), m_at = m_new == -INFINITY ? 0.0f : m_new;
+      const float f = __builtin_amdgcn_exp2f(m - m_at), f_part = __builtin_amdgcn_exp2f(m_part - m_at);
+      l = l * f + __builtin_bit_cast(float, x1) * f_part;
+      m = m_new;
+#pragma unroll
+      for (int n = 0; n < DC; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t v = y[n * 8 + i / 2][i % 2];
+          o[n][i] = (p == 0 ? 0.0f : o[n][i] * f) + __builtin_bit_cast(float, v) * f_part;
+        }
+    }
+  }
   if (r >= rows) return;
   const int64_t at = (s.row0 + token) * a.out_row + (head * a.share + r % a.share) * a.out_head;
   // (a row that sees nothing is zeros)
@@ -602,7 +656,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
 // What a call needs: tiles of rows, splits, and bytes of the workspace.
 struct Plan {
   int64_t units, tiles, prompt_tiles;  // prompt_tiles: of 128 rows, 0 where they are too few to fill the chip
-  int splits, part_rows, few;
+  int splits, part_rows, few, prompt_splits;
   size_t bytes;
 };
 Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new, int type) {
@@ -623,6 +677,14 @@ Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads
   p.splits = (int)std::max<int64_t>(std::min({ceil_div(256, std::max<int64_t>(p.units, 1)), ceil_div(table_width, 4), (int64_t)kMostSplits}), 1);
   if (p.units > kCounters) p.splits = 1;
   p.bytes = p.splits == 1 ? 0 : kCounters * 4 + (size_t)p.units * p.splits * p.part_rows * (kv_row_bytes((int)dim) + 4) * 4;
+  p.prompt_splits = 1;
+  if (p.prompt_tiles) {
+    const int64_t units = p.prompt_tiles * heads * sequences;
+    // As many workgroups as the chip holds at once, two a CU up to 128 values and one beyond, of 16 pages each at least (a join is four pages' time).
+    // 512 new tokens, 32 heads on 8 of 128, over 4096 with 128, 256, 512 workgroups: 122, 72, 68 us; over 2048: 67, 46, 50.
+    p.prompt_splits = (int)std::max<int64_t>(std::min<int64_t>((dim <= 128 ? 512 : 256) / units, table_width / kLeastPages), 1);
+    if (p.prompt_splits > 1) p.bytes = std::max(p.bytes, kCounters * 4 + (size_t)units * p.prompt_splits * 128 * (kv_row_bytes((int)dim) + 4) * 4);
+  }
   return p;
 }
 
@@ -636,11 +698,11 @@ void launch(const bmx_kv_cache& c, const Args& a, const Plan& p, hipStream_t s) 
   }
   if constexpr (TYPE != BMX_F32) {
     if (p.prompt_tiles) {
-      const dim3 grid(c.heads, (uint32_t)p.prompt_tiles, c.sequences);
+      const dim3 grid(c.heads * a.prompt_splits, (uint32_t)p.prompt_tiles, c.sequences);
       Args b = a;
       if (!c.starts || c.sequences == 1) b.few = 0;
-      launch_kernel(kv_prompt_kernel<TYPE, DC>, grid, dim3(256), 0, s, c, b);
-      note_kernel("kv_prompt_kernel<%d,%d> grid %ux%ux%u block 256", TYPE, DC, grid.x, grid.y, grid.z);
+      launch_kernel(a.prompt_splits > 1 ? kv_prompt_kernel<TYPE, DC, true> : kv_prompt_kernel<TYPE, DC, false>, grid, dim3(256), 0, s, c, b);
+      note_kernel("kv_prompt_kernel<%d,%d,%d> grid %ux%ux%u block 256", TYPE, DC, a.prompt_splits > 1, grid.x, grid.y, grid.z);
     }
   }
 }
@@ -670,8 +732,9 @@ hipError_t launch_kv_attention(const bmx_kv_cache& c, const void* q, int type, i
   const Plan p = plan(c.sequences, c.table_width, c.heads, q_heads, c.dim, max_new, type);
   uint32_t* arrived = static_cast<uint32_t*>(workspace);
   const Args a = {q, q_row, q_head, out, out_row, out_head, lse, reinterpret_cast<float*>(arrived + kCounters), arrived, q_heads,
-                  q_heads / c.heads, rows, max_new, window, p.splits, p.part_rows, p.few, causal, aligned, scale};
-  if (fresh && p.splits > 1) launch_kernel(clear_kernel, dim3((uint32_t)ceil_div(p.units, 256)), dim3(256), 0, s, arrived);
+                  q_heads / c.heads, rows, max_new, window, p.splits, p.part_rows, p.prompt_splits, p.few, causal, aligned, scale};
+  const int64_t counters = std::max(p.splits > 1 ? p.units : 0, p.prompt_splits > 1 ? p.prompt_tiles * c.heads * c.sequences : 0);
+  if (fresh && counters) launch_kernel(clear_kernel, dim3((uint32_t)ceil_div(counters, 256)), dim3(256), 0, s, arrived);
   const auto f = type == BMX_F32 ? launch_typed<BMX_F32> : type == BMX_F16 ? launch_typed<BMX_F16> : launch_typed<BMX_BF16>;
   f(c, a, p, s);
   return launch_error();

@@ -617,6 +617,30 @@ def test_kv_attention_one_workspace_for_calls_of_all_sizes():
             assert torch.equal(o, B.kv_attention(q, c.pages, c.scales, c.table, c.lens(), workspace=ws))
 
 
+@pytest.mark.parametrize("lengths,rows,heads,share,dim,block,kind,splits", [
+    ([4400], [130], 16, 8, 64, 16, "bf16", 3), ([2500], [300], 8, 7, 128, 32, "f16", 2), ([2100], [70], 16, 16, 200, 16, "bf16", 1),
+    ([2100], [60], 16, 16, 200, 16, "bf16", 2), ([4400, 2100, 300, 0], [100, 12, 5, 3], 8, 8, 96, 64, "f16", 2),
+    ([1, 2600], [40, 90], 12, 8, 20, 16, "bf16", 2)])
+def test_kv_attention_many_rows_long(lengths, rows, heads, share, dim, block, kind, splits):
+    """Many rows over sequences so long that workgroups share their pages: with sequences of few rows and none beside them, rows of positions
+    below 0, windows; and the same bits in several calls and on a workspace that goes from one to the next."""
+    width = -(-max(lengths) // 64) + 2
+    c = Cache(len(lengths), width, heads, dim, block, 40 + dim)
+    g = fill(c, lengths, kind, dim)
+    q = torch.randn((sum(rows), heads * share, dim), device="cuda", generator=g).to(TYPES[kind][0])
+    starts = torch.tensor(np.cumsum([0] + rows), dtype=torch.int32, device="cuda")
+    need = B.workspace_bytes(B.OP_KV_ATTENTION, (len(lengths), width, heads, heads * share, dim, max(rows)))
+    ws = torch.zeros((max(need, 16),), dtype=torch.uint8, device="cuda")
+    for causal, window in ((True, 0), (False, 0), (True, 1500), (False, 1100)):
+        out, lse = B.kv_attention(q, c.pages, c.scales, c.table, c.lens(), starts=starts, max_new=max(rows), causal=causal, window=window, lse=True)
+        name = B.last_kernel()
+        assert "kv_prompt_kernel" in name and int(name.split("grid ")[1].split("x")[0]) == splits * heads
+        check_attention(out, q, c, rows, kind, causal, window, lse=lse)
+        for _ in range(3):
+            assert torch.equal(out, B.kv_attention(q, c.pages, c.scales, c.table, c.lens(), starts=starts, max_new=max(rows), causal=causal,
+                                                   window=window, workspace=ws))
+
+
 def test_decoder_calls_in_a_graph():
     """A step of a layer captured once and replayed on new inputs, with eager work between the replays."""
     heads, dim, seqs = 2, 64, 3
