@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "../../include/bmx.h"
+#include "kv_range.h"
 
 namespace bmx {
 
@@ -14,8 +15,6 @@ using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
 using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
-
-constexpr int kPage = 64;  // tokens of a page
 
 __host__ __device__ static inline int type_bytes(int type) { return type == BMX_F32 ? 4 : 2; }
 // Bytes that a token's head takes in a page.
@@ -62,28 +61,10 @@ __device__ static inline void load_eight(const void* p, int64_t at, int left, bo
   }
 }
 
-// Which rows, positions and pages are a sequence's.  lengths and starts come from device memory: whatever they hold, the
-// rows stay inside [0, rows), the positions inside the table.
-struct KvSpan {
-  int row0, count;  // its new rows
-  int first;        // position of the first of them (negative where there are more rows than tokens)
-  int length;       // its tokens, new ones included, as far as the table reaches
-};
+// A sequence's rows and positions (lengths and starts come from device memory).
 __device__ static inline KvSpan kv_span(const bmx_kv_cache& c, int seq, int rows, int max_new) {
-  KvSpan s;
-  if (c.starts) {
-    s.row0 = min(max(c.starts[seq], 0), rows);
-    s.count = min(max(c.starts[seq + 1], s.row0), rows) - s.row0;
-  } else {
-    s.count = rows / c.sequences;
-    s.row0 = seq * s.count;
-  }
-  s.count = min(s.count, max_new);
-  const int64_t most = (int64_t)c.table_width * kPage;
-  const int n = max(c.lengths[seq], 0);
-  s.first = n - s.count;
-  s.length = (int)(n < most ? n : most);
-  return s;
+  const int each = c.starts ? 0 : rows / c.sequences, begin = c.starts ? c.starts[seq] : seq * each, end = c.starts ? c.starts[seq + 1] : begin + each;
+  return kv_span_of(begin, end, c.lengths[seq], rows, max_new, c.table_width);
 }
 // The page at place `at` of a sequence's row of the table; negative where there is none.
 __device__ static inline int kv_page(const bmx_kv_cache& c, int seq, int at) {

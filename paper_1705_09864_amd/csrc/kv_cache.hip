@@ -113,20 +113,11 @@ __device__ inline bool page_of(const bmx_kv_cache& c, int rows, int max_new, int
   const int seq = blockIdx.x / span, head = blockIdx.y / 2, which = blockIdx.y % 2;
   const KvSpan s = kv_span(c, seq, rows, max_new);
   if (s.count == 0) return false;
+  const int low = FLOOR ? s.first : max(s.first, 0), high = FLOOR ? s.first + s.count : s.length;
   int pg;
-  if constexpr (FLOOR) {
-    pg = (s.first < 0 ? (s.first - (kPage - 1)) / kPage : s.first / kPage) + blockIdx.x % span;
-    if (pg * kPage >= s.first + s.count) return false;
-    p->page = pg < 0 || pg >= c.table_width ? -1 : kv_page(c, seq, pg);
-    p->t1 = min(s.first + s.count - pg * kPage, kPage);
-  } else {
-    pg = max(s.first, 0) / kPage + blockIdx.x % span;
-    if (pg * kPage >= s.length) return false;
-    p->page = kv_page(c, seq, pg);
-    if (p->page < 0) return false;
-    p->t1 = min(s.length - pg * kPage, kPage);
-  }
-  p->t0 = max((FLOOR ? s.first : max(s.first, 0)) - pg * kPage, 0);
+  if (!kv_page_at(low, high, blockIdx.x % span, &pg, &p->t0, &p->t1)) return false;
+  p->page = pg < 0 || pg >= c.table_width ? -1 : kv_page(c, seq, pg);
+  if (!FLOOR && p->page < 0) return false;
   p->log_block = 31 - __builtin_clz(c.block);
   const int64_t unit = ((int64_t)max(p->page, 0) * c.heads + head) * 2 + which;
   p->body = c.pages + unit * kPage * kv_row_bytes(c.dim);
@@ -416,7 +407,7 @@ auto pick_read(int dim) {
 
 hipError_t launch_kv_write(const bmx_kv_cache& c, const void* k, const void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row,
                            int64_t v_head, int rows, int max_new, hipStream_t s) {
-  const int span = (max_new + kPage - 2) / kPage + 1;
+  const int span = (int)kv_pages_of(max_new);
   const dim3 grid((uint32_t)(c.sequences * (int64_t)span), c.heads * 2);
   // (64 sequences, 8 heads of 128 bf16: 1 token each 4.9 us, and by pages 9.5; 8 tokens 15.5 and 18.4 with a read of one behind them; 16 tokens 20.1, 19.3)
   if (max_new <= 8) {
@@ -433,7 +424,7 @@ hipError_t launch_kv_write(const bmx_kv_cache& c, const void* k, const void* v, 
 
 hipError_t launch_kv_read(const bmx_kv_cache& c, void* k, void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head,
                           int rows, int max_new, hipStream_t s) {
-  const int span = (max_new + kPage - 2) / kPage + 1;
+  const int span = (int)kv_pages_of(max_new);
   const dim3 grid((uint32_t)(c.sequences * (int64_t)span), c.heads * 2);
   const auto kern = type == BMX_F32 ? pick_read<BMX_F32>(c.dim) : type == BMX_F16 ? pick_read<BMX_F16>(c.dim) : pick_read<BMX_BF16>(c.dim);
   launch_kernel(kern, grid, dim3(256), 0, s, c, k, v, k_row, k_head, v_row, v_head, rows, max_new, span);
