@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
   const int high_any = a.causal ? min(s.first + tok1 + 1, s.length) : s.length, high_all = a.causal ? min(s.first + tok0 + 1, s.length) : s.length;
   const int low_any = a.window ? max(max(s.first + tok0, 0) - a.window + 1, 0) : 0, low_all = a.window ? max(max(s.first + tok1, 0) - a.window + 1, 0) : 0;
   // this workgroup's pages
-  const int page0 = low_any / kPage, pages = max((high_any + kPage - 1) / kPage - page0, 0);
+  const int page0 = low_any / kPage, pages = max(kv_pages_to(high_any) - page0, 0);
   // (to join parts takes as long as two pages of a wave, so up to three pages each stay in one workgroup: 8 pages 7.8 us, in two 9.3;
   // 16 pages 10.6, in four 9.3)
   const int per = pages <= 3 * kWaves ? pages : max((pages + a.splits - 1) / a.splits, kWaves), used = pages > 0 ? (pages + per - 1) / per : 1;
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
       for (int i = 0; i < 4; ++i) p[u][i] = z[i];
     }
     load_keys();
-    if (t0 >= low_all && t0 + kPage <= high_all) {
+    if (kv_all_in(t0, kPage, low_all, high_all)) {
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const float f = factor * key_scale[u];
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
       for (int u = 0; u < 4; ++u) {
         const int t = t0 + 16 * u;
         const float f = factor * key_scale[u];
-        if (t >= high_any || t + 16 <= low_any) value_scale[u] = 0.0f;  // (a block that nobody has written has any scale)
+        if (t >= high_any || t + 15 < low_any) value_scale[u] = 0.0f;  // (a block that nobody has written has any scale)
         most_new = fmaxf(most_new, value_scale[u]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -424,9 +424,9 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
   u32x2 kt;
   float scale_in = 0.0f;  // lanes 0 to 3: the coming page's scales of keys; 4 to 7: of values
   const int scale_at = (lane / 4 % 2) * blocks + (lane % 4 * 16 >> log_block);
-  int begin = low_group / kPage, last = (high_group + kPage - 1) / kPage, used = 1;
+  int begin = low_group / kPage, last = kv_pages_to(high_group), used = 1;
   if constexpr (SPLIT) {  // this split's pages: as many for the rows that see few as for those that see most, which then are in fewer splits
-    const int pages = max(last - begin, 0), most_pages = (s.length + kPage - 1) / kPage - first_seen(token_of((rows - 1) / 128 * 128)) / kPage;
+    const int pages = max(last - begin, 0), most_pages = kv_pages_to(s.length) - first_seen(token_of((rows - 1) / 128 * 128)) / kPage;
     const int per = max((max(most_pages, pages) + a.prompt_splits - 1) / a.prompt_splits, kLeastPages);
     used = max((pages + per - 1) / per, 1);
     if (split >= used) return;
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
   f32x16 o[DC] = {};
   for (int buf = 0; pg < last; buf ^= 1) {
     const int next = fetch(pg + 1), t0 = pg * kPage;
-    if (t0 < high_any && t0 + kPage > low_any) {
+    if (t0 < high_any && t0 + kPage - 1 >= low_any) {
       f32x16 z[2] = {};
 #pragma unroll
       for (int i = 0; i < NS; ++i)
@@ -518,7 +518,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
       for (int u = 0; u < 4; ++u) {
         key_scale[u] = factor * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale_of), u));
         value_scale[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale_of), 4 + u));
-        if (t0 + 16 * u >= high_any || t0 + 16 * u + 16 <= low_any) value_scale[u] = 0.0f;  // (a block that nobody has written has any scale)
+        if (t0 + 16 * u >= high_any || t0 + 16 * u + 15 < low_any) value_scale[u] = 0.0f;  // (a block that nobody has written has any scale)
         most_new = fmaxf(most_new, value_scale[u]);
       }
       // (scales below 2^-126 are those of levels that are all 0)
@@ -526,7 +526,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
       float f[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) f[u] = value_scale[u] * inverse * 0x1p14f;
-      const bool full = __builtin_amdgcn_readfirstlane(t0 >= low_all && t0 + kPage <= high_all && fminf(fminf(f[0], f[1]), fminf(f[2], f[3])) >= 0x1p-8f);
+      const bool full = __builtin_amdgcn_readfirstlane(kv_all_in(t0, kPage, low_all, high_all) && fminf(fminf(f[0], f[1]), fminf(f[2], f[3])) >= 0x1p-8f);
       u32x4 w[4];
       if (full) {
 #pragma unroll

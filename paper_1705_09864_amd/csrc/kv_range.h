@@ -38,4 +38,8 @@ __host__ __device__ static inline bool kv_page_at(int low, int high, int at, int
 // How many pages a sequence's new rows lie in at most.
 __host__ __device__ static inline int64_t kv_pages_of(int max_new) { return ((int64_t)max_new + kPage - 2) / kPage + 1; }
 
+// How many pages positions 0 to `end` (not it) lie in, and whether the n positions from t0 on are all in [low, high); t0 + n - 1 fits.
+__host__ __device__ static inline int kv_pages_to(int end) { return end > 0 ? (end - 1) / kPage + 1 : 0; }
+__host__ __device__ static inline bool kv_all_in(int t0, int n, int low, int high) { return t0 >= low && high >= n && t0 <= high - n; }
+
 }  // namespace bmx

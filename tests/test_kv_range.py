@@ -16,6 +16,8 @@ extern "C" void span_of(int begin, int end, int tokens, int rows, int max_new, i
   out[0] = s.row0, out[1] = s.count, out[2] = s.first, out[3] = s.length;
 }
 extern "C" int page_at(int low, int high, int at, int* out) { return bmx::kv_page_at(low, high, at, out, out + 1, out + 2); }
+extern "C" int pages_to(int end) { return bmx::kv_pages_to(end); }
+extern "C" int all_in(int t0, int n, int low, int high) { return bmx::kv_all_in(t0, n, low, high); }
 extern "C" int64_t pages_of(int max_new) { return bmx::kv_pages_of(max_new); }
 """
 TOP = 2**31 - 1
@@ -80,3 +82,12 @@ def test_pages_of_a_launch(lib):
     for n in (0, 1, 2, 3, 63, 64, 65, 66, 67, TOP - 63, TOP - 62, TOP - 61, TOP):
         most = max((low + n - 1) // 64 - low // 64 + 1 for low in (0, 1, 31, 62, 63)) if n else 0
         assert most <= lib.pages_of(n) <= n // 64 + 2
+
+
+def test_pages_and_places_that_a_row_sees(lib):
+    for end in NUMBERS:
+        assert lib.pages_to(end) == max(0, -(-end // 64))
+    for t0 in [0, 64, 128, (TOP >> 6 << 6) - 64, TOP >> 6 << 6]:
+        for low in NUMBERS[3:]:
+            for high in NUMBERS:
+                assert bool(lib.all_in(t0, 64, low, high)) == (t0 >= low and t0 + 64 <= high)

@@ -27,3 +27,24 @@ def test_kv_lengths_at_the_end_of_32_bits(rows, below):
         assert not bool(x[:rows].any()) and float((x[rows:] - kv[rows:]).abs().max()) < 0.03
     out = B.kv_attention(torch.randn((2 * rows, heads, dim), device="cuda"), pages, scales, table, lengths)
     assert bool(torch.isfinite(out).all())
+
+
+def test_kv_attention_positions_at_the_end_of_32_bits():
+    """A table as wide as positions have room for, of which the last pages are there: what a short table of the same pages gives."""
+    heads, dim, width, there = 1, 32, 1 << 25, 40
+    pages, scales = B.kv_cache(there, heads, dim)
+    pages.random_(-127, 128)
+    scales.uniform_(0.001, 0.01)
+    scales[-1, :, :, -1] = 0.004
+    short = torch.arange(there, dtype=torch.int32, device="cuda")[None]
+    wide = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    wide[:, -there:] = short
+    lengths = [torch.tensor([n], dtype=torch.int32, device="cuda") for n in (there * 64 - 1, TOP)]
+    for rows, share, window, causal in ((1, 1, 100, True), (3, 4, 700, True), (5, 2, 100, False), (2048, 8, 100, True)):
+        for kind in (torch.float32, torch.bfloat16):
+            if rows * share > 64 and kind == torch.float32:
+                continue
+            q = torch.randn((rows, share, dim), device="cuda").to(kind)
+            want, got = (B.kv_attention(q, pages, scales, t, n, causal=causal, window=window) for t, n in zip((short, wide), lengths))
+            assert float(want.float().abs().min()) > 0 or rows > 64
+            assert float((got.float() - want.float()).abs().max()) <= 2.0**-7 * float(want.float().abs().max()), (rows, kind)
