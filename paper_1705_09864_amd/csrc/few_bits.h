@@ -79,7 +79,9 @@ __device__ static inline int kv_key_at(int row, int t, int d) {
 }
 __device__ static inline int kv_value_at(int t, int d) { return d / 16 * 1024 + t % 16 / 4 * 256 + d % 16 * 16 + t / 16 * 4 + t % 4; }
 
-// Memory as a buffer of so many bytes: a read behind its end gives zeros and moves nothing.
+// Memory as a buffer of so many bytes.  A read whose lane_at is behind its end gives zeros and moves nothing; what the hardware compares with the end
+// need not hold `at`, so lane_at alone says whether there is anything to read (kNowhere added: there is not).
+constexpr int kNowhere = 1 << 30;
 using Rsrc = __amdgpu_buffer_rsrc_t;
 __device__ inline Rsrc buffer(const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000); }
 // (lane_at differs from lane to lane, at does not)

@@ -149,20 +149,22 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
       if (page >= 0) break;
     }
     at = next++;
-    const Rsrc r = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)head * 2 * kPage * ROW, page >= 0 ? kPage * ROW : 0);
+    const int none = page >= 0 ? 0 : kNowhere;
+    const Rsrc r = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)head * 2 * kPage * ROW, kPage * ROW);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
 #pragma unroll
-      for (int w = 0; w < WIDE; ++w) k[u][w] = load16(r, lane * 16, u * 16 * ROW + w * 1024);
-      if constexpr (DC % 2) k_tail[u] = load8(r, lane * 8, u * 16 * ROW + WIDE * 1024);
+      for (int w = 0; w < WIDE; ++w) k[u][w] = load16(r, lane * 16 + none, u * 16 * ROW + w * 1024);
+      if constexpr (DC % 2) k_tail[u] = load8(r, lane * 8 + none, u * 16 * ROW + WIDE * 1024);
     }
-    const Rsrc rs = buffer(c.scales + ((int64_t)max(page, 0) * c.heads + head) * 2 * blocks, page >= 0 ? 8 * blocks : 0);
-    scale_of = __builtin_bit_cast(float, load4(rs, scale_at * 4, 0));
+    const Rsrc rs = buffer(c.scales + ((int64_t)max(page, 0) * c.heads + head) * 2 * blocks, 8 * blocks);
+    scale_of = __builtin_bit_cast(float, load4(rs, scale_at * 4 + none, 0));
   };
   const auto load_values = [&] {
-    const Rsrc r = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)(head * 2 + 1) * kPage * ROW, page >= 0 ? kPage * ROW : 0);
+    const int none = page >= 0 ? 0 : kNowhere;
+    const Rsrc r = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)(head * 2 + 1) * kPage * ROW, kPage * ROW);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) v[dt] = load16(r, lane * 16, dt * 1024);
+    for (int dt = 0; dt < DT; ++dt) v[dt] = load16(r, lane * 16 + none, dt * 1024);
   };
   load_keys();
   load_values();
@@ -433,6 +435,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
     last = begin + min(pages, (split + 1) * per);
     begin += split * per;
   }
+  const int none = c.num_pages > 0 ? 0 : kNowhere;
   // the first page from `pg` on that is there, on its way into registers
   const auto fetch = [&](int pg) {
     int page = -1;
@@ -440,17 +443,18 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
       page = kv_page(c, seq, pg);
       if (page >= 0) break;
     }
-    const Rsrc rk = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)head * 2 * kPage * ROW, page >= 0 ? 2 * kPage * ROW : 0);
-    const Rsrc rs = buffer(c.scales + ((int64_t)max(page, 0) * c.heads + head) * 2 * blocks, page >= 0 ? 8 * blocks : 0);
-    scale_in = __builtin_bit_cast(float, load4(rs, scale_at * 4, 0));
+    // (behind the last page: page 0 once more, which nobody uses; a branch here cost 5% at 256 values a head)
+    const Rsrc rk = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)head * 2 * kPage * ROW, 2 * kPage * ROW);
+    const Rsrc rs = buffer(c.scales + ((int64_t)max(page, 0) * c.heads + head) * 2 * blocks, 8 * blocks);
+    scale_in = __builtin_bit_cast(float, load4(rs, scale_at * 4 + none, 0));
 #pragma unroll
-    for (int w = 0; w < WIDE; ++w) kr[w] = load16(rk, lane * 16, wave * 16 * ROW + w * 1024);
-    if constexpr (DC % 2) kt = load8(rk, lane * 8, wave * 16 * ROW + WIDE * 1024);
+    for (int w = 0; w < WIDE; ++w) kr[w] = load16(rk, lane * 16 + none, wave * 16 * ROW + w * 1024);
+    if constexpr (DC % 2) kt = load8(rk, lane * 8 + none, wave * 16 * ROW + WIDE * 1024);
 #pragma unroll
     for (int n = 0; n < VN; ++n) {
       const int q = min(wave + 4 * n, DC - 1);
 #pragma unroll
-      for (int g = 0; g < 2; ++g) vr[n][g] = load16(rk, (lane % 32 / 16) * 1024 + h * 256 + lane % 16 * 16, kPage * ROW + q * 2048 + g * 512);
+      for (int g = 0; g < 2; ++g) vr[n][g] = load16(rk, (lane % 32 / 16) * 1024 + h * 256 + lane % 16 * 16 + none, kPage * ROW + q * 2048 + g * 512);
     }
     return pg;
   };

@@ -7,6 +7,7 @@
 // three bf16 parts (24 bits together), against q - 8.
 #include "bmx_internal.h"
 #include "few_bits.h"
+#include "k_steps.h"
 
 #include <algorithm>
 
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(kMostWaves * 64) void w4_rows_kernel(const void* x,
 #pragma unroll
     for (int gi = 0; gi < PER; ++gi) sb[d][gi] = load16(scale_rows, g * 16, (kt * PER + gi) * 64);
   };
-  const auto load_x = [&](int d, int kt, int i, int step) { xs[d][i][step].load(x, row[i] + min(kt, full - 1) * 128 + 32 * step); };
+  const auto load_x = [&](int d, int kt, int i, int step) { xs[d][i][step].load(x, row[i] + kt * 128 + 32 * step); };
   // a step's products; next: the step to load in its place
   const auto multiply = [&](int d, int groups, int next) {
 #pragma unroll
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(kMostWaves * 64) void w4_rows_kernel(const void* x,
   if (wave < full) {
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
-      const int kt = wave + d * waves;
+      const int kt = k_step(wave, waves, d, full);
       load(d, kt);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(kMostWaves * 64) void w4_rows_kernel(const void* x,
     for (int kt = wave; kt < full;) {
 #pragma unroll
       for (int d = 0; d < DEPTH; ++d) {
-        if (kt < full) multiply(d, PER, kt + DEPTH * waves);
+        if (kt < full) multiply(d, PER, k_step(kt, waves, DEPTH, full));
         kt += waves;
       }
     }
