@@ -320,7 +320,7 @@ typedef struct bmx_kv_cache {
  *   that holds older tokens keeps its scale s_old unless a new value is past 127 * s_old, and then the older levels become
  *   round(q * (s_old / s)).  New levels are round(x * (1 / s)) (all 0 where s < 2^-126), to the nearest, ties to even.  Scales are taken over
  *   finite values; an infinity is level +-127, NaN is level 0.
- * bmx_kv_read: the rows' values q * scale; rows of tokens that are not there are zeros.
+ * bmx_kv_read: the rows' values q * scale, an fp32 product rounded to the type; rows of tokens that are not there are zeros.
  * bmx_kv_attention: out = softmax(scale * q k^T) v with q_heads heads of queries, a multiple of cache->heads: head h reads head
  *   h / (q_heads / heads) of the cache.  A row at position p sees the tokens t < its sequence's length, with causal those t <= p, with
  *   window > 0 those t > p - window.  A row that sees nothing is zeros.  lse fp32 [rows][q_heads] or NULL: the logarithm of the

@@ -100,6 +100,14 @@ __device__ inline float byte_of(const u32x4& b, int j) {
   return (float)(int8_t)(w >> (8 * (j % 4)));
 }
 
+// A level's value: the 32-bit product, which the type's rounding follows.  (Without the barrier f16 would be one rounding of the exact product,
+// v_fma_mixlo_f16, and a value read as f16 another than the same value read as f32 and rounded.)
+__device__ inline float value_of(float level, float scale) {
+  float x = level * scale;
+  asm("" : "+v"(x));
+  return x;
+}
+
 // A page of one head, its keys or its values, and the new tokens in it: [t0, t1).
 struct Page {
   int8_t* body;
@@ -367,7 +375,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(bmx_kv_cache c, void* k, v
       }
       Run<TYPE, 16> x;
 #pragma unroll
-      for (int j = 0; j < 16; j += 2) x.set2(j, byte_of(q, j) * s, byte_of(q, j + 1) * s);
+      for (int j = 0; j < 16; j += 2) x.set2(j, value_of(byte_of(q, j), s), value_of(byte_of(q, j + 1), s));
       x.store(k, p.base + t * x_row + d, c.dim - d);
     }
   } else {
@@ -387,7 +395,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(bmx_kv_cache c, void* k, v
       for (int j = 0; j < 16; ++j) {
         const int t = j / 4 * 16 + 4 * wave + j % 4;
         Run<TYPE, 2> x;
-        x.set2(0, byte_of(q[0], j) * s[j / 4], byte_of(q[1], j) * s[j / 4]);
+        x.set2(0, value_of(byte_of(q[0], j), s[j / 4]), value_of(byte_of(q[1], j), s[j / 4]));
         if (t >= p.t0 && t < p.t1) x.store(v, p.base + t * x_row + d, c.dim - d);
       }
     }

@@ -48,3 +48,35 @@ def test_kv_attention_positions_at_the_end_of_32_bits():
             want, got = (B.kv_attention(q, pages, scales, t, n, causal=causal, window=window) for t, n in zip((short, wide), lengths))
             assert float(want.float().abs().min()) > 0 or rows > 64
             assert float((got.float() - want.float()).abs().max()) <= 2.0**-7 * float(want.float().abs().max()), (rows, kind)
+
+
+def test_kv_read_rounds_the_product():
+    """Levels and scales whose fp32 product lies halfway between two 16-bit values, and the exact product beside it: the product is rounded to
+    fp32, then to the type, whatever the type, for keys as for values."""
+    rng = np.random.default_rng(0)
+    found = []
+    while len(found) < 64:
+        s = rng.uniform(0.001, 0.1, 400000).astype(np.float32)
+        q = rng.integers(1, 128, s.size)
+        exact = s.astype(np.float64) * q
+        other = np.flatnonzero(exact.astype(np.float16) != exact.astype(np.float32).astype(np.float16))
+        found += [(s[i], q[i]) for i in other]
+    dim, n = 64, 64  # a block of 16 tokens for each pair, four to a page
+    pages, scales = B.kv_cache(n // 4, 1, dim)
+    s = torch.tensor([a for a, _ in found[:n]]).view(n // 4, 1, 1, 4)
+    q = torch.tensor([b for _, b in found[:n]]).view(n // 4, 4)
+    scales.copy_(s.expand(-1, -1, 2, -1))
+    t, d = np.arange(64)[:, None], np.arange(dim)[None, :]
+    key = t // 16 * 16 * dim + d % 64 // 16 * 256 + t % 16 * 16 + d % 16
+    value = d // 16 * 1024 + t % 16 // 4 * 256 + d % 16 * 16 + t // 16 * 4 + t % 4
+    body = torch.zeros((n // 4, 1, 2, 64 * dim), dtype=torch.int8)
+    levels = q.repeat_interleave(16, 1)[:, :, None].expand(-1, -1, dim) * torch.where(torch.arange(dim) % 2 == 0, 1, -1)
+    for i, at in enumerate((key, value)):
+        body[:, 0, i, torch.from_numpy(at).reshape(-1)] = levels.reshape(n // 4, -1).to(torch.int8)
+    pages.copy_(body)
+    table = torch.arange(n // 4, dtype=torch.int32, device="cuda")[None]
+    lengths = torch.tensor([16 * n], dtype=torch.int32, device="cuda")
+    want = (levels.float() * s.view(-1, 4).repeat_interleave(16, 1)[:, :, None]).reshape(16 * n, 1, dim)
+    for kind in (torch.float32, torch.float16, torch.bfloat16):
+        for x in B.kv_read(pages, scales, table, lengths, dim, kind, 16 * n):
+            assert torch.equal(x.cpu(), want.to(kind)), kind
