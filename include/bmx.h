@@ -70,7 +70,7 @@ extern "C" {
 #define BMX_OP_QUANT_GEMM 3    /* dims = {M, N, K, bits_a, bits_w} */
 #define BMX_OP_BINARY_CONV2D_BITS 4 /* dims = {N, C, H, W, O, KH, KW, stride, pad, out_pad} */
 #define BMX_OP_XNOR_GEMM_W32 5 /* dims = {M, N, K} */
-#define BMX_OP_KV_ATTENTION 6 /* dims = {sequences, table_width, heads, q_heads, dim, max_new} */
+#define BMX_OP_KV_ATTENTION 6 /* dims = {sequences, table_width, heads, q_heads, dim, max_new[, rows]} */
 
 /* Sign-binarise and bit-pack (Sec. 1: binarisation with the sign function, 64
  * values per word; Sec. 3.1: the per-forward-pass input binarisation step).
@@ -325,9 +325,11 @@ typedef struct bmx_kv_cache {
  *   h / (q_heads / heads) of the cache.  A row at position p sees the tokens t < its sequence's length, with causal those t <= p, with
  *   window > 0 those t > p - window.  A row that sees nothing is zeros.  lse fp32 [rows][q_heads] or NULL: the logarithm of the
  *   softmax's sum (-infinity where nothing is seen).
- *   workspace >= bmx_workspace_bytes(BMX_OP_KV_ATTENTION, {sequences, table_width, heads, q_heads, dim, max_new}, 6), 16-byte aligned, all
- *   zeros before the first call that uses it; every call leaves it ready for the next on its stream, whatever that one's sizes.  NULL
- *   where that is 0. */
+ *   workspace >= bmx_workspace_bytes(BMX_OP_KV_ATTENTION, {sequences, table_width, heads, q_heads, dim, max_new}, 6), which is enough for every
+ *   call of these sizes with at most max_new new rows a sequence (0: however many); with the rows of one call as a seventh number, what that call
+ *   needs.  16-byte aligned, all zeros before the first call that uses it; every call leaves it ready for the next on its stream, whatever
+ *   that one's sizes.  NULL where that is 0.  At most 1048560 rows of queries for a sequence and a head of the cache (max_new * q_heads /
+ *   heads, with rows for a max_new of 0): BMX_ERR_SHAPE. */
 int bmx_kv_write(const bmx_kv_cache* cache, const void* k, const void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row,
                  int64_t v_head, int64_t rows, int max_new, void* stream);
 int bmx_kv_read(const bmx_kv_cache* cache, void* k, void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head,

@@ -318,7 +318,8 @@ def kv_attention(q, pages, scales, table, lengths, starts=None, max_new=0, scale
                  workspace=None, stream=None):
     """Attention of each sequence's last tokens, q [rows, q_heads, dim], over its part of the cache; scale: 1 / sqrt(dim) if None.
     lse: returns (out, log of the softmax's sum, fp32 [rows, q_heads]).  workspace: a tensor of
-    workspace_bytes(OP_KV_ATTENTION, (sequences, pages of one, heads, q_heads, dim, max_new)) bytes or more, zeros before its first use and
-    kept from call to call on one stream; None: made and cleared in the call."""
+    workspace_bytes(OP_KV_ATTENTION, (sequences, pages of one, heads, q_heads, dim, max_new)) bytes or more (max_new there: the most new rows
+    of any call that uses it, 0: any number), zeros before its first use and kept from call to call on one stream; None: made and cleared
+    in the call."""
     return (_native or _host()).kv_attention(q, pages, scales, table, lengths, starts, max_new, scale, causal, window, lse, out,
                                              workspace, stream)

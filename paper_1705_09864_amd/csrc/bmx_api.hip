@@ -82,17 +82,22 @@ int w4_check(int N, int K, int group) {
   return BMX_OK;
 }
 
+constexpr int kMostSequences = 65535, kMostHeads = 32767, kMostRows = 65535 * 16;  // (kMostRows: of a sequence and a head of the cache)
+
+// No sequence has more new rows than this, of `rows` in all.
+int64_t new_rows(int64_t max_new, int64_t rows) { return max_new == 0 || max_new > rows ? rows : max_new; }
+
 // The description of a cache and the number of a call's rows; *max_new becomes what it stands for.
 int kv_check(const bmx_kv_cache* c, int type, int64_t rows, int* max_new) {
   if (!c) return BMX_ERR_NULL;
-  if (c->sequences < 0 || c->sequences > 65535 || c->table_width < 0 || c->num_pages < 0 || c->heads <= 0 || c->heads > 32767 ||
+  if (c->sequences < 0 || c->sequences > kMostSequences || c->table_width < 0 || c->num_pages < 0 || c->heads <= 0 || c->heads > kMostHeads ||
       c->dim <= 0 || c->dim > 256 || rows < 0 || rows >= ((int64_t)1 << 31) || *max_new < 0)
     return BMX_ERR_SHAPE;
   if (!is_type(type) || (c->block != 16 && c->block != 32 && c->block != 64)) return BMX_ERR_UNSUPPORTED;
   if (rows > 0 && c->sequences == 0) return BMX_ERR_SHAPE;
   if (!c->starts && rows > 0 && rows % c->sequences) return BMX_ERR_SHAPE;
   if (!c->starts) *max_new = rows > 0 ? (int)(rows / c->sequences) : 0;
-  else if (*max_new == 0 || *max_new > rows) *max_new = (int)rows;
+  else *max_new = (int)new_rows(*max_new, rows);
   if (c->sequences * ((int64_t)*max_new / 64 + 2) >= ((int64_t)1 << 31)) return BMX_ERR_SHAPE;  // (workgroups of a launch)
   if (rows == 0) return BMX_OK;
   if (!c->pages || !c->scales || !c->lengths || (!c->table && c->table_width > 0)) return BMX_ERR_NULL;
@@ -228,11 +233,14 @@ size_t bmx_workspace_bytes(int op, const int64_t* dims, int ndims) {
           .total;
     }
     case BMX_OP_KV_ATTENTION: {
-      if (ndims != 6) return 0;
-      for (int i = 0; i < 6; ++i)
+      if (ndims != 6 && ndims != 7) return 0;
+      for (int i = 0; i < ndims; ++i)
         if (dims[i] < (i == 2 || i == 3 || i == 4) || dims[i] >= ((int64_t)1 << 31)) return 0;
       if (dims[3] % dims[2] || dims[4] > 256) return 0;
-      return round256(bmx::kv_attention_workspace(dims[0], dims[1], dims[2], dims[3], dims[4], dims[5]));
+      if (ndims == 6) return round256(bmx::kv_attention_workspace(dims[0], dims[1], dims[2], dims[3], dims[4], dims[5]));
+      const int64_t most = new_rows(dims[5], dims[6]);
+      if (dims[0] > kMostSequences || dims[2] > kMostHeads || most * (dims[3] / dims[2]) > kMostRows) return 0;  // (refused)
+      return round256(bmx::kv_attention_workspace_of_call(dims[0], dims[1], dims[2], dims[3], dims[4], most));
     }
     default: return 0;
   }
@@ -779,13 +787,12 @@ static int kv_attention(const bmx_kv_cache* cache, const void* q, int type, int6
   int st = kv_check(cache, type, rows, &max_new);
   if (st != BMX_OK) return st;
   if (q_heads <= 0 || q_heads % cache->heads || q_heads > 65535 || window < 0) return BMX_ERR_SHAPE;
-  if ((int64_t)max_new * (q_heads / cache->heads) > 65535 * 16) return BMX_ERR_SHAPE;
+  if ((int64_t)max_new * (q_heads / cache->heads) > kMostRows) return BMX_ERR_SHAPE;
   if (rows == 0) return BMX_OK;
   if ((st = kv_rows_check(q, type, q_row, q_head, rows, q_heads, cache->dim)) != BMX_OK) return st;
   if ((st = kv_rows_check(out, type, out_row, out_head, rows, q_heads, cache->dim)) != BMX_OK) return st;
   if (misaligned(lse, 4)) return BMX_ERR_ALIGN;
-  const int64_t dims[6] = {cache->sequences, cache->table_width, cache->heads, q_heads, cache->dim, max_new};
-  const size_t need = bmx_workspace_bytes(BMX_OP_KV_ATTENTION, dims, 6);
+  const size_t need = round256(bmx::kv_attention_workspace_of_call(cache->sequences, cache->table_width, cache->heads, q_heads, cache->dim, max_new));
   if (need && (!workspace || workspace_bytes < need)) return BMX_ERR_WORKSPACE;
   if (need && misaligned(workspace, 16)) return BMX_ERR_ALIGN;
   return hip_status(bmx::launch_kv_attention(*cache, q, type, q_row, q_head, q_heads, (int)rows, max_new, scale, causal != 0, window, out,

@@ -261,7 +261,9 @@ hipError_t launch_kv_read(const bmx_kv_cache& c, void* k, void* v, int type, int
 hipError_t launch_kv_attention(const bmx_kv_cache& c, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int rows,
                                int max_new, float scale, bool causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
                                void* workspace, bool fresh, hipStream_t s);  // fresh: the workspace is not known to be zeros
+// What any call of at most max_new new rows a sequence (0: any) needs, and what one of exactly so many does.
 size_t kv_attention_workspace(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new);
+size_t kv_attention_workspace_of_call(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new);
 
 // The same convolution on the GEMM kernel (filters = A rows streamed through SGPRs, im2col
 // rows gathered per chunk): for K that does not fit the stationary kernel or grids with too

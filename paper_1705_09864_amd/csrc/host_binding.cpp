@@ -621,7 +621,7 @@ FUNCTION(kv_attention, 14) {
   const int64_t most = c.starts ? max_new ? std::min<int64_t>(max_new, rows) : rows : rows / std::max(c.sequences, 1);
   Workspace ws;
   const bool fresh = !ws.given(a[12]);
-  if (fresh) ws.allocate(BMX_OP_KV_ATTENTION, {c.sequences, c.table_width, c.heads, heads, c.dim, most}, q, s);
+  if (fresh) ws.allocate(BMX_OP_KV_ATTENTION, {c.sequences, c.table_width, c.heads, heads, c.dim, most, rows}, q, s);
   call("bmx_kv_attention", fresh ? bmx_fresh_kv_attention : bmx_kv_attention, &c, q->data_ptr(), type_of(type), q->stride(0),
        q->stride(1), heads, rows, max_new, (float)scale, (int)truth(a[8]), window, out->data_ptr(), out->stride(0), out->stride(1),
        lse ? ptr<float>(lse->t) : nullptr, ws.p, ws.bytes, s);

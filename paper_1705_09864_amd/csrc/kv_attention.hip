@@ -107,6 +107,8 @@ constexpr int kWaves = 4;
 constexpr int kCounters = 16384;  // of the workspace's head; what needs more than these has rows enough not to be split
 constexpr int kMostSplits = 128;
 constexpr int kLeastPages = 16;   // of a split of many rows
+constexpr int kLeastTiles = 128;  // of 128 rows, for the kernel for many
+constexpr int64_t kMostTiles = 65535;  // of 16 rows: a launch's second dimension
 
 template <int TYPE, int DC>
 __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache c, Args a) {
@@ -668,7 +670,7 @@ Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads
   int64_t rows = max_new * (q_heads / heads);
   p.few = 0x7fffffff;
   p.prompt_tiles = 0;
-  if (type != BMX_F32 && ceil_div(rows, 128) * heads * sequences >= 128 && rows > 64) {
+  if (type != BMX_F32 && ceil_div(rows, 128) * heads * sequences >= kLeastTiles && rows > 64) {
     p.prompt_tiles = ceil_div(rows, 128);
     p.few = 64;
     rows = 64;
@@ -723,6 +725,21 @@ __global__ void clear_kernel(uint32_t* p) { p[blockIdx.x * 256 + threadIdx.x] = 
 }  // namespace
 
 size_t kv_attention_workspace(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new) {
+  // The largest of the calls' bytes, which first grow with the rows and then, where rows fill the chip without splits, fall.  In closed form: of
+  // `each` units a tile, and splits that bring t tiles to 256 workgroups, each * t * splits <= 255 + each * t while that is worth a split.
+  const int64_t each = sequences * heads, rows = max_new > 0 ? std::min(max_new * (q_heads / heads), kMostTiles * 16) : kMostTiles * 16;
+  const size_t line = (kv_row_bytes((int)dim) + 4) * 4;
+  size_t most = 0;
+  if (each == 0) return 0;
+  const int64_t units = each * std::min(ceil_div(rows, 16), 255 / each), splits = std::min<int64_t>(ceil_div(table_width, 4), kMostSplits);
+  if (units > 0 && splits > 1) most = std::min(units * splits, units + 255) * std::min<int64_t>(rows, 16) * line;
+  const int64_t places = dim <= 128 ? 512 : 256, tiles = each * std::min(ceil_div(rows, 128), places / 2 / each);
+  if (rows > 64 && tiles >= kLeastTiles && table_width / kLeastPages > 1)
+    most = std::max<size_t>(most, std::min(places, tiles * (table_width / kLeastPages)) * 128 * line);
+  return most ? kCounters * 4 + most : 0;
+}
+
+size_t kv_attention_workspace_of_call(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new) {
   // (whatever the type)
   return std::max(plan(sequences, table_width, heads, q_heads, dim, max_new, BMX_F32).bytes,
                   plan(sequences, table_width, heads, q_heads, dim, max_new, BMX_F16).bytes);
