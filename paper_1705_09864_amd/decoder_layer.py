@@ -21,11 +21,16 @@ class Pages:
         self.lengths = torch.zeros((sequences,), dtype=torch.int32, device=device)
 
     def extend(self, new):
-        """Room for new[i] more tokens of sequence i; returns the rows' starts, None where each has as many."""
-        for i, n in enumerate(new):
-            need = -(-(self.tokens[i] + n) // B.PAGE)
-            if need > self.table.shape[1] or need - self.count[i] > len(self.free):
-                raise ValueError("sequence %d: no room for %d more tokens" % (i, n))
+        """Room for new[i] more tokens of sequence i; returns the rows' starts, None where each has as many.  Where there is no room for all of
+        them, nothing changes."""
+        if len(new) != len(self.tokens) or min(new, default=0) < 0:
+            raise ValueError("expected how many tokens are new for each of %d sequences, got %r" % (len(self.tokens), new))
+        needs, left = [-(-(t + n) // B.PAGE) for t, n in zip(self.tokens, new)], len(self.free)
+        for i, need in enumerate(needs):
+            left -= max(0, need - self.count[i])
+            if need > self.table.shape[1] or left < 0:
+                raise ValueError("sequence %d: no room for %d more tokens" % (i, new[i]))
+        for i, (n, need) in enumerate(zip(new, needs)):
             if need > self.count[i]:
                 pages = [self.free.pop() for _ in range(need - self.count[i])]
                 self.table[i, self.count[i]:need] = torch.tensor(pages, dtype=torch.int32)
