@@ -53,7 +53,7 @@ class FewBitAttention:
 
     def __init__(self, w_qkv, w_out, heads, kv_heads, dim, num_pages, group=128, block=16):
         self.heads, self.kv_heads, self.dim = heads, kv_heads, dim
-        self.n_qkv, self.n_out = w_qkv.shape[0], w_out.shape[0]
+        self.n_qkv, self.n_out, self.hidden = w_qkv.shape[0], w_out.shape[0], w_qkv.shape[1]
         if self.n_qkv != (heads + 2 * kv_heads) * dim or w_out.shape[1] != heads * dim:
             raise ValueError("w_qkv and w_out do not fit the heads")
         self.qkv, self.out = B.w4_quantize(w_qkv, group), B.w4_quantize(w_out, group)
@@ -68,10 +68,12 @@ class FewBitAttention:
         return self.scratch
 
     def step(self, x, where, new):
-        """x [sum(new), hidden], new[i] more tokens of sequence i; `where`: the sequences' Pages."""
-        starts = where.extend(new)
+        """x [sum(new), hidden], new[i] more tokens of sequence i; `where`: the sequences' Pages, unchanged where the step is refused."""
+        if x.dim() != 2 or tuple(x.shape) != (sum(new), self.hidden):
+            raise ValueError("x: expected the shape [%d, %d], got %r" % (sum(new), self.hidden, list(x.shape)))
         q, k, v = (B.w4_fc(x, *self.qkv, self.n_qkv).view(x.shape[0], -1, self.dim)
                    .split([self.heads, self.kv_heads, self.kv_heads], 1))
+        starts = where.extend(new)
         cache = (self.pages, self.scales, where.table, where.lengths)
         B.kv_write(k, v, *cache, starts=starts, max_new=max(new))
         o = B.kv_attention(q, *cache, starts=starts, max_new=max(new),
