@@ -7,7 +7,9 @@
 // holds values, so the weights never leave their lane.
 // For 16-bit results the products are f16's:
 //   q goes in with its row's largest value brought to [128, 256) by a power of two (exact but for values 2^-21 below the row's largest);
-//   p goes in as p * (c_b / C) * 2^14 with C the largest c_b so far: at most 2^14, and with all of f16's 11 bits down to 2^-28 of that.
+//   p goes in as p * c_b / W * 2^14 with W the row's own largest |p c_b| so far: at most 2^14, and with all of f16's 11 bits down to 2^-28 of that.
+//   So neither tokens that the row does not see nor values without weight say how well the others are held.  W is kept as its logarithm, `lead`,
+//   relative to the running maximum.
 // For f32 results they are bf16's, q and p * c_b in three parts of 8 bits each, which together are all of them whatever the range; levels
 // are exact in bf16 too.
 //
@@ -87,6 +89,24 @@ __device__ inline u32x2 get(const float* p) {
 __device__ inline f32x4 get4(const float* p) {
   const u32x2 a = get(p), b = get(p + 2);
   return __builtin_bit_cast(f32x4, u32x4{a[0], a[1], b[0], b[1]});
+}
+
+// A value's scale times what a row's weights are multiplied with.  Bounded, as a weight of 0 has to bring 0: also in a block that nobody has
+// written, where the scale is anything, and where the row's other weights are far below it.
+__device__ inline float bounded(float x) { return __builtin_amdgcn_fmed3f(x, -0x1.fffffep127f, 0x1.fffffep127f); }
+__device__ inline float or_zero(float x) { return x == -INFINITY ? 0.0f : x; }
+constexpr float kLeastLead = -100.0f;  // (so that its power stays a number: a row whose weights times scales are all below 2^-100 is held to that)
+
+// The larger of x and that of the lane 16, and 32, away.
+__device__ inline float max_16(float x) {
+  const auto two = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a = two[0], b = two[1];
+  return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+__device__ inline float max_32(float x) {
+  const auto two = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a = two[0], b = two[1];
+  return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
 struct Args {
@@ -206,15 +226,17 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
       }
   }
 
-  float m = -INFINITY, l = 0.0f, most = 0.0f;
+  float m = -INFINITY, l = 0.0f, lead = kLeastLead;
   f32x4 o[DT] = {};
   while (page >= 0) {
     const int t0 = (begin + wave + at * kWaves) * kPage;
-    float p[4][4], key_scale[4], value_scale[4], top = -INFINITY, most_new = most;
+    float p[4][4], key_scale[4], value_scale[4], value_log[4], tops[4];
+    const float log_of = F16 ? __builtin_amdgcn_logf(fabsf(scale_of)) : 0.0f;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       key_scale[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale_of), u));
       value_scale[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale_of), 4 + u));
+      if constexpr (F16) value_log[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, log_of), 4 + u));
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -234,41 +256,41 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
       for (int i = 0; i < 4; ++i) p[u][i] = z[i];
     }
     load_keys();
-    if (kv_all_in(t0, kPage, low_all, high_all)) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float f = factor * key_scale[u];
-        most_new = fmaxf(most_new, value_scale[u]);
+    for (int u = 0; u < 4; ++u) {
+      const float f = factor * key_scale[u];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, p[u][i] *= f);
-      }
-    } else {
+      for (int i = 0; i < 4; ++i) p[u][i] *= f;
+    }
+    if (!kv_all_in(t0, kPage, low_all, high_all)) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int t = t0 + 16 * u;
-        const float f = factor * key_scale[u];
-        if (t >= high_any || t + 15 < low_any) value_scale[u] = 0.0f;  // (a block that nobody has written has any scale)
-        most_new = fmaxf(most_new, value_scale[u]);
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          p[u][i] = t + 4 * g + i < high && t + 4 * g + i >= low ? p[u][i] * f : -INFINITY;
-          top = fmaxf(top, p[u][i]);
+          const int t = t0 + 16 * u + 4 * g + i;
+          p[u][i] = t < high && t >= low ? p[u][i] : -INFINITY;
         }
-      }
     }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float m_new = fmaxf(m, top), m_at = m_new == -INFINITY ? 0.0f : m_new;
-    const float shrink = __builtin_amdgcn_exp2f(m - m_at);
-    float sum = 0.0f;
-    // (scales below 2^-126 are those of levels that are all 0)
-    const float inverse = most_new >= 0x1p-126f ? 1.0f / most_new : 0.0f, shrink_o = F16 ? shrink * (most * inverse) : shrink;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) tops[u] = fmaxf(fmaxf(p[u][0], p[u][1]), fmaxf(p[u][2], p[u][3]));
+    float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    top = max_32(max_16(top));
+    const float m_new = fmaxf(m, top), m_at = or_zero(m_new), shrink = __builtin_amdgcn_exp2f(m - m_at);
+    float sum = 0.0f, shrink_o = shrink, unit = 1.0f;
+    if constexpr (F16) {
+      const float before = lead + (m - m_at);
+      lead = fmaxf(before, kLeastLead);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) lead = fmaxf(lead, tops[u] - m_at + value_log[u]);
+      lead = max_32(max_16(lead));
+      shrink_o = __builtin_amdgcn_exp2f(before - lead);
+      unit = __builtin_amdgcn_exp2f(-lead);
+    }
     m = m_new;
-    most = most_new;
     u32x4 w[PARTS][2];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const float f = F16 ? value_scale[u] * inverse * 0x1p14f : value_scale[u];
+      const float f = bounded(F16 ? value_scale[u] * unit * 0x1p14f : value_scale[u]);
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
         const float e0 = __builtin_amdgcn_exp2f(p[u][i] - m_at), e1 = __builtin_amdgcn_exp2f(p[u][i + 1] - m_at);
@@ -294,9 +316,10 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   if (g == 0) red_m[wave][lane] = m, red_l[wave][lane] = l;
+  const float unit_of = __builtin_amdgcn_exp2f(lead) * 0x1p-14f;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
-    *reinterpret_cast<f32x4*>(&red[(wave * 16 + lane % 16) * LINE + dt * 16 + 4 * g]) = F16 ? o[dt] * (most * 0x1p-14f) : o[dt];
+    *reinterpret_cast<f32x4*>(&red[(wave * 16 + lane % 16) * LINE + dt * 16 + 4 * g]) = F16 ? o[dt] * unit_of : o[dt];
   __syncthreads();
   const int rows = min(s.count * a.share - r0, 16), quads = rows * (ROW / 4);
   const int64_t unit = ((int64_t)seq * gridDim.y + blockIdx.y) * c.heads + head;
@@ -395,8 +418,8 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
 // 29% of the time, vector ALU 50%).  2 prompts of 2048 new tokens over 4096, 32 heads on 8 of 128: 289 us, 710 TFLOP/s; 16 rows a wave, each
 // with pages of its own, 508.  The next page's scores computed beside this page's exponentials, which takes more registers than two
 // waves have: 385.
-// So where all of a page is seen and no scale of its values is far below the largest, the scale goes into the exponent,
-//   p c / C 2^14 = 2^(s + log2(c / C 2^14) - m),
+// So where all of a page is seen and no scale of its values is far below the row's W, the scale goes into the exponent,
+//   p c / W 2^14 = 2^(s + log2(c / W 2^14) - m),
 // and comes out of the sum of p again once for each 16 tokens.
 // SPLIT: tiles of rows fewer than the chip holds workgroups at once, whose pages are split and joined as above (a kernel of its own: the
 // splits' arithmetic in the one kernel cost it 1%).  512 new tokens over 4096: 68 us, 120 unsplit; the join is some 15 us of that.
@@ -509,7 +532,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
   float scale_of = scale_in;
   __syncthreads();
 
-  float m = -INFINITY, l = 0.0f, most = 0.0f;
+  float m = -INFINITY, l = 0.0f, lead = kLeastLead;
   f32x16 o[DC] = {};
   for (int buf = 0; pg < last; buf ^= 1) {
     const int next = fetch(pg + 1), t0 = pg * kPage;
@@ -519,50 +542,53 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
       for (int i = 0; i < NS; ++i)
 #pragma unroll
         for (int t = 0; t < 2; ++t) z[t] = mfma32(lds[buf][0][(t * NS + i) * 64 + lane], q[i], z[t]);
-      float key_scale[4], value_scale[4], most_new = most, top = -INFINITY;
+      float key_scale[4], value_log[4], tops[4];
+      const float log_of = __builtin_amdgcn_logf(fabsf(scale_of));
+      const auto of_lane = [](float x, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); };
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        key_scale[u] = factor * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale_of), u));
-        value_scale[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale_of), 4 + u));
-        if (t0 + 16 * u >= high_any || t0 + 16 * u + 15 < low_any) value_scale[u] = 0.0f;  // (a block that nobody has written has any scale)
-        most_new = fmaxf(most_new, value_scale[u]);
-      }
-      // (scales below 2^-126 are those of levels that are all 0)
-      const float inverse = most_new >= 0x1p-126f ? 1.0f / most_new : 0.0f;
-      float f[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) f[u] = value_scale[u] * inverse * 0x1p14f;
-      const bool full = __builtin_amdgcn_readfirstlane(kv_all_in(t0, kPage, low_all, high_all) && fminf(fminf(f[0], f[1]), fminf(f[2], f[3])) >= 0x1p-8f);
-      u32x4 w[4];
+      for (int u = 0; u < 4; ++u) key_scale[u] = factor * of_lane(scale_of, u), value_log[u] = of_lane(log_of, 4 + u);
+      // (every lane has one of the eight scales)
+      const bool full = __builtin_amdgcn_readfirstlane(kv_all_in(t0, kPage, low_all, high_all) && __all(scale_of >= 0x1p-100f));
       if (full) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           float t = z[u / 2][u % 2 * 8];
 #pragma unroll
           for (int i = 1; i < 8; ++i) t = fmaxf(t, z[u / 2][u % 2 * 8 + i]);
-          top = fmaxf(top, t * key_scale[u]);
+          tops[u] = t * key_scale[u];
         }
       } else {
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < 4; ++u) {
+          tops[u] = -INFINITY;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int t = t0 + 16 * u + i / 4 * 8 + 4 * h + i % 4;
             const float x = t < high && t >= low ? z[u / 2][u % 2 * 8 + i] * key_scale[u] : -INFINITY;
             z[u / 2][u % 2 * 8 + i] = x;
-            top = fmaxf(top, x);
+            tops[u] = fmaxf(tops[u], x);
           }
+        }
       }
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float m_new = fmaxf(m, top), m_at = m_new == -INFINITY ? 0.0f : m_new;
-      const float shrink = __builtin_amdgcn_exp2f(m - m_at), shrink_o = shrink * (most * inverse);
+      float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+      top = max_32(top);
+      const float m_new = fmaxf(m, top), m_at = or_zero(m_new), shrink = __builtin_amdgcn_exp2f(m - m_at);
+      const float before = lead + (m - m_at);
+      lead = fmaxf(before, kLeastLead);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) lead = fmaxf(lead, tops[u] - m_at + value_log[u]);
+      lead = max_32(lead);
+      const float shrink_o = __builtin_amdgcn_exp2f(before - lead);
       m = m_new;
-      most = most_new;
       l *= shrink;
-      if (full) {
+      u32x4 w[4];
+      const float least = fminf(fminf(value_log[0], value_log[1]), fminf(value_log[2], value_log[3]));
+      if (full && __all(least - lead >= -64.0f)) {
+        const float out_of = __builtin_amdgcn_rcpf(scale_of);
+        float all = 0.0f;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const float at = __builtin_amdgcn_logf(f[u]) - m_at;
+          const float at = value_log[u] - lead + 14.0f - m_at;
           float sum = 0.0f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -573,19 +599,23 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
             pair<1>(y0, y1, part);
             w[u][i] = part[0];
           }
-          l += sum * __builtin_amdgcn_rcpf(f[u]);
+          all += sum * of_lane(out_of, 4 + u);
         }
+        l += all * __builtin_amdgcn_exp2f(lead - 14.0f);
       } else {
+        const float unit = __builtin_amdgcn_exp2f(-lead);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < 4; ++u) {
+          const float f = bounded(of_lane(scale_of, 4 + u) * unit * 0x1p14f), k = full ? key_scale[u] : 1.0f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float e0 = __builtin_amdgcn_exp2f(z[u / 2][u % 2 * 8 + 2 * i] - m_at), e1 = __builtin_amdgcn_exp2f(z[u / 2][u % 2 * 8 + 2 * i + 1] - m_at);
+            const float e0 = __builtin_amdgcn_exp2f(z[u / 2][u % 2 * 8 + 2 * i] * k - m_at), e1 = __builtin_amdgcn_exp2f(z[u / 2][u % 2 * 8 + 2 * i + 1] * k - m_at);
             l += e0 + e1;
             uint32_t part[1];
-            pair<1>(e0 * f[u], e1 * f[u], part);
+            pair<1>(e0 * f, e1 * f, part);
             w[u][i] = part[0];
           }
+        }
       }
       if (__any(shrink_o != 1.0f)) {  // (most pages hold no new maximum)
 #pragma unroll
@@ -602,13 +632,13 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
     __syncthreads();
   }
   l += __shfl_xor(l, 32);
+  float unit_of = __builtin_amdgcn_exp2f(lead) * 0x1p-14f;
   if (SPLIT && used > 1) {  // the parts: each lane's numbers at the same place in all of them
     const int64_t unit = ((int64_t)seq * ((a.max_new * a.share + 127) / 128) + r0 / 128) * c.heads + head;
     constexpr int PART = 64 * (DC * 16 + 2);
     float* at = a.parts + (unit * a.prompt_splits * 4 + wave) * PART + lane * 2;
     if (r_wave < rows) {
       float* to = at + (int64_t)split * 4 * PART;
-      const float unit_of = most * 0x1p-14f;
 #pragma unroll
       for (int n = 0; n < DC; ++n)
 #pragma unroll
@@ -623,7 +653,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
     if (place != (uint32_t)used - 1) return;
     if (threadIdx.x == 0) __hip_atomic_store(a.arrived + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (r_wave >= rows) return;
-    m = -INFINITY, l = 0.0f, most = 0x1p14f;
+    m = -INFINITY, l = 0.0f, unit_of = 1.0f;
     for (int p = 0; p < used; ++p) {
       const float* from = at + (int64_t)p * 4 * PART;
       const u32x2 x = get(from + DC * 1024);
@@ -647,7 +677,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
   if (r >= rows) return;
   const int64_t at = (s.row0 + token) * a.out_row + (head * a.share + r % a.share) * a.out_head;
   // (a row that sees nothing is zeros)
-  const float share_of = l == 0.0f ? 0.0f : most * 0x1p-14f / l;
+  const float share_of = l == 0.0f ? 0.0f : unit_of / l;
 #pragma unroll
   for (int n = 0; n < DC; ++n)
 #pragma unroll

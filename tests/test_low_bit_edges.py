@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_1705_09864_amd import binding as B
+from test_low_bit import TYPES, Cache, host
 
 pytestmark = pytest.mark.gpu
 TOP = 2**31 - 1
@@ -80,3 +81,77 @@ def test_kv_read_rounds_the_product():
     for kind in (torch.float32, torch.float16, torch.bfloat16):
         for x in B.kv_read(pages, scales, table, lengths, dim, kind, 16 * n):
             assert torch.equal(x.cpu(), want.to(kind)), kind
+
+
+# ------------------------------------------------------------------ what a row does not see or weigh leaves it as it is
+def check_rows(out, q, c, rows, kind, scale=None, first=0, last=None):
+    """Rows `first` to `last` of each sequence's `rows` new ones, causal.  As in test_low_bit.py, but what a weight in f16 loses is bounded by the
+    row itself: a weight times its block's scale is held to 2^-25 of 2^14, which stands for the row's largest, for each token."""
+    u, w = TYPES[kind][1], 2.0**-20 if kind == "f32" else 2.0**-11
+    scale = c.dim**-0.5 if scale is None else scale
+    share, last = q.shape[1] // c.heads, rows if last is None else last
+    x, got = host(q), host(out)
+    for seq, n in enumerate(c.lengths):
+        mine = slice(seq * rows + first, seq * rows + last)
+        pos, t = np.arange(n - rows + first, n - rows + last)[:, None], np.arange(n)[None, :]
+        kv = c.values(seq).astype(np.float64)
+        for h in range(q.shape[1]):
+            k, v = kv[0, h // share], kv[1, h // share]
+            z = np.where(t <= pos, x[mine, h] @ k.T * scale, -np.inf)
+            e = np.where(t <= pos, (2.0**-21 + c.dim * 2.0**-24) * abs(scale) * (np.abs(x[mine, h]) @ np.abs(k).T), 0).max(1, keepdims=True)
+            p = np.exp(z - z.max(1, keepdims=True))
+            p = p / p.sum(1, keepdims=True)
+            want, size = p @ v, p @ np.abs(v)
+            bound = u * np.abs(want) + (2 * e + w + (n + 100) * 2.0**-24) * size + 1e-30
+            if kind != "f32":
+                steps = np.repeat(np.abs(c.s[seq, 1, h // share].astype(np.float64)), c.block)[:n]
+                bound = bound + n * 2.0**-39 * 127 * (p * steps).max(1, keepdims=True) + (2.0**-25 if kind == "f16" else 0)
+            err = np.abs(got[mine, h] - want)
+            assert (err <= bound).all(), (seq, h, (err / bound).max())
+
+
+# the kernel of 16 rows and, for 16-bit types, the one of many
+@pytest.mark.parametrize("seqs", [1, 64])
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_kv_attention_values_behind_a_row(kind, block, seqs):
+    """Tokens behind a row's position, of its page and beside rows of its tile that see them, hold values 2^60 times as large."""
+    rows, c = 40, Cache(seqs, 3, 2, 64, block, 50)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    c.write([88] * seqs, "f32", g)
+    large = (112 if block == 16 else 96) - 88  # from a block's first token on
+
+    def change(kv):
+        kv.unflatten(1, (seqs, rows))[1, :, large:] *= 2.0**60
+    c.write([rows] * seqs, "f32", g, change)
+    q = torch.randn((seqs * rows, 6, 64), device="cuda", generator=g).to(TYPES[kind][0])
+    out = B.kv_attention(q, c.pages, c.scales, c.table, c.lens())
+    assert ("kv_prompt" in B.last_kernel()) == (seqs > 1 and kind != "f32")
+    check_rows(out, q, c, rows, kind, last=large)
+    if kind != "f16":  # (there these are infinities)
+        check_rows(out, q, c, rows, kind, first=large)
+
+
+@pytest.mark.parametrize("seqs", [1, 64])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_kv_attention_values_without_weight(kind, seqs):
+    """A block of large values whose weights are nothing, and one whose weights are 2^-40 and bring as much as all others."""
+    rows, c = 40, Cache(seqs, 3, 2, 64, 16, 51)
+    g = torch.Generator(device="cuda").manual_seed(4)
+
+    def change(kv):
+        x = kv.unflatten(1, (seqs, 130))
+        x[0, :, :, :, 0] = 0
+        x[0, :, 16:32] = 0
+        x[0, :, 16:32, :, 0] = -100
+        x[1, :, 16:32] *= 2.0**60
+        x[0, :, 48:64] = 0
+        x[0, :, 48:64, :, 0] = -2.2
+        x[1, :, 48:64] *= 2.0**36
+    c.write([130] * seqs, "f32", g, change)
+    q = torch.randn((seqs * rows, 6, 64), device="cuda", generator=g)
+    q[:, :, 0] = 100
+    q = q.to(TYPES[kind][0])
+    out = B.kv_attention(q, c.pages, c.scales, c.table, c.lens())
+    assert ("kv_prompt" in B.last_kernel()) == (seqs > 1 and kind != "f32")
+    check_rows(out, q, c, rows, kind)
