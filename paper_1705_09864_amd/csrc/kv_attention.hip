@@ -94,6 +94,13 @@ __device__ inline f32x4 get4(const float* p) {
 // A value's scale times what a row's weights are multiplied with.  Bounded, as a weight of 0 has to bring 0: also in a block that nobody has
 // written, where the scale is anything, and where the row's other weights are far below it.
 __device__ inline float bounded(float x) { return __builtin_amdgcn_fmed3f(x, -0x1.fffffep127f, 0x1.fffffep127f); }
+// A score: the product, rounded.  (The barrier keeps it from becoming one operation with the difference from the maximum, which is a rounded product: of
+// scores beyond 2^24 that difference need not be below 0 then, and 2 to its power not below 1.)
+__device__ inline float score(float x, float f) {
+  float z = x * f;
+  asm("" : "+v"(z));
+  return z;
+}
 __device__ inline float or_zero(float x) { return x == -INFINITY ? 0.0f : x; }
 constexpr float kLeastLead = -100.0f;  // (so that its power stays a number: a row whose weights times scales are all below 2^-100 is held to that)
 
@@ -260,7 +267,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
     for (int u = 0; u < 4; ++u) {
       const float f = factor * key_scale[u];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[u][i] *= f;
+      for (int i = 0; i < 4; ++i) p[u][i] = score(p[u][i], f);
     }
     if (!kv_all_in(t0, kPage, low_all, high_all)) {
 #pragma unroll
@@ -583,7 +590,8 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
       l *= shrink;
       u32x4 w[4];
       const float least = fminf(fminf(value_log[0], value_log[1]), fminf(value_log[2], value_log[3]));
-      if (full && __all(least - lead >= -64.0f)) {
+      // (scores beyond 2^20 lose too much in the sum of the exponents)
+      if (full && __all(least - lead >= -64.0f && fabsf(m_at) < 0x1p20f)) {
         const float out_of = __builtin_amdgcn_rcpf(scale_of);
         float all = 0.0f;
 #pragma unroll
@@ -609,7 +617,8 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
           const float f = bounded(of_lane(scale_of, 4 + u) * unit * 0x1p14f), k = full ? key_scale[u] : 1.0f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float e0 = __builtin_amdgcn_exp2f(z[u / 2][u % 2 * 8 + 2 * i] * k - m_at), e1 = __builtin_amdgcn_exp2f(z[u / 2][u % 2 * 8 + 2 * i + 1] * k - m_at);
+            const float e0 = __builtin_amdgcn_exp2f(score(z[u / 2][u % 2 * 8 + 2 * i], k) - m_at);
+            const float e1 = __builtin_amdgcn_exp2f(score(z[u / 2][u % 2 * 8 + 2 * i + 1], k) - m_at);
             l += e0 + e1;
             uint32_t part[1];
             pair<1>(e0 * f, e1 * f, part);

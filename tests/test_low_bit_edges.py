@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_1705_09864_amd import binding as B
-from test_low_bit import TYPES, Cache, host
+from test_low_bit import TYPES, Cache, fill, host
 
 pytestmark = pytest.mark.gpu
 TOP = 2**31 - 1
@@ -155,3 +155,32 @@ def test_kv_attention_values_without_weight(kind, seqs):
     out = B.kv_attention(q, c.pages, c.scales, c.table, c.lens())
     assert ("kv_prompt" in B.last_kernel()) == (seqs > 1 and kind != "f32")
     check_rows(out, q, c, rows, kind)
+
+
+# ------------------------------------------------------------------ scores beyond what 32 bits tell apart
+@pytest.mark.parametrize("seqs", [1, 64])
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("log_scale", [14, 18, 22, 26, 40, 80])
+def test_kv_attention_large_scores(kind, seqs, log_scale):
+    """Scores of 2^17 to 2^83: results stay inside what values there are, and where the largest score stands out it is its token's value."""
+    rows, c, scale = 40, Cache(seqs, 5, 2, 64, 16, 52), 2.0**log_scale
+    g = fill(c, [260] * seqs, "f32", 9)
+    q = torch.randn((seqs * rows, 6, 64), device="cuda", generator=g).to(TYPES[kind][0])
+    out, lse = B.kv_attention(q, c.pages, c.scales, c.table, c.lens(), scale=scale, lse=True)
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    x, got = host(q), host(out)
+    for seq in range(seqs):
+        kv = c.values(seq).astype(np.float64)
+        pos, t = np.arange(260 - rows, 260)[:, None], np.arange(260)[None, :]
+        for h in range(6):
+            k, v = kv[0, h // 3], kv[1, h // 3]
+            mine = slice(seq * rows, seq * rows + rows)
+            z = np.where(t <= pos, x[mine, h] @ k.T * scale, -np.inf)
+            e = (2.0**-21 + 64 * 2.0**-24) * scale * (np.abs(x[mine, h]) @ np.abs(k).T).max(1)
+            order = np.argsort(z, 1)
+            gap = np.take_along_axis(z, order[:, -1:], 1)[:, 0] - np.take_along_axis(z, order[:, -2:-1], 1)[:, 0]
+            assert (np.abs(got[mine, h]) <= np.abs(v).max() * (1 + 2.0**-7)).all()
+            clear = gap > 4 * e + 100
+            assert clear.sum() > rows // 4
+            want = v[order[:, -1]]
+            assert (np.abs(got[mine, h] - want) <= (TYPES[kind][1] + 2.0**-11) * np.abs(want) + 2.0**-25 + 260 * 2.0**-39 * np.abs(v).max())[clear].all()
