@@ -295,7 +295,8 @@ int bmx_w4_fc(const void* x, int type, int64_t ldx, const uint8_t* tiles, const 
  *                      t/16*16*row + d/64*1024 + d%32/8*128 + t%16*8 + d%8;
  *           values at  d/16*1024 + t%16/4*256 + d%16*16 + t/16*4 + t%4.
  *           (In the order of the matrix cores' lanes.)  What lies between dim and row does not matter.
- *   scales  fp32 [num_pages][heads][2][64/block].
+ *   scales  fp32 [num_pages][heads][2][64/block].  bmx_kv_write leaves none below 0 and takes those of blocks in use to be so; bmx_kv_read and
+ *           bmx_kv_attention take either sign.
  *   table   int32 [sequences][table_ld], table_width pages of each sequence in order, each a page number.  What tokens do not reach is not read.
  *           A page that new tokens go to belongs to one sequence.
  *   lengths int32 [sequences]: tokens of each sequence, those of the call in hand included.

@@ -184,3 +184,29 @@ def test_kv_attention_large_scores(kind, seqs, log_scale):
             assert clear.sum() > rows // 4
             want = v[order[:, -1]]
             assert (np.abs(got[mine, h] - want) <= (TYPES[kind][1] + 2.0**-11) * np.abs(want) + 2.0**-25 + 260 * 2.0**-39 * np.abs(v).max())[clear].all()
+
+
+# ------------------------------------------------------------------ scales of either sign
+@pytest.mark.parametrize("seqs", [1, 64])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_kv_attention_negative_scales(kind, seqs):
+    """A value is its level times its block's scale, whatever the scale's sign."""
+    rows, c = 40, Cache(seqs, 4, 2, 64, 16, 53)
+    g = fill(c, [230] * seqs, "f32", 10)
+    rng = np.random.default_rng(1)
+    c.s *= rng.choice([-1.0, 1.0], c.s.shape).astype(np.float32)
+    c.s[:, :, :, :6] = -np.abs(c.s[:, :, :, :6])
+    table = c.table.cpu().numpy()
+    scales = c.scales.cpu().numpy()
+    for seq in range(seqs):
+        for b in range(-(-230 // 16)):
+            scales[table[seq, b // 4], :, :, b % 4] = c.s[seq, :, :, b].T
+    c.scales.copy_(torch.from_numpy(scales))
+    q = torch.randn((seqs * rows, 6, 64), device="cuda", generator=g).to(TYPES[kind][0])
+    for scale in (0.125, -0.3):
+        out = B.kv_attention(q, c.pages, c.scales, c.table, c.lens(), scale=scale)
+        assert ("kv_prompt" in B.last_kernel()) == (seqs > 1 and kind != "f32")
+        check_rows(out, q, c, rows, kind, scale=scale)
+    k, v = B.kv_read(c.pages, c.scales, c.table, c.lens(), 64, torch.float32, 230 * seqs)
+    want = np.concatenate([c.values(i).transpose(0, 2, 1, 3) for i in range(seqs)], 1)
+    np.testing.assert_array_equal(torch.stack([k, v]).cpu().numpy(), want)
