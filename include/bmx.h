@@ -282,7 +282,7 @@ int bmx_quant_gemm(const float* a, int64_t lda, int bits_a, const float* w, int6
  *   q = round((w - b) / s) to the nearest, ties to even, clamped to 0..15 (all 0 where s < 2^-126); NaN is level 0.
  * bmx_w4_dequantize: w = s * q + b in fp32, [N, ldw].
  * bmx_w4_fc: out[m][n] = sum_k x[m][k] * w[n][k] + bias[n], x [M, ldx] and out [M, ldo] of `type`, bias fp32 [N] or NULL.  Exact weights
- *   and x against fp32 sums: neither is rounded on the way.  M, N < 2^22. */
+ *   and x against fp32 sums: neither is rounded on the way; infinities and NaN in x give what the sum has for them.  M, N < 2^22. */
 int bmx_w4_quantize(const float* w, int64_t ldw, int N, int K, int group, uint8_t* tiles, uint16_t* scales, void* stream);
 int bmx_w4_dequantize(const uint8_t* tiles, const uint16_t* scales, int N, int K, int group, float* w, int64_t ldw, void* stream);
 int bmx_w4_fc(const void* x, int type, int64_t ldx, const uint8_t* tiles, const uint16_t* scales, int group, const float* bias,

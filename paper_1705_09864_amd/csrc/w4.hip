@@ -94,6 +94,29 @@ struct Eight {
   }
 };
 
+// One result by its definition, value by value.  The kernels' sums are inf - inf where x holds an infinity, and infinite where 31 x is beyond fp32
+// and x w is not; what they find not to be finite comes from here.  (A NaN in x ends it.  Rare, and slow: an infinity in every row of 64 x 4096 x 4096
+// bf16 1.3 ms, of 256 rows 5.0; without any the test of the results does not show.)
+template <int TYPE, int GROUP>
+__device__ inline float by_value(const void* x, int64_t ldx, const u32x4* tiles, const uint32_t* scales, int K, int m, int n) {
+  const int64_t tile0 = (int64_t)(n / 16) * ((K + 127) / 128);
+  float v = 0.0f;
+#pragma unroll 1
+  for (int k = 0; k < K && v == v; k += 8) {
+    const int64_t tile = tile0 + k / 128;
+    uint32_t w = reinterpret_cast<const uint32_t*>(tiles)[(tile * 64 + n % 16 + k % 32 / 8 * 16) * 4 + k % 128 / 32];
+    const uint32_t sb = scales[(tile * (128 / GROUP) + k % 128 / GROUP) * 16 + n % 16];
+    const float s = bf16_float(sb & 0xffff), b = __builtin_bit_cast(float, sb & 0xffff0000u);
+#pragma unroll 1
+    for (int j = 0; j < 8 && k + j < K; ++j) {
+      const float q = (float)(w >> (j % 2 ? 16 + 2 * (j - 1) : 2 * j) & 15);
+      v = __builtin_fmaf(load_one<TYPE>(x, m * ldx + k + j), s * q + b, v);
+    }
+  }
+  return v;
+}
+__device__ inline bool finite(float v) { return fabsf(v) < INFINITY; }
+
 constexpr int kMostWaves = 8;
 
 // 16 outputs x 16 MT rows per workgroup, K dealt out to its waves in steps of 128 (1 KB of weights, 16 bytes a lane).  Each wave has DEPTH
@@ -190,6 +213,7 @@ __global__ __launch_bounds__(kMostWaves * 64) void w4_rows_kernel(const void* x,
 #pragma unroll
     for (int w = 0; w < kMostWaves; ++w) v += w < waves ? red[w][m / 16][m % 16 + 16 * (n / 4)][n % 4] : 0.0f;
     if (m0 + m < M && nt * 16 + n < N) {
+      if (!finite(v)) v = by_value<TYPE, GROUP>(x, ldx, tiles, scales, K, m0 + m, nt * 16 + n);
       if (bias) v += bias[nt * 16 + n];
       store_one<TYPE>(out, (int64_t)(m0 + m) * ldo + nt * 16 + n, v);
     }
@@ -295,6 +319,7 @@ __global__ __launch_bounds__(1024 / MT) void w4_few_kernel(const uint16_t* x, in
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) v += red[(w * MT + m / 16) * 64 + m % 16 + 16 * (n / 4)][n % 4];
     if (m0 + m < M && nt * 16 + n < N) {
+      if (!finite(v)) v = by_value<TYPE, GROUP>(x, ldx, tiles, scales, K, m0 + m, nt * 16 + n);
       if (bias) v += bias[nt * 16 + n];
       store_one<TYPE>(out, (int64_t)(m0 + m) * ldo + nt * 16 + n, v);
     }
@@ -461,6 +486,7 @@ __global__ __launch_bounds__(256) void w4_f32_kernel(const void* x, int64_t ldx,
     if (t + 1 < steps) store(1 - buf);
     __syncthreads();
   }
+  bool good = true;
 #pragma unroll
   for (int c = 0; c < CB; ++c) {
     if (col[c] >= N) continue;
@@ -471,7 +497,15 @@ __global__ __launch_bounds__(256) void w4_f32_kernel(const void* x, int64_t ldx,
       for (int i = 0; i < 16; ++i) {
         const int m = m0 + (wm * RB + r) * 32 + 8 * (i / 4) + 4 * h + i % 4;
         if (m < M) store_one<BMX_F32>(out, (int64_t)m * ldo + col[c], acc[r][c][i] + add);
+        good &= finite(acc[r][c][i]);
       }
+  }
+  if (good) return;
+#pragma unroll 1
+  for (int e = 0; e < CB * RB * 16; ++e) {  // (from this lane's own stores, so that no register waits for it)
+    const int n = n0 + (wn * CB + e / (RB * 16)) * 32 + lane % 32, m = m0 + (wm * RB + e / 16 % RB) * 32 + e % 16 / 4 * 8 + 4 * h + e % 4;
+    if (m >= M || n >= N || finite(load_one<BMX_F32>(out, (int64_t)m * ldo + n))) continue;
+    store_one<BMX_F32>(out, (int64_t)m * ldo + n, by_value<BMX_F32, GROUP>(x, ldx, tiles, scales, K, m, n) + (bias ? bias[n] : 0.0f));
   }
 }
 
@@ -636,6 +670,7 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : SPLIT) void w4_deep_k
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[0][0][i] += part[((p * 4 + wave) * 16 + i) * 64 + lane];
   }
+  bool good = true;
 #pragma unroll
   for (int c = 0; c < CB; ++c) {
     if (col[c] >= N) continue;
@@ -646,7 +681,15 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : SPLIT) void w4_deep_k
       for (int i = 0; i < 16; ++i) {
         const int m = m0 + (wm * RB + r) * 32 + 8 * (i / 4) + 4 * h + i % 4;
         if (m < M) store_one<TYPE>(out, (int64_t)m * ldo + col[c], acc[r][c][i] + add);
+        good &= finite(acc[r][c][i]);
       }
+  }
+  if (good) return;
+#pragma unroll 1
+  for (int e = 0; e < CB * RB * 16; ++e) {  // (from this lane's own stores, so that no register waits for it)
+    const int n = n0 + (wn * CB + e / (RB * 16)) * 32 + lane % 32, m = m0 + (wm * RB + e / 16 % RB) * 32 + e % 16 / 4 * 8 + 4 * h + e % 4;
+    if (m >= M || n >= N || finite(load_one<TYPE>(out, (int64_t)m * ldo + n))) continue;
+    store_one<TYPE>(out, (int64_t)m * ldo + n, by_value<TYPE, GROUP>(x, ldx, tiles, scales, K, m, n) + (bias ? bias[n] : 0.0f));
   }
 }
 

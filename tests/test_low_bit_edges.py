@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_1705_09864_amd import binding as B
-from test_low_bit import TYPES, Cache, fill, host
+from test_low_bit import TYPES, Cache, check_fc, fill, host, random_tiles, unpack
 
 pytestmark = pytest.mark.gpu
 TOP = 2**31 - 1
@@ -210,3 +210,50 @@ def test_kv_attention_negative_scales(kind, seqs):
     k, v = B.kv_read(c.pages, c.scales, c.table, c.lens(), 64, torch.float32, 230 * seqs)
     want = np.concatenate([c.values(i).transpose(0, 2, 1, 3) for i in range(seqs)], 1)
     np.testing.assert_array_equal(torch.stack([k, v]).cpu().numpy(), want)
+
+
+# ------------------------------------------------------------------ 4-bit products of values that are not finite, or nearly so
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("M,N,K,group", [(6, 70, 300, 32), (6, 100, 1100, 128), (20, 40, 330, 64), (33, 60, 300, 32), (50, 70, 520, 128), (64, 6200, 200, 64),
+                                         (100, 130, 300, 64), (260, 4100, 200, 32), (520, 4200, 200, 64), (1050, 4250, 150, 128), (330, 2100, 300, 64)])
+def test_w4_fc_not_finite(M, N, K, group, kind):
+    """Infinities of one sign, of both, on weights that are 0, beside a NaN; values whose 31-fold is beyond fp32: what the definition gives, and the
+    rows beside them as ever."""
+    g = torch.Generator(device="cuda").manual_seed(M)
+    tiles = random_tiles(g, N, K, group)[0]
+    s = (torch.rand((tiles.shape[0], tiles.shape[1] * 128 // group, 16), device="cuda", generator=g) * 0.01 + 0.001).bfloat16()
+    scales = torch.stack([s, -8 * s], -1)  # (level 8 is a weight of 0)
+    x = torch.randn((M, K), device="cuda", generator=g).to(TYPES[kind][0])
+    top = 65504.0 if kind == "f16" else 2.9e38
+    x[0, 3] = float("inf")
+    x[1, K - 1] = -float("inf")
+    x[2, 5], x[2, K - 2] = float("inf"), -float("inf")
+    x[3, 7], x[3, 40] = float("inf"), float("nan")
+    x[4, :6] = torch.tensor([top, -top, top, top, -top, top], device="cuda")
+    special = list(range(5)) + ([M - 1] if M > 6 else [])
+    x[special[-1] if M > 6 else 0, 9] = float("inf")
+    bias = torch.randn((N,), device="cuda", generator=g)
+    out = B.w4_fc(x, tiles, scales, N, bias=bias)
+    q, sc, b = unpack(tiles, scales, N, K)
+    w, xs, add = q * sc + b, host(x), host(bias)
+    got = host(out)
+    u = TYPES[kind][1]
+    for r in special:
+        with np.errstate(invalid="ignore"):
+            terms = xs[r][None] * w
+            want = terms.sum(1) + add
+            size = np.abs(terms).sum(1) + np.abs(add)
+        fine = np.isfinite(want)
+        assert (np.isnan(got[r]) == np.isnan(want)).all(), r
+        assert (got[r][np.isinf(want)] == want[np.isinf(want)]).all(), r
+        if fine.any():
+            assert r == 4
+            # (results beyond the type's largest value are infinite)
+            limit = {"f16": 65504.0, "bf16": 3.3895e38, "f32": 3.4028e38}[kind]
+            bound = u * np.abs(want) + K * 2.0**-24 * size + 2.0**-25
+            inside = fine & (np.abs(want) + bound < limit)
+            assert (np.abs(got[r] - want) <= bound)[inside].all(), r
+            assert (np.abs(got[r]) >= limit * (1 - 2.0**-7))[fine & (np.abs(want) - bound > limit)].all()
+    rest = [r for r in range(M) if r not in special]
+    if rest:
+        check_fc(out[rest[:50]], x[rest[:50]], tiles, scales, N, K, kind, bias)
