@@ -73,6 +73,21 @@ struct Eight {
       }
     }
   }
+  // 16-bit types: values k to k + 7 of a row of K >= 8 values that begins at `row`, those from K on 0, by one load.  Where the row ends inside, it
+  // is of the row's last eight values, and they move down.
+  __device__ void load_within(const uint16_t* x, int64_t row, int k, int K) {
+    static_assert(TYPE != BMX_F32, "");
+    load(x, row + min(k, K - 8));
+    const int over = min(max(k + 8 - K, 0), 8);
+    u32x4 v = raw[0];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_alignbit(j < 3 ? v[j < 3 ? j + 1 : 3] : 0, v[j], 16 * (over & 1));
+#pragma unroll
+    for (int by = 1; by <= 4; by *= 2)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = over / 2 & by ? (j + by < 4 ? v[j + by < 4 ? j + by : 3] : 0) : v[j];
+    raw[0] = v;
+  }
   __device__ void parts(u32x4 (&part)[kParts]) const {
     if constexpr (TYPE != BMX_F32) {
       part[0] = raw[0];
@@ -261,13 +276,21 @@ __global__ __launch_bounds__(1024 / MT) void w4_few_kernel(const uint16_t* x, in
         const char* b = base + kt * 256;
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(from[i]), "s"(b) : "memory");
       }
-    } else {  // rows on odd elements, and the last step of fewer than 128 values
+    } else {  // rows on odd elements, and the last step of fewer than 128 values: eight loads on their way at a time
+      int id = lane;
+      asm volatile("" : "+v"(id));  // (its addresses are made here, not ahead of the loop for every launch)
+      const auto row = [&](int i) { return (int64_t)min(m0 + 4 * i + id / 16, M - 1) * ldx; };
+      const auto chunk = [&](int i) { return kt * 128 + ((id % 16) ^ ((4 * i + id / 16) % 16)) * 8; };
 #pragma unroll 1
-      for (int i = 0; i < MINE; ++i) {
-        const int chunk = (lane % 16) ^ ((4 * i + g) % 16);
-        Eight<TYPE> in;
-        in.load(x, (int64_t)min(m0 + 4 * i + g, M - 1) * ldx + kt * 128 + chunk * 8, K - kt * 128 - chunk * 8);
-        mem[wave][buf][i * 64 + lane] = in.raw[0];
+      for (int i0 = 0; i0 < MINE; i0 += 8) {
+        Eight<TYPE> in[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (K >= 8) in[i].load_within(x, row(i0 + i), chunk(i0 + i), K);
+          else in[i].load(x, row(i0 + i) + chunk(i0 + i), K - chunk(i0 + i));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mem[wave][buf][(i0 + i) * 64 + lane] = in[i].raw[0];
       }
     }
     const int64_t tile = (int64_t)nt * all + kt;
@@ -557,12 +580,21 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : SPLIT) void w4_deep_k
         const char* b = base + t * 256;
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(from[i]), "s"(b) : "memory");
       }
-    } else {  // rows on odd elements, and the last step of fewer than 128 values
+    } else {  // rows on odd elements, and the last step of fewer than 128 values: four loads on their way at a time
+      int id = tid;
+      asm volatile("" : "+v"(id));  // (its addresses are made here, not ahead of the loop for every launch)
+      const int k = t * 128 + (id % 16 ^ id / 16) * 8;
 #pragma unroll 1
-      for (int i = 0; i < MINE; ++i) {
-        Eight<TYPE> in;
-        in.load(x, (int64_t)min(m0 + tid / 16 + 16 * i, M - 1) * ldx + t * 128 + chunk * 8, K - t * 128 - chunk * 8);
-        mem[at_x(buf) + i * 256 + tid] = in.raw[0];
+      for (int i0 = 0; i0 < MINE; i0 += 4) {
+        Eight<TYPE> in[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int64_t row = (int64_t)min(m0 + id / 16 + 16 * (i0 + i), M - 1) * ldx;
+          if (K >= 8) in[i].load_within(x, row, k, K);
+          else in[i].load(x, row + k, K - k);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mem[at_x(buf) + (i0 + i) * 256 + tid] = in[i].raw[0];
       }
     }
   };

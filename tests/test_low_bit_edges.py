@@ -257,3 +257,23 @@ def test_w4_fc_not_finite(M, N, K, group, kind):
     rest = [r for r in range(M) if r not in special]
     if rest:
         check_fc(out[rest[:50]], x[rest[:50]], tiles, scales, N, K, kind, bias)
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("K", [1, 2, 7, 8, 9, 15, 63, 120, 127, 129, 134, 200, 255, 257, 383])
+@pytest.mark.parametrize("M,N", [(10, 40), (30, 50), (40, 70), (64, 33), (100, 64), (9, 6200), (200, 1100)])
+def test_w4_fc_rows_that_end_in_a_step(M, N, K, kind):
+    """Row lengths that end anywhere in a step of 128 and in eight values, rows on whole dwords and on odd elements, the last of them at the end of
+    its memory; what lies behind a row is NaN."""
+    g = torch.Generator(device="cuda").manual_seed(K)
+    tiles, scales = random_tiles(g, N, K, 64)
+    q, s, b = (torch.from_numpy(a).cuda() for a in unpack(tiles, scales, N, K))
+    for ld, shift in ((K, 0), (K + 1, 0), (K + 3, 1), (K + (K % 2) + 2, 0), (K + 8, 2)):
+        memory = torch.full((M * ld,), float("nan"), device="cuda", dtype=TYPES[kind][0])
+        x = memory.as_strided((M, K), (ld, 1), shift if shift + (M - 1) * ld + K <= M * ld else 0)
+        x.copy_(torch.randn((M, K), device="cuda", generator=g))
+        y = B.w4_fc(x, tiles, scales, N)
+        want = x.double() @ (q * s + b).t().contiguous()
+        size = x.double().abs() @ (31 * s.abs() + (b - 16 * s).abs()).t().contiguous()
+        least = 2.0**-25 if kind == "f16" else 1e-30  # (a float16 is a multiple of 2^-24)
+        assert bool(((y.double() - want).abs() <= TYPES[kind][1] * want.abs() + (K / 32 + 64) * 2.0**-24 * size + least).all()), (ld, shift)
