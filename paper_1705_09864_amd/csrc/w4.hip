@@ -238,9 +238,12 @@ __global__ __launch_bounds__(kMostWaves * 64) void w4_rows_kernel(const void* x,
 template <int TYPE, int MT>
 void launch_rows(const void* x, int64_t ldx, const void* tiles, const void* scales, int group, const float* bias, int M, int N, int K,
                  void* out, int64_t ldo, hipStream_t s) {
-  // Four waves; eight where a CU has one workgroup and each wave many steps (1 x 4096 x 9216: 8.2 -> 7.8 us; x 4096: 5.0 -> 5.2).
+  // Four waves; eight where a CU has one workgroup, each wave many steps and x few rows.  us with four and eight, 4096 columns: bf16, one row, K = 9216 8.0, 7.7,
+  // 8192 7.3, 7.1, 6144 6.3, 6.4, 4096 4.6, 5.0; four rows of 9216 9.2, 9.5, eight 10.5, 11.4.  f32, one row 4096 10.0, 8.7, 9216 19.2, 15.8; eight rows 10.2,
+  // 9.8 and 20.3, 17.2; of K = 1024 5.2, 5.6; twelve rows of 4096 11.9, 12.6.
   const dim3 grid((N + 15) / 16, (M + 16 * MT - 1) / (16 * MT));
-  const dim3 block(64 * std::min(grid.x * grid.y <= 256 && K >= 8192 ? 8 : 4, (K + 127) / 128));
+  const bool deep = TYPE == BMX_F32 ? M <= 8 && K >= 4096 : M <= 2 && K >= 8192;
+  const dim3 block(64 * std::min(grid.x * grid.y <= 256 && deep ? 8 : 4, (K + 127) / 128));
   auto* t = static_cast<const u32x4*>(tiles);
   auto* sc = static_cast<const uint32_t*>(scales);
   const auto kern = group == 32 ? w4_rows_kernel<TYPE, MT, 32> : group == 64 ? w4_rows_kernel<TYPE, MT, 64> : w4_rows_kernel<TYPE, MT, 128>;
@@ -248,7 +251,7 @@ void launch_rows(const void* x, int64_t ldx, const void* tiles, const void* scal
   note_kernel("w4_rows_kernel<%d,%d,%d> grid %dx%d block %d", TYPE, MT, group, (int)grid.x, (int)grid.y, (int)block.x);
 }
 
-// 16-bit types, 17 to 64 rows: as w4_rows_kernel, but a wave brings its steps of x into LDS of its own, a step ahead, and takes the operands from
+// 16-bit types, 9 to 64 rows: as w4_rows_kernel, but a wave brings its steps of x into LDS of its own, a step ahead, and takes the operands from
 // there.  (A lane's operand is 16 bytes of a row, and lanes side by side have rows below each other: read from memory so, 16 rows lie
 // on the same banks of the L1, and 64 rows of 4096 took 13 of 18 us to come.)
 template <int TYPE, int MT, int GROUP>
@@ -745,26 +748,34 @@ void launch_deep(const void* x, int64_t ldx, const void* tiles, const void* scal
 }
 
 // Few rows: 16 columns a workgroup, a stream of weights.  More: tiles of 64 x 64, or of 128 x 128 where they fill the chip.
-// bf16, 4096 columns, K = 4096, us: 16 rows 8.0, through LDS 5.7; 32 rows 11.8, 6.6, in tiles in four sets of waves 18; 64 rows 18, 11.5, 18; of
-// 9216 columns 32 rows 16 through LDS, in tiles 18, 64 rows 30 and 18.  In four, two, one set: 256 rows 20, 22, 28; 512 rows 37, 35, 36;
-// 2048 rows 145, 127, 120, and 89 in tiles of 128 x 128.  f32: 64 rows 38, in tiles 94; 256 rows 152, 94; 2048 rows 1150, 294.
+// 16-bit types, us of the kernel of few rows, through LDS, in tiles.  K = 4096, 4096 columns: 16 rows 8.1, 5.7, 17; 32 rows 12.1, 6.7, 18; 64 rows 21,
+// 11.6, 18.5.  Up to 32 rows LDS is ahead for more columns too where rows are whole (steps of 128, on whole dwords): 32 rows of 6144 21.0, 11.0,
+// 18.4; 9216 30.0, 15.8, 18.7; 12288 30.1, 16.6, 19.2; 16384 39, 21.4, 20.4; of K = 1024 13.7, 7.6, 8.8 at 9216; where they are not it is behind from
+// 6145 on: K = 1028, 9216 columns, 17 rows 9.5, 11.5, 8.9, 16 rows 8.6, 11.2, 8.8; on odd elements (K = 1023) 25, 11.9, 10.4 and 31, 12.2, 11.1.  33 to 64 rows
+// come through LDS while a CU has one workgroup of them: 64 rows of 4096 and of 4112 columns, K = 1024, 10.3, 6.1, 9.2 and 13.8, 9.9, 9.2; K = 8192 35.7,
+// 18.8, 31.0 and 51.6, 32.4, 31.3; and not on odd elements (K = 4095: 67, 60, 31; K = 513: 23, 12.4, 9.9).
+// Tiles in four, two, one set: 256 rows 20, 22, 28; 512 rows 37, 35, 36; 2048 rows 145, 127, 120, and 90 in tiles of 128 x 128.
+// f32: the tiles' time is 6 us and 0.0255 for each of K while the chip holds them at once, that of few rows 0.0165 us and 1.43e-5 of K for each of its workgroups (of 32
+// rows): level at 1780 (K + 235) / (K + 1150) of them.  4096 columns, few rows and tiles: K = 512, 96 rows 19.6, 19.1, 160 rows 30.5, 19.3; K = 2048, 160 rows
+// 58.8, 58.6; K = 4096, 160 rows 95, 110, 192 rows 114, 110; K = 8192, 192 rows 200, 215; 2048 rows of K = 4096 1150, 294.
 template <int TYPE>
 void launch_typed(const void* x, int64_t ldx, const void* tiles, const void* scales, int group, const float* bias, int M, int N, int K,
                   void* out, int64_t ldo, hipStream_t s) {
+  const bool dwords = (uintptr_t)x % 4 == 0 && (M == 1 || ldx % 2 == 0);  // (rows on whole dwords)
   const int64_t small = ceil_div(M, 64) * ceil_div(N, 64), large = ceil_div(M, 128) * ceil_div(N, 128);
   if constexpr (TYPE == BMX_F32) {
-    if (M > 32 && (int64_t)M * N > 160 * 4096) {
+    if (M > 32 && ceil_div(M, 32) * ceil_div(N, 16) * (K + 1150) > 1780 * (int64_t)(K + 235)) {
       const dim3 grid((uint32_t)(ceil_div(ceil_div(M, 64) * ceil_div(N, 128), 8) * 8));
       const auto kern = group == 32 ? w4_f32_kernel<32> : group == 64 ? w4_f32_kernel<64> : w4_f32_kernel<128>;
       launch_kernel(kern, grid, dim3(256), 0, s, x, ldx, static_cast<const u32x4*>(tiles), static_cast<const uint32_t*>(scales), bias, M, N, K, out, ldo);
       note_kernel("w4_f32_kernel<%d> grid %d block 256", group, (int)grid.x);
       return;
     }
-  } else if (M > 8 && M <= 64 && N <= 6144 && ldx < (1 << 24)) {
+  } else if (M > 8 && (M <= 32 ? N <= 6144 || (N <= 12288 && K % 128 == 0 && dwords) : M <= 64 && N <= 4096 && dwords) && ldx < (1 << 24)) {
     const auto f = M <= 32 ? launch_few<TYPE, 2> : launch_few<TYPE, 4>;
     f(x, ldx, tiles, scales, group, bias, M, N, K, out, ldo, s);
     return;
-  } else if ((M > 32 || (M > 16 && N > 6144)) && ldx < (1 << 24)) {  // (offsets within a tile's rows in 32 bits)
+  } else if (M > 8 && (M > 32 || (N > 6144 && (M > 16 || !dwords))) && ldx < (1 << 24)) {  // (offsets within a tile's rows in 32 bits)
     const auto f = group == 128 && large >= 256 ? launch_deep<TYPE, 2, 2, 1> : small <= 256 ? launch_deep<TYPE, 1, 1, 4>
                  : small <= 512 ? launch_deep<TYPE, 1, 1, 2> : launch_deep<TYPE, 1, 1, 1>;
     f(x, ldx, tiles, scales, group, bias, M, N, K, out, ldo, s);

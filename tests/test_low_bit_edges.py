@@ -277,3 +277,24 @@ def test_w4_fc_rows_that_end_in_a_step(M, N, K, kind):
         size = x.double().abs() @ (31 * s.abs() + (b - 16 * s).abs()).t().contiguous()
         least = 2.0**-25 if kind == "f16" else 1e-30  # (a float16 is a multiple of 2^-24)
         assert bool(((y.double() - want).abs() <= TYPES[kind][1] * want.abs() + (K / 32 + 64) * 2.0**-24 * size + least).all()), (ld, shift)
+
+
+@pytest.mark.parametrize("M,N,K,group,kind,pad,kernel", [
+    (2, 700, 8192, 128, "bf16", 0, "block 512"), (3, 700, 8192, 128, "bf16", 0, "block 256"), (1, 4113, 8192, 128, "f16", 0, "block 256"),
+    (8, 300, 4096, 32, "f32", 0, "block 512"), (9, 300, 4096, 32, "f32", 0, "block 256"), (8, 300, 4000, 32, "f32", 0, "block 256"),
+    (9, 12288, 256, 64, "bf16", 0, "few_kernel<2,2"), (32, 12289, 256, 64, "bf16", 0, "deep_kernel"), (16, 12289, 256, 64, "bf16", 0, "rows_kernel"),
+    (16, 6145, 260, 64, "f16", 0, "rows_kernel"), (16, 6145, 256, 64, "f16", 1, "deep_kernel"), (16, 6144, 255, 64, "f16", 0, "few_kernel<1,2"),
+    (33, 4096, 300, 128, "f16", 0, "few_kernel<1,4"), (33, 4097, 300, 128, "f16", 0, "deep_kernel"), (64, 500, 300, 128, "f16", 1, "deep_kernel"),
+    (96, 4096, 512, 64, "f32", 0, "rows_kernel"), (160, 4096, 512, 64, "f32", 0, "f32_kernel"), (160, 2048, 2048, 64, "f32", 0, "rows_kernel")])
+def test_w4_fc_on_both_sides_of_each_line(M, N, K, group, kind, pad, kernel):
+    """Which kernel takes a call: sizes, types and alignment beside each line, and the kernels' results there."""
+    g = torch.Generator(device="cuda").manual_seed(M + K)
+    tiles, scales = random_tiles(g, N, K, group)
+    x = torch.randn((M, K + pad), device="cuda", generator=g).to(TYPES[kind][0])[:, :K]
+    y = B.w4_fc(x, tiles, scales, N)
+    assert kernel in B.last_kernel(), B.last_kernel()
+    q, s, b = (torch.from_numpy(a).cuda() for a in unpack(tiles, scales, N, K))
+    want = x.double() @ (q * s + b).t().contiguous()
+    size = x.double().abs() @ (31 * s.abs() + (b - 16 * s).abs()).t().contiguous()
+    bound = TYPES[kind][1] * want.abs() + (K / 32 + 64) * 2.0**-24 * size + (2.0**-25 if kind == "f16" else 1e-30)
+    assert bool(((y.double() - want).abs() <= bound).all())
