@@ -270,7 +270,7 @@ int bmx_quant_gemm(const float* a, int64_t lda, int bits_a, const float* w, int6
 /* ---- A decoder layer in few bits: 4-bit weights, a cache of 8 bits, attention over it ----
  *
  * Values are of `type` (BMX_F32, BMX_F16 or BMX_BF16) where a pointer is void*; sums, running maxima and scales are fp32, and a
- * result is rounded to its type once, at the end.
+ * result is rounded to its type once, at the end.  (For 16-bit results attention's weights go into the second product with 11 bits.)
  *
  * 4-bit weights with group scales.  Row n of W [N, K] is cut into groups of `group` = 32, 64 or 128 values, each with a scale s and an
  * offset b in bf16; a weight is w = s * q + b with a level q in 0..15.
@@ -315,8 +315,8 @@ typedef struct bmx_kv_cache {
 } bmx_kv_cache;
 
 /* Calls on the cache.  k, v and q, out are `rows` rows of heads, element d of head h of row r at r*X_row + h*X_head + d.  max_new: no
- * sequence has more rows in this call (0: not known; rows beyond it are not looked at); with starts NULL it follows from rows, a
- * multiple of sequences.
+ * sequence has more rows in this call (0: not known; rows beyond it, and rows that starts gives to no sequence, are neither read nor
+ * written); with starts NULL it follows from rows, a multiple of sequences.
  * bmx_kv_write: quantises the rows into the cache, at each sequence's last positions.  A block's scale is max |x| / 127 over its tokens; one
  *   that holds older tokens keeps its scale s_old unless a new value is past 127 * s_old, and then the older levels become
  *   round(q * (s_old / s)).  New levels are round(x * (1 / s)) (all 0 where s < 2^-126), to the nearest, ties to even.  Scales are taken over

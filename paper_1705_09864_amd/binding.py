@@ -310,13 +310,15 @@ def kv_write(k, v, pages, scales, table, lengths, starts=None, max_new=0, stream
 
 
 def kv_read(pages, scales, table, lengths, dim, dtype, rows, starts=None, max_new=0, out_k=None, out_v=None, stream=None):
-    """The last tokens of each sequence, `rows` in all, as kv_write takes them: (k, v), each [rows, heads, dim] of `dtype`."""
+    """The last tokens of each sequence, `rows` in all, as kv_write takes them: (k, v), each [rows, heads, dim] of `dtype`.  Rows that are no
+    sequence's (by starts and max_new) are not written."""
     return (_native or _host()).kv_read(pages, scales, table, lengths, dim, dtype, rows, starts, max_new, out_k, out_v, stream)
 
 
 def kv_attention(q, pages, scales, table, lengths, starts=None, max_new=0, scale=None, causal=True, window=0, lse=False, out=None,
                  workspace=None, stream=None):
-    """Attention of each sequence's last tokens, q [rows, q_heads, dim], over its part of the cache; scale: 1 / sqrt(dim) if None.
+    """Attention of each sequence's last tokens, q [rows, q_heads, dim], over its part of the cache; scale: 1 / sqrt(dim) if None.  Rows that
+    are no sequence's (by starts and max_new) are not written.
     lse: returns (out, log of the softmax's sum, fp32 [rows, q_heads]).  workspace: a tensor of
     workspace_bytes(OP_KV_ATTENTION, (sequences, pages of one, heads, q_heads, dim, max_new)) bytes or more (max_new there: the most new rows
     of any call that uses it, 0: any number), zeros before its first use and kept from call to call on one stream; None: made and cleared

@@ -9,7 +9,8 @@
 //   q goes in with its row's largest value brought to [128, 256) by a power of two (exact but for values 2^-21 below the row's largest);
 //   p goes in as p * c_b / W * 2^14 with W the row's own largest |p c_b| so far: at most 2^14, and with all of f16's 11 bits down to 2^-28 of that.
 //   So neither tokens that the row does not see nor values without weight say how well the others are held.  W is kept as its logarithm, `lead`,
-//   relative to the running maximum.
+//   relative to the running maximum.  11 bits beside results of 11 or 8: error against 64 bits, f16, 5 rows over a window of 1000 2.4e-4, with weights in 32 bits 2.1e-4;
+//   bf16, all cases, 1.7e-3 with either.
 // For f32 results they are bf16's, q and p * c_b in three parts of 8 bits each, which together are all of them whatever the range; levels
 // are exact in bf16 too.
 //
@@ -134,7 +135,9 @@ constexpr int kWaves = 4;
 constexpr int kCounters = 16384;  // of the workspace's head; what needs more than these has rows enough not to be split
 constexpr int kMostSplits = 128;
 constexpr int kLeastPages = 16;   // of a split of many rows
-constexpr int kLeastTiles = 128;  // of 128 rows, for the kernel for many
+// Tiles of 128 rows for the kernel for many.  With fewer the two are level by lengths, which only the device knows: 256 new tokens (64 tiles, 32 heads on 8 of
+// 128) over 512 13 us in 16 rows and 27 in 128, over 4096 49 and 49, over 16384 173 and 118; 128 new ones over 4096 32 and 49, over 65536 396 and 220.
+constexpr int kLeastTiles = 128;
 constexpr int64_t kMostTiles = 65535;  // of 16 rows: a launch's second dimension
 
 template <int TYPE, int DC>
@@ -422,7 +425,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
 // converts it on its way), and a lane has one row's scores of 16 of 32 tokens, which again are those of its own column of P^T.
 // Bound by the vector ALU: 64 tokens x 32 rows are 32 matrix-core products, 1024 cycles, and 32 exponentials, maxima, conversions a lane,
 // 1600 cycles, and of two waves on a SIMD the one's products overlap little with the other's instructions (counters: matrix cores busy
-// 29% of the time, vector ALU 50%).  2 prompts of 2048 new tokens over 4096, 32 heads on 8 of 128: 289 us, 710 TFLOP/s; 16 rows a wave, each
+// 29% of the time, vector ALU 50%).  2 prompts of 2048 new tokens over 4096, 32 heads on 8 of 128: 283 to 287 us, 720 TFLOP/s; 16 rows a wave, each
 // with pages of its own, 508.  The next page's scores computed beside this page's exponentials, which takes more registers than two
 // waves have: 385.
 // So where all of a page is seen and no scale of its values is far below the row's W, the scale goes into the exponent,
@@ -430,7 +433,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
 // and comes out of the sum of p again once for each 16 tokens.
 // SPLIT: tiles of rows fewer than the chip holds workgroups at once, whose pages are split and joined as above (a kernel of its own: the
 // splits' arithmetic in the one kernel cost it 1%).  512 new tokens over 4096: 68 us, 120 unsplit; the join is some 15 us of that.
-// Eight waves to a page, which halves the conversions, fill the chip less evenly: 272 us where 289 is, but 163 where 122, 713 where 677.
+// Eight waves to a page, which halves the conversions, fill the chip less evenly: 272 us where 289 was, but 163 where 122, 713 where 677.
 template <int TYPE, int DC, bool SPLIT>
 __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_cache c, Args a) {
   static_assert(TYPE != BMX_F32, "");

@@ -535,9 +535,9 @@ __global__ __launch_bounds__(256) void w4_f32_kernel(const void* x, int64_t ldx,
   }
 }
 
-// 16-bit types: 64 RB x 64 CB of y per workgroup of 2 x 2 waves, 32 RB x 32 CB each.  x comes into LDS without passing registers, a step ahead.  Sums over the groups of x, which the
-// offsets take, are products with ones on the matrix cores; of two 32-row blocks of a wave each column of waves makes its own, and they
-// meet through LDS a step later.  With SPLIT the workgroup has as many sets of four waves, which take turns at K's steps and join at the end.
+// 16-bit types: 64 RB x 64 CB of y per workgroup of 2 x 2 waves, 32 RB x 32 CB each.  x comes into LDS without passing registers, a step ahead.  Sums
+// over the groups of x, which the offsets take, are products with ones on the matrix cores: one for each other at 64 x 64, one for four at 128 x 128, where of a
+// wave's two 32-row blocks each column of waves makes its own, and they meet through LDS a step later.  With SPLIT the workgroup has as many sets of four waves, which take turns at K's steps and join at the end.
 template <int TYPE, int RB, int CB, int GROUP, int SPLIT>
 __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : SPLIT) void w4_deep_kernel(const uint16_t* x, int64_t ldx, bool async, const u32x4* tiles,
                                                                  const uint32_t* scales, const float* bias, int M, int N, int K,

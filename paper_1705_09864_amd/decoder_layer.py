@@ -3,7 +3,7 @@
     python -m paper_1705_09864_amd.decoder_layer
 
 runs prompts of uneven lengths and then a token at a time, and prints how far the layer is from the same layer in float32 with
-its own weights, and what a step takes.
+its own weights, and what a step takes.  It rotates nothing by position and gives no pages back, and a step copies the lengths from the host.
 """
 import torch
 

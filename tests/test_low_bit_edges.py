@@ -298,3 +298,21 @@ def test_w4_fc_on_both_sides_of_each_line(M, N, K, group, kind, pad, kernel):
     size = x.double().abs() @ (31 * s.abs() + (b - 16 * s).abs()).t().contiguous()
     bound = TYPES[kind][1] * want.abs() + (K / 32 + 64) * 2.0**-24 * size + (2.0**-25 if kind == "f16" else 1e-30)
     assert bool(((y.double() - want).abs() <= bound).all())
+
+
+def test_kv_rows_of_no_sequence_are_left_alone():
+    """Rows before, between and behind those that starts gives out, and rows beyond max_new."""
+    c = Cache(3, 2, 2, 64, 16, 60)
+    g = fill(c, [70, 5, 30], "bf16", 11)
+    starts = torch.tensor([2, 6, 6, 11], dtype=torch.int32, device="cuda")  # (rows 2 to 5, none, 6 to 10)
+    q = torch.randn((13, 4, 64), device="cuda", generator=g).bfloat16()
+    taken = [2, 3, 4, 6, 7, 8]
+    out, k, v = (torch.full((13, h, 64), 7.0, device="cuda", dtype=torch.bfloat16) for h in (4, 2, 2))
+    B.kv_attention(q, c.pages, c.scales, c.table, c.lens(), starts=starts, max_new=3, out=out)
+    B.kv_read(c.pages, c.scales, c.table, c.lens(), 64, torch.bfloat16, 13, starts=starts, max_new=3, out_k=k, out_v=v)
+    for x in (out, k, v):
+        rest = [r for r in range(13) if r not in taken]
+        assert bool((x[rest] == 7.0).all()) and not bool((x[taken] == 7.0).any())
+    q[rest] = float("nan")
+    again = B.kv_attention(q, c.pages, c.scales, c.table, c.lens(), starts=starts, max_new=3, out=torch.empty_like(out))
+    assert torch.equal(again[taken], out[taken])
