@@ -92,13 +92,12 @@ __device__ inline f32x4 get4(const float* p) {
   return __builtin_bit_cast(f32x4, u32x4{a[0], a[1], b[0], b[1]});
 }
 
-// A value's scale times what a row's weights are multiplied with.  Bounded, as a weight of 0 has to bring 0: also in a block that nobody has
-// written, where the scale is anything, and where the row's other weights are far below it.
-__device__ inline float bounded(float x) { return __builtin_amdgcn_fmed3f(x, -0x1.fffffep127f, 0x1.fffffep127f); }
-// A score: the product, rounded.  (The barrier keeps it from becoming one operation with the difference from the maximum, which is a rounded product: of
-// scores beyond 2^24 that difference need not be below 0 then, and 2 to its power not below 1.)
-__device__ inline float score(float x, float f) {
-  float z = x * f;
+// A value's scale times what a row's weights are multiplied with.  Bounded, as a weight of 0 has to bring 0 where the row's other weights times scales
+// are far below this scale; NaN stays.
+__device__ inline float bounded(float x) { return fabsf(x) > 0x1.fffffep127f ? copysignf(0x1.fffffep127f, x) : x; }
+// A rounded product as it is, at the place where it is used: the barrier keeps it from becoming one operation with the difference from the maximum, which is
+// of rounded products (of scores beyond 2^24 that difference need not be below 0 then, and 2 to its power not below 1).
+__device__ inline float rounded(float z) {
   asm("" : "+v"(z));
   return z;
 }
@@ -270,19 +269,19 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
     for (int u = 0; u < 4; ++u) {
       const float f = factor * key_scale[u];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[u][i] = score(p[u][i], f);
+      for (int i = 0; i < 4; ++i) p[u][i] *= f;
+      tops[u] = fmaxf(fmaxf(fmaxf(p[u][0], p[u][1]), p[u][2]), p[u][3]);
     }
     if (!kv_all_in(t0, kPage, low_all, high_all)) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < 4; ++u) {
+        const int t = t0 + 16 * u;
+        if (t >= high || t + 15 < low) value_scale[u] = 0.0f;  // (a block that the row does not see, or that nobody has written, has any scale)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = t0 + 16 * u + 4 * g + i;
-          p[u][i] = t < high && t >= low ? p[u][i] : -INFINITY;
-        }
+        for (int i = 0; i < 4; ++i) p[u][i] = t + 4 * g + i < high && t + 4 * g + i >= low ? p[u][i] : -INFINITY;
+        tops[u] = fmaxf(fmaxf(fmaxf(p[u][0], p[u][1]), p[u][2]), p[u][3]);
+      }
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) tops[u] = fmaxf(fmaxf(p[u][0], p[u][1]), fmaxf(p[u][2], p[u][3]));
     float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     top = max_32(max_16(top));
     const float m_new = fmaxf(m, top), m_at = or_zero(m_new), shrink = __builtin_amdgcn_exp2f(m - m_at);
@@ -300,10 +299,10 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
     u32x4 w[PARTS][2];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const float f = bounded(F16 ? value_scale[u] * unit * 0x1p14f : value_scale[u]);
+      const float f = F16 ? bounded(value_scale[u] * unit * 0x1p14f) : value_scale[u];
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
-        const float e0 = __builtin_amdgcn_exp2f(p[u][i] - m_at), e1 = __builtin_amdgcn_exp2f(p[u][i + 1] - m_at);
+        const float e0 = __builtin_amdgcn_exp2f(rounded(p[u][i]) - m_at), e1 = __builtin_amdgcn_exp2f(rounded(p[u][i + 1]) - m_at);
         sum += e0 + e1;
         uint32_t part[PARTS];
         pair<PARTS>(e0 * f, e1 * f, part);
@@ -617,11 +616,13 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
         const float unit = __builtin_amdgcn_exp2f(-lead);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const float f = bounded(of_lane(scale_of, 4 + u) * unit * 0x1p14f), k = full ? key_scale[u] : 1.0f;
+          // (a block that the row does not see, or that nobody has written, has any scale)
+          const bool sees = full || (t0 + 16 * u < high && t0 + 16 * u + 15 >= low);
+          const float f = sees ? bounded(of_lane(scale_of, 4 + u) * unit * 0x1p14f) : 0.0f, k = full ? key_scale[u] : 1.0f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float e0 = __builtin_amdgcn_exp2f(score(z[u / 2][u % 2 * 8 + 2 * i], k) - m_at);
-            const float e1 = __builtin_amdgcn_exp2f(score(z[u / 2][u % 2 * 8 + 2 * i + 1], k) - m_at);
+            const float e0 = __builtin_amdgcn_exp2f(rounded(z[u / 2][u % 2 * 8 + 2 * i] * k) - m_at);
+            const float e1 = __builtin_amdgcn_exp2f(rounded(z[u / 2][u % 2 * 8 + 2 * i + 1] * k) - m_at);
             l += e0 + e1;
             uint32_t part[1];
             pair<1>(e0 * f, e1 * f, part);

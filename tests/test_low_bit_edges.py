@@ -316,3 +316,33 @@ def test_kv_rows_of_no_sequence_are_left_alone():
     q[rest] = float("nan")
     again = B.kv_attention(q, c.pages, c.scales, c.table, c.lens(), starts=starts, max_new=3, out=torch.empty_like(out))
     assert torch.equal(again[taken], out[taken])
+
+
+@pytest.mark.parametrize("seqs", [1, 64])
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 20), (False, 0)])
+def test_kv_attention_scales_that_are_no_numbers(kind, seqs, causal, window):
+    """A block whose scale is NaN or infinite spoils the rows that see it, of keys as of values, and no row beside them in their tile."""
+    rows, c = 40, Cache(seqs, 3, 2, 64, 16, 70)
+    g = fill(c, [128] * seqs, "f32", 12)
+    q = torch.randn((seqs * rows, 6, 64), device="cuda", generator=g).to(TYPES[kind][0])
+    args = dict(causal=causal, window=window)
+    want = B.kv_attention(q, c.pages, c.scales, c.table, c.lens(), **args)
+    assert ("kv_prompt" in B.last_kernel()) == (seqs > 1 and kind != "f32")
+    pos = torch.arange(88, 128, device="cuda")
+    for which in (0, 1):
+        for bad in (float("nan"), float("inf")):
+            for block in (7, 6, 5):  # (positions 112 to 127, 96 to 111, 80 to 95)
+                scales = c.scales.clone()
+                scales[c.table[:, block // 4].long(), 1, which, block % 4] = bad  # (of the second head of the cache)
+                out = B.kv_attention(q, c.pages, scales, c.table, c.lens(), **args).unflatten(0, (seqs, rows))
+                sees = torch.ones(rows, dtype=torch.bool, device="cuda")
+                if causal:
+                    sees &= pos >= 16 * block
+                if window:
+                    sees &= pos - window < 16 * block + 15
+                clean = want.unflatten(0, (seqs, rows))
+                assert torch.equal(out[:, :, :3], clean[:, :, :3]) and torch.equal(out[:, ~sees], clean[:, ~sees])
+                if which == 0 and bad == float("inf"):  # (a score of -infinity is no weight)
+                    continue
+                assert not bool(torch.isfinite(out[:, sees][:, :, 3:]).all(-1).any())
