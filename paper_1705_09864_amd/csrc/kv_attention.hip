@@ -614,15 +614,21 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
         l += all * __builtin_amdgcn_exp2f(lead - 14.0f);
       } else {
         const float unit = __builtin_amdgcn_exp2f(-lead);
+        if (full) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[u / 2][u % 2 * 8 + i] *= key_scale[u];
+        }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           // (a block that the row does not see, or that nobody has written, has any scale)
           const bool sees = full || (t0 + 16 * u < high && t0 + 16 * u + 15 >= low);
-          const float f = sees ? bounded(of_lane(scale_of, 4 + u) * unit * 0x1p14f) : 0.0f, k = full ? key_scale[u] : 1.0f;
+          const float f = sees ? bounded(of_lane(scale_of, 4 + u) * unit * 0x1p14f) : 0.0f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float e0 = __builtin_amdgcn_exp2f(rounded(z[u / 2][u % 2 * 8 + 2 * i] * k) - m_at);
-            const float e1 = __builtin_amdgcn_exp2f(rounded(z[u / 2][u % 2 * 8 + 2 * i + 1] * k) - m_at);
+            const float e0 = __builtin_amdgcn_exp2f(rounded(z[u / 2][u % 2 * 8 + 2 * i]) - m_at);
+            const float e1 = __builtin_amdgcn_exp2f(rounded(z[u / 2][u % 2 * 8 + 2 * i + 1]) - m_at);
             l += e0 + e1;
             uint32_t part[1];
             pair<1>(e0 * f, e1 * f, part);
