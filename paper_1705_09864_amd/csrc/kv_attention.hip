@@ -102,6 +102,7 @@ __device__ inline float rounded(float z) {
   return z;
 }
 __device__ inline float or_zero(float x) { return x == -INFINITY ? 0.0f : x; }
+constexpr float kLargeScore = 0x1p20f;  // scores from here on lose too much beside a scale's logarithm: its sums are taken relative to the maximum
 constexpr float kLeastLead = -100.0f;  // (so that its power stays a number: a row whose weights times scales are all below 2^-100 is held to that)
 
 // The larger of x and that of the lane 16, and 32, away.
@@ -282,16 +283,23 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
         tops[u] = fmaxf(fmaxf(fmaxf(p[u][0], p[u][1]), p[u][2]), p[u][3]);
       }
     }
-    float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), ahead = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) ahead = F16 ? fmaxf(ahead, tops[u] + value_log[u]) : 0.0f;
     top = max_32(max_16(top));
+    if constexpr (F16) ahead = max_32(max_16(ahead));
     const float m_new = fmaxf(m, top), m_at = or_zero(m_new), shrink = __builtin_amdgcn_exp2f(m - m_at);
     float sum = 0.0f, shrink_o = shrink, unit = 1.0f;
     if constexpr (F16) {
       const float before = lead + (m - m_at);
-      lead = fmaxf(before, kLeastLead);
+      ahead -= m_at;
+      if (__any(fabsf(m_at) >= kLargeScore)) {
+        ahead = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) lead = fmaxf(lead, tops[u] - m_at + value_log[u]);
-      lead = max_32(max_16(lead));
+        for (int u = 0; u < 4; ++u) ahead = fmaxf(ahead, tops[u] - m_at + value_log[u]);
+        ahead = max_32(max_16(ahead));
+      }
+      lead = fmaxf(fmaxf(before, ahead), kLeastLead);
       shrink_o = __builtin_amdgcn_exp2f(before - lead);
       unit = __builtin_amdgcn_exp2f(-lead);
     }
@@ -579,21 +587,27 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_
           }
         }
       }
-      float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-      top = max_32(top);
+      float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), ahead = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) ahead = fmaxf(ahead, tops[u] + value_log[u]);
+      top = max_32(top), ahead = max_32(ahead);
       const float m_new = fmaxf(m, top), m_at = or_zero(m_new), shrink = __builtin_amdgcn_exp2f(m - m_at);
       const float before = lead + (m - m_at);
-      lead = fmaxf(before, kLeastLead);
+      const bool large = __any(fabsf(m_at) >= kLargeScore);
+      ahead -= m_at;
+      if (large) {
+        ahead = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) lead = fmaxf(lead, tops[u] - m_at + value_log[u]);
-      lead = max_32(lead);
+        for (int u = 0; u < 4; ++u) ahead = fmaxf(ahead, tops[u] - m_at + value_log[u]);
+        ahead = max_32(ahead);
+      }
+      lead = fmaxf(fmaxf(before, ahead), kLeastLead);
       const float shrink_o = __builtin_amdgcn_exp2f(before - lead);
       m = m_new;
       l *= shrink;
       u32x4 w[4];
       const float least = fminf(fminf(value_log[0], value_log[1]), fminf(value_log[2], value_log[3]));
-      // (scores beyond 2^20 lose too much in the sum of the exponents)
-      if (full && __all(least - lead >= -64.0f && fabsf(m_at) < 0x1p20f)) {
+      if (full && !large && __all(least - lead >= -64.0f)) {
         const float out_of = __builtin_amdgcn_rcpf(scale_of);
         float all = 0.0f;
 #pragma unroll
