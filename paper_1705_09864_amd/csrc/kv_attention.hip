@@ -432,14 +432,14 @@ __global__ __launch_bounds__(kWaves * 64) void kv_attention_kernel(bmx_kv_cache 
 // converts it on its way), and a lane has one row's scores of 16 of 32 tokens, which again are those of its own column of P^T.
 // Bound by the vector ALU: 64 tokens x 32 rows are 32 matrix-core products, 1024 cycles, and 32 exponentials, maxima, conversions a lane,
 // 1600 cycles, and of two waves on a SIMD the one's products overlap little with the other's instructions (counters: matrix cores busy
-// 29% of the time, vector ALU 50%).  2 prompts of 2048 new tokens over 4096, 32 heads on 8 of 128: 283 to 287 us, 720 TFLOP/s; 16 rows a wave, each
+// 29% of the time, vector ALU 50%).  2 prompts of 2048 new tokens over 4096, 32 heads on 8 of 128: 283 to 297 us by the card, 690 to 730 TFLOP/s; 16 rows a wave, each
 // with pages of its own, 508.  The next page's scores computed beside this page's exponentials, which takes more registers than two
 // waves have: 385.
 // So where all of a page is seen and no scale of its values is far below the row's W, the scale goes into the exponent,
 //   p c / W 2^14 = 2^(s + log2(c / W 2^14) - m),
 // and comes out of the sum of p again once for each 16 tokens.
 // SPLIT: tiles of rows fewer than the chip holds workgroups at once, whose pages are split and joined as above (a kernel of its own: the
-// splits' arithmetic in the one kernel cost it 1%).  512 new tokens over 4096: 68 us, 120 unsplit; the join is some 15 us of that.
+// splits' arithmetic in the one kernel cost it 1%).  512 new tokens over 4096: 70 us, 120 unsplit; the join is some 15 us of that.
 // Eight waves to a page, which halves the conversions, fill the chip less evenly: 272 us where 289 was, but 163 where 122, 713 where 677.
 template <int TYPE, int DC, bool SPLIT>
 __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv_prompt_kernel(bmx_kv_cache c, Args a) {
