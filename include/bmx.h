@@ -71,6 +71,7 @@ extern "C" {
 #define BMX_OP_BINARY_CONV2D_BITS 4 /* dims = {N, C, H, W, O, KH, KW, stride, pad, out_pad} */
 #define BMX_OP_XNOR_GEMM_W32 5 /* dims = {M, N, K} */
 #define BMX_OP_KV_ATTENTION 6 /* dims = {sequences, table_width, heads, q_heads, dim, max_new[, rows]} */
+#define BMX_OP_KV4_ATTENTION 7 /* as for BMX_OP_KV_ATTENTION */
 
 /* Sign-binarise and bit-pack (Sec. 1: binarisation with the sign function, 64
  * values per word; Sec. 3.1: the per-forward-pass input binarisation step).
@@ -338,6 +339,67 @@ int bmx_kv_read(const bmx_kv_cache* cache, void* k, void* v, int type, int64_t k
 int bmx_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
                      int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Which pages of a cache are whose, on the device: sequence i is to have change[i] tokens more, or that many fewer where it is below 0.
+ *   table, table_ld, table_width, lengths as a cache's; lengths are those before the call, and the new ones behind it.
+ *   pool    int32 [2 + num_pages]: how many pages are free, the call's status, and the stack of free pages, its top last.
+ *   starts  int32 [sequences + 1]: prefix sums of the sequences' new tokens, as the calls on the cache take them.
+ *   positions int32 [rows], slots int64 [rows], either or both NULL: for each new token's row its position, and 64 * its page + its place there; -1 and -1 in
+ *           rows behind the last.
+ * Pages that a sequence no longer reaches go onto the stack first, in the order of the sequences, each one's last page first; then pages are taken from the
+ * stack's top in the order of the sequences and of their places.  Places of the table, and of the stack, that are not in use keep what they held.
+ * All of it or nothing: pool[1] becomes 0, or, where a sequence would have fewer than no tokens or more than 64 * table_width, the pages run out or
+ * the new rows are more than `rows`, the number, from 1 on, of the first sequence that finds no room; then lengths, table and the rest of the pool are as they
+ * were, starts are zeros (so the calls behind this one find no rows), positions and slots -1.  A pool that is none (a count of free pages below 0 or above
+ * num_pages) gives -1 in the same way.  Kernels stay inside the buffers whatever the integers are.  One call at a time works on a pool. */
+int bmx_kv_resize(const int32_t* change, int sequences, int32_t* table, int64_t table_ld, int table_width, int32_t* lengths, int32_t* pool,
+                  int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int64_t rows, void* stream);
+
+/* Heads rotated by position: of each of `rows` rows of heads (element d of head h of row r at r*x_row + h*x_head + d) the first `rot` values, an even number up
+ * to dim, are pairs (a, b) that become
+ *   a' = factor * (a cos t - b sin t), b' = factor * (b cos t + a sin t),  t = positions[r] * freq[j],
+ * j the pair's number of rot/2: values 2j and 2j + 1 with interleaved, otherwise j and rot/2 + j.  The others are copied.  inverse: by -t, which with
+ * the same factor is the gradient's way.
+ *   positions int32 [rows], any; freq fp64 [rot/2], angles per position, of which the nearest whole number of turns is taken off in 64 bits (so far
+ *   positions turn as near ones do).  Results are fp32 sums rounded to the type.  out may be x itself, with the same strides; otherwise they must not
+ *   overlap.  heads up to 65535, rows up to 2^23. */
+int bmx_rotary(const void* x, int type, int64_t x_row, int64_t x_head, int heads, int dim, int64_t rows, const int32_t* positions,
+               const double* freq, int rot, int interleaved, float factor, int inverse, void* out, int64_t out_row, int64_t out_head,
+               void* stream);
+
+/* A paged cache of keys and values in 4 bits: as the cache of 8 bits, but each token's head has a scale s and an offset o of its own, for its key and for its
+ * value: a value is q * s + o with a level q in 0..15.
+ *   pages   uint8 [num_pages][heads][2][64*row], 16-byte aligned, row = dim rounded up to 32, halved; keys (0), then values (1).  Token t, value d: the low half
+ *           of a byte if d is even, the high one if not,
+ *           keys at    t*row + d/2,
+ *           values at  d/32*1024 + t%16/4*256 + d%32/2*16 + t/16*4 + t%4.
+ *           (In the order of the matrix cores' lanes; no byte has two tokens.)  What lies between dim and 2*row does not matter.
+ *   scales  bf16 [num_pages][heads][2][64][2], 16-byte aligned: s and o.
+ *   table, lengths, starts and the trust in them as in bmx_kv_cache. */
+typedef struct bmx_kv4_cache {
+  uint8_t* pages;
+  uint16_t* scales;
+  const int32_t* table;
+  int64_t table_ld;
+  const int32_t* lengths;
+  const int32_t* starts;
+  int sequences, table_width, num_pages, heads, dim; /* dim in 1..256 */
+} bmx_kv4_cache;
+
+/* Calls on it, with the arguments of the cache of 8 bits.
+ * bmx_kv4_write: quantises the rows into the cache, at each sequence's last positions: o = the least of a token's head's values and s = (the largest - o) / 15,
+ *   rounded to bf16 (a difference beyond fp32 counts as its largest number, one below 0, by o's rounding, as 0), levels round((x - o) / s), to the nearest, ties to even, 0 to 15, all 0 where s
+ *   is 0.  Both are taken over finite values; infinity is level 15, -infinity and NaN level 0.  No other token changes.
+ * bmx_kv4_read: the rows' values q * s + o, one rounding to fp32, then to the type; rows of tokens that are not there are zeros.
+ * bmx_kv4_attention: as bmx_kv_attention; workspace by BMX_OP_KV4_ATTENTION with the same numbers.  Either cache's workspace may be any stream's own, not
+ *   two streams' (nor two graphs' that run at once).  A row that sees a token whose scale or offset is no finite number has results that are none either. */
+int bmx_kv4_write(const bmx_kv4_cache* cache, const void* k, const void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row,
+                  int64_t v_head, int64_t rows, int max_new, void* stream);
+int bmx_kv4_read(const bmx_kv4_cache* cache, void* k, void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head,
+                 int64_t rows, int max_new, void* stream);
+int bmx_kv4_attention(const bmx_kv4_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
+                      int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                      void* workspace, size_t workspace_bytes, void* stream);
 
 /* alpha[r] = mean_j |w[r][j]| over cols entries per row (the XNOR-Net weight scale the
  * abstract refers to), accumulated in fp64 and rounded once to fp32.

@@ -9,6 +9,7 @@ no CPU fallback: if the HIP library cannot be loaded the import of this module's
 functions fails loudly on first use.
 """
 import ctypes
+import math
 import os
 
 import torch
@@ -20,7 +21,7 @@ _lib = None
 _native = None
 
 OP_BINARY_FC, OP_BINARY_CONV2D, OP_QUANT_GEMM, OP_BINARY_CONV2D_BITS, OP_XNOR_GEMM_W32 = 1, 2, 3, 4, 5
-OP_KV_ATTENTION = 6
+OP_KV_ATTENTION, OP_KV4_ATTENTION = 6, 7
 PAGE = 64  # tokens of a page of a cache
 EXPORTS = ["bmx_binarize_pack", "bmx_xnor_gemm", "bmx_binary_fc", "bmx_pack_conv_weights",
            "bmx_binary_conv2d", "bmx_quant_gemm", "bmx_alpha_mean_abs", "bmx_pack_nchw",
@@ -29,7 +30,7 @@ EXPORTS = ["bmx_binarize_pack", "bmx_xnor_gemm", "bmx_binary_fc", "bmx_pack_conv
            "bmx_binary_conv2d_bits", "bmx_xnor_gemm_count", "bmx_unpack_pm1", "bmx_widen_words32",
            "bmx_xnor_gemm_w32", "bmx_binary_fc_static", "bmx_last_kernel",
            "bmx_probe_valu", "bmx_w4_quantize", "bmx_w4_dequantize", "bmx_w4_fc", "bmx_kv_write", "bmx_kv_read",
-           "bmx_kv_attention"]
+           "bmx_kv_attention", "bmx_kv_resize", "bmx_rotary", "bmx_kv4_write", "bmx_kv4_read", "bmx_kv4_attention"]
 
 _i64, _int, _p, _sz = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
 
@@ -38,6 +39,11 @@ class KvCache(ctypes.Structure):
     """bmx_kv_cache of include/bmx.h, for calls of the C functions themselves."""
     _fields_ = [("pages", _p), ("scales", _p), ("table", _p), ("table_ld", _i64), ("lengths", _p), ("starts", _p), ("sequences", _int),
                 ("table_width", _int), ("num_pages", _int), ("heads", _int), ("dim", _int), ("block", _int)]
+
+
+class Kv4Cache(ctypes.Structure):
+    """bmx_kv4_cache of include/bmx.h."""
+    _fields_ = KvCache._fields_[:-1]
 
 
 class BmxError(RuntimeError):
@@ -102,7 +108,12 @@ def lib():
         L.bmx_kv_read.argtypes = L.bmx_kv_write.argtypes
         L.bmx_kv_attention.argtypes = [_kv, _p, _int, _i64, _i64, _int, _i64, _int, ctypes.c_float, _int, _int, _p, _i64, _i64,
                                        _p, _p, _sz, _p]
-        for name in EXPORTS[-6:]:
+        _kv4 = ctypes.POINTER(Kv4Cache)
+        L.bmx_kv_resize.argtypes = [_p, _int, _p, _i64, _int, _p, _p, _int, _p, _p, _p, _i64, _p]
+        L.bmx_rotary.argtypes = [_p, _int, _i64, _i64, _int, _int, _i64, _p, _p, _int, _int, ctypes.c_float, _int, _p, _i64, _i64, _p]
+        L.bmx_kv4_write.argtypes = L.bmx_kv4_read.argtypes = [_kv4] + L.bmx_kv_write.argtypes[1:]
+        L.bmx_kv4_attention.argtypes = [_kv4] + L.bmx_kv_attention.argtypes[1:]
+        for name in EXPORTS[-11:]:
             getattr(L, name).restype = _int
         for name in EXPORTS[:9]:
             getattr(L, name).restype = _int
@@ -325,3 +336,66 @@ def kv_attention(q, pages, scales, table, lengths, starts=None, max_new=0, scale
     in the call."""
     return (_native or _host()).kv_attention(q, pages, scales, table, lengths, starts, max_new, scale, causal, window, lse, out,
                                              workspace, stream)
+
+
+def page_pool(num_pages, device="cuda"):
+    """The pool of a cache of num_pages pages that are all free, for kv_resize: the number of free pages, the last call's status, the stack of
+    free pages.  Page 0 is the first that is taken."""
+    pool = torch.zeros((num_pages + 2,), dtype=torch.int32)
+    pool[0] = num_pages
+    pool[2:] = torch.arange(num_pages - 1, -1, -1)
+    return pool.to(device)
+
+
+def kv_resize(change, table, lengths, pool, rows, starts=None, positions=None, slots=None, stream=None):
+    """Sequence i has change[i] tokens more from here on (fewer where it is below 0): lengths, table and pool follow, on the GPU.  Returns (starts, positions,
+    slots): int32 [sequences + 1], the new tokens' rows as kv_write takes them; int32 [rows] and int64 [rows], each new token's position, and 64 * its page + its
+    place there, -1 in rows behind the last.  Where not everything has room (in the table, in the pool, among `rows` rows) nothing changes, pool[1] is the
+    number, from 1 on, of the first sequence that has none (0 otherwise), and starts are zeros, so the calls behind it find no rows."""
+    return (_native or _host()).kv_resize(change, table, lengths, pool, rows, starts, positions, slots, stream)
+
+
+def rotary_frequencies(rot, base=10000.0, stretch=1.0, trained=0, slow=1.0, fast=4.0, device="cuda"):
+    """Angles per position of the rot/2 pairs of rotary, fp64: base^(-2j/rot), for contexts `stretch` times as long as trained ones divided by stretch: all of them if
+    trained is 0; otherwise those that turn fewer than `slow` times over `trained` positions, and none that turn more than `fast` times, and in between a share
+    that grows evenly as the turns get fewer."""
+    if rot <= 0 or rot % 2 or base <= 0 or stretch <= 0 or trained < 0 or (trained and not 0 <= slow < fast):
+        raise ValueError("rotary_frequencies: no such frequencies: %r" % ((rot, base, stretch, trained, slow, fast),))
+    freq = float(base) ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
+    if trained:
+        keep = ((freq * (trained / (2 * math.pi)) - slow) / (fast - slow)).clamp(0, 1)
+        freq = freq * keep + freq / stretch * (1 - keep)
+    else:
+        freq = freq / stretch
+    return freq.to(device)
+
+
+def rotary(x, positions, freq, interleaved=False, factor=1.0, inverse=False, out=None, stream=None):
+    """x [rows, heads, dim], its heads' first 2 * len(freq) values rotated by their rows' positions (int32 [rows]) times freq (fp64, rotary_frequencies): pairs of
+    neighbours if interleaved, otherwise of a value and the one len(freq) behind it, times `factor`; inverse: the other way round, which is the gradient's.
+    out: may be x itself."""
+    return (_native or _host()).rotary(x, positions, freq, interleaved, factor, inverse, out, stream)
+
+
+def kv4_cache(num_pages, heads, dim, device="cuda"):
+    """New memory of a cache of 4 bits, (pages, scales): num_pages pages of 64 tokens, a scale and an offset for each token and head."""
+    row = (dim + 31) // 32 * 16
+    return (torch.zeros((num_pages, heads, 2, PAGE * row), dtype=torch.uint8, device=device),
+            torch.zeros((num_pages, heads, 2, PAGE, 2), dtype=torch.bfloat16, device=device))
+
+
+def kv4_write(k, v, pages, scales, table, lengths, starts=None, max_new=0, stream=None):
+    """As kv_write, into a cache of 4 bits."""
+    return (_native or _host()).kv4_write(k, v, pages, scales, table, lengths, starts, max_new, stream)
+
+
+def kv4_read(pages, scales, table, lengths, dim, dtype, rows, starts=None, max_new=0, out_k=None, out_v=None, stream=None):
+    """As kv_read, out of a cache of 4 bits."""
+    return (_native or _host()).kv4_read(pages, scales, table, lengths, dim, dtype, rows, starts, max_new, out_k, out_v, stream)
+
+
+def kv4_attention(q, pages, scales, table, lengths, starts=None, max_new=0, scale=None, causal=True, window=0, lse=False, out=None,
+                  workspace=None, stream=None):
+    """As kv_attention, over a cache of 4 bits; its workspace by workspace_bytes(OP_KV4_ATTENTION, ...)."""
+    return (_native or _host()).kv4_attention(q, pages, scales, table, lengths, starts, max_new, scale, causal, window, lse, out,
+                                              workspace, stream)

@@ -6,6 +6,7 @@
 #include "lazy_calls.h"
 
 #include <mutex>
+#include <type_traits>
 
 // Scratch memory of bmx_binary_fc_static, the entry point for callers that cannot allocate: one
 // copy per GPU the library runs on, held until the process ends.  In host code this name is only
@@ -87,13 +88,19 @@ constexpr int kMostSequences = 65535, kMostHeads = 32767, kMostRows = 65535 * 16
 // No sequence has more new rows than this, of `rows` in all.
 int64_t new_rows(int64_t max_new, int64_t rows) { return max_new == 0 || max_new > rows ? rows : max_new; }
 
+inline bool block_fits(const bmx_kv_cache& c) { return c.block == 16 || c.block == 32 || c.block == 64; }
+inline bool block_fits(const bmx_kv4_cache&) { return true; }
+constexpr size_t scales_align(const bmx_kv_cache*) { return 4; }
+constexpr size_t scales_align(const bmx_kv4_cache*) { return 16; }
+
 // The description of a cache and the number of a call's rows; *max_new becomes what it stands for.
-int kv_check(const bmx_kv_cache* c, int type, int64_t rows, int* max_new) {
+template <class Cache>
+int kv_check(const Cache* c, int type, int64_t rows, int* max_new) {
   if (!c) return BMX_ERR_NULL;
   if (c->sequences < 0 || c->sequences > kMostSequences || c->table_width < 0 || c->num_pages < 0 || c->heads <= 0 || c->heads > kMostHeads ||
       c->dim <= 0 || c->dim > 256 || rows < 0 || rows >= ((int64_t)1 << 31) || *max_new < 0)
     return BMX_ERR_SHAPE;
-  if (!is_type(type) || (c->block != 16 && c->block != 32 && c->block != 64)) return BMX_ERR_UNSUPPORTED;
+  if (!is_type(type) || !block_fits(*c)) return BMX_ERR_UNSUPPORTED;
   if (rows > 0 && c->sequences == 0) return BMX_ERR_SHAPE;
   if (!c->starts && rows > 0 && rows % c->sequences) return BMX_ERR_SHAPE;
   if (!c->starts) *max_new = rows > 0 ? (int)(rows / c->sequences) : 0;
@@ -102,7 +109,7 @@ int kv_check(const bmx_kv_cache* c, int type, int64_t rows, int* max_new) {
   if (rows == 0) return BMX_OK;
   if (!c->pages || !c->scales || !c->lengths || (!c->table && c->table_width > 0)) return BMX_ERR_NULL;
   if (c->table_ld < c->table_width) return BMX_ERR_LD;
-  if (misaligned(c->pages, 16) || misaligned(c->scales, 4) || misaligned(c->table, 4) || misaligned(c->lengths, 4) ||
+  if (misaligned(c->pages, 16) || misaligned(c->scales, scales_align(c)) || misaligned(c->table, 4) || misaligned(c->lengths, 4) ||
       misaligned(c->starts, 4))
     return BMX_ERR_ALIGN;
   return BMX_OK;
@@ -114,6 +121,31 @@ int kv_rows_check(const void* p, int type, int64_t row, int64_t head, int64_t ro
   if ((rows > 1 && row < dim) || (heads > 1 && head < dim)) return BMX_ERR_LD;
   if (misaligned(p, type == BMX_F32 ? 4 : 2)) return BMX_ERR_ALIGN;
   return BMX_OK;
+}
+
+template <class Cache>
+int kv_attention(const Cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
+                        int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                        void* workspace, size_t workspace_bytes, void* stream, bool fresh) {
+  constexpr bool few = std::is_same_v<Cache, bmx_kv4_cache>;
+  int st = kv_check(cache, type, rows, &max_new);
+  if (st != BMX_OK) return st;
+  if (q_heads <= 0 || q_heads % cache->heads || q_heads > 65535 || window < 0) return BMX_ERR_SHAPE;
+  if ((int64_t)max_new * (q_heads / cache->heads) > kMostRows) return BMX_ERR_SHAPE;
+  if (rows == 0) return BMX_OK;
+  if ((st = kv_rows_check(q, type, q_row, q_head, rows, q_heads, cache->dim)) != BMX_OK) return st;
+  if ((st = kv_rows_check(out, type, out_row, out_head, rows, q_heads, cache->dim)) != BMX_OK) return st;
+  if (misaligned(lse, 4)) return BMX_ERR_ALIGN;
+  const size_t need = round256((few ? bmx::kv4_attention_workspace_of_call : bmx::kv_attention_workspace_of_call)(
+      cache->sequences, cache->table_width, cache->heads, q_heads, cache->dim, max_new));
+  if (need && (!workspace || workspace_bytes < need)) return BMX_ERR_WORKSPACE;
+  if (need && misaligned(workspace, 16)) return BMX_ERR_ALIGN;
+  if constexpr (few)
+    return hip_status(bmx::launch_kv4_attention(*cache, q, type, q_row, q_head, q_heads, (int)rows, max_new, scale, causal != 0, window, out,
+                                                out_row, out_head, lse, workspace, fresh, (hipStream_t)stream));
+  else
+    return hip_status(bmx::launch_kv_attention(*cache, q, type, q_row, q_head, q_heads, (int)rows, max_new, scale, causal != 0, window, out,
+                                               out_row, out_head, lse, workspace, fresh, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -232,15 +264,18 @@ size_t bmx_workspace_bytes(int op, const int64_t* dims, int ndims) {
                       (int)dims[4])
           .total;
     }
-    case BMX_OP_KV_ATTENTION: {
+    case BMX_OP_KV_ATTENTION:
+    case BMX_OP_KV4_ATTENTION: {
+      const auto any = op == BMX_OP_KV_ATTENTION ? bmx::kv_attention_workspace : bmx::kv4_attention_workspace;
+      const auto one = op == BMX_OP_KV_ATTENTION ? bmx::kv_attention_workspace_of_call : bmx::kv4_attention_workspace_of_call;
       if (ndims != 6 && ndims != 7) return 0;
       for (int i = 0; i < ndims; ++i)
         if (dims[i] < (i == 2 || i == 3 || i == 4) || dims[i] >= ((int64_t)1 << 31)) return 0;
       if (dims[3] % dims[2] || dims[4] > 256) return 0;
-      if (ndims == 6) return round256(bmx::kv_attention_workspace(dims[0], dims[1], dims[2], dims[3], dims[4], dims[5]));
+      if (ndims == 6) return round256(any(dims[0], dims[1], dims[2], dims[3], dims[4], dims[5]));
       const int64_t most = new_rows(dims[5], dims[6]);
       if (dims[0] > kMostSequences || dims[2] > kMostHeads || most * (dims[3] / dims[2]) > kMostRows) return 0;  // (refused)
-      return round256(bmx::kv_attention_workspace_of_call(dims[0], dims[1], dims[2], dims[3], dims[4], most));
+      return round256(one(dims[0], dims[1], dims[2], dims[3], dims[4], most));
     }
     default: return 0;
   }
@@ -781,24 +816,6 @@ int bmx_kv_read(const bmx_kv_cache* cache, void* k, void* v, int type, int64_t k
   return hip_status(bmx::launch_kv_read(*cache, k, v, type, k_row, k_head, v_row, v_head, (int)rows, max_new, (hipStream_t)stream));
 }
 
-static int kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
-                        int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
-                        void* workspace, size_t workspace_bytes, void* stream, bool fresh) {
-  int st = kv_check(cache, type, rows, &max_new);
-  if (st != BMX_OK) return st;
-  if (q_heads <= 0 || q_heads % cache->heads || q_heads > 65535 || window < 0) return BMX_ERR_SHAPE;
-  if ((int64_t)max_new * (q_heads / cache->heads) > kMostRows) return BMX_ERR_SHAPE;
-  if (rows == 0) return BMX_OK;
-  if ((st = kv_rows_check(q, type, q_row, q_head, rows, q_heads, cache->dim)) != BMX_OK) return st;
-  if ((st = kv_rows_check(out, type, out_row, out_head, rows, q_heads, cache->dim)) != BMX_OK) return st;
-  if (misaligned(lse, 4)) return BMX_ERR_ALIGN;
-  const size_t need = round256(bmx::kv_attention_workspace_of_call(cache->sequences, cache->table_width, cache->heads, q_heads, cache->dim, max_new));
-  if (need && (!workspace || workspace_bytes < need)) return BMX_ERR_WORKSPACE;
-  if (need && misaligned(workspace, 16)) return BMX_ERR_ALIGN;
-  return hip_status(bmx::launch_kv_attention(*cache, q, type, q_row, q_head, q_heads, (int)rows, max_new, scale, causal != 0, window, out,
-                                             out_row, out_head, lse, workspace, fresh, (hipStream_t)stream));
-}
-
 int bmx_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
                      int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
                      void* workspace, size_t workspace_bytes, void* stream) {
@@ -809,6 +826,66 @@ int bmx_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t
 int bmx_fresh_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
                            int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
                            void* workspace, size_t workspace_bytes, void* stream) {
+  return kv_attention(cache, q, type, q_row, q_head, q_heads, rows, max_new, scale, causal, window, out, out_row, out_head, lse,
+                      workspace, workspace_bytes, stream, true);
+}
+
+int bmx_kv_resize(const int32_t* change, int sequences, int32_t* table, int64_t table_ld, int table_width, int32_t* lengths, int32_t* pool,
+                  int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int64_t rows, void* stream) {
+  if (sequences < 0 || sequences > kMostSequences || table_width < 0 || num_pages < 0 || num_pages > 0x7ffffffd || rows < 0 || rows >= ((int64_t)1 << 31)) return BMX_ERR_SHAPE;
+  if (!pool || !starts || (sequences > 0 && (!change || !lengths || (!table && table_width > 0)))) return BMX_ERR_NULL;
+  if (table_ld < table_width) return BMX_ERR_LD;
+  if (misaligned(change, 4) || misaligned(table, 4) || misaligned(lengths, 4) || misaligned(pool, 4) || misaligned(starts, 4) ||
+      misaligned(positions, 4) || misaligned(slots, 8))
+    return BMX_ERR_ALIGN;
+  return hip_status(bmx::launch_kv_resize(change, sequences, table, table_ld, table_width, lengths, pool, num_pages, starts, positions, slots, (int)rows,
+                                          (hipStream_t)stream));
+}
+
+int bmx_rotary(const void* x, int type, int64_t x_row, int64_t x_head, int heads, int dim, int64_t rows, const int32_t* positions,
+               const double* freq, int rot, int interleaved, float factor, int inverse, void* out, int64_t out_row, int64_t out_head,
+               void* stream) {
+  if (heads <= 0 || heads > 65535 || dim <= 0 || dim > 256 || rot <= 0 || rot > dim || rot % 2 || rows < 0 || rows > (1 << 23)) return BMX_ERR_SHAPE;
+  if (!is_type(type)) return BMX_ERR_UNSUPPORTED;
+  if (rows == 0) return BMX_OK;
+  if (!positions || !freq) return BMX_ERR_NULL;
+  int st;
+  if ((st = kv_rows_check(x, type, x_row, x_head, rows, heads, dim)) != BMX_OK) return st;
+  if ((st = kv_rows_check(out, type, out_row, out_head, rows, heads, dim)) != BMX_OK) return st;
+  if (x == out && ((rows > 1 && x_row != out_row) || (heads > 1 && x_head != out_head))) return BMX_ERR_LD;
+  if (misaligned(positions, 4) || misaligned(freq, 8)) return BMX_ERR_ALIGN;
+  return hip_status(bmx::launch_rotary(x, type, x_row, x_head, heads, dim, (int)rows, positions, freq, rot, interleaved != 0, factor, inverse != 0, out,
+                                       out_row, out_head, (hipStream_t)stream));
+}
+
+int bmx_kv4_write(const bmx_kv4_cache* cache, const void* k, const void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row,
+                  int64_t v_head, int64_t rows, int max_new, void* stream) {
+  int st = kv_check(cache, type, rows, &max_new);
+  if (st != BMX_OK || rows == 0) return st;
+  if ((st = kv_rows_check(k, type, k_row, k_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
+  if ((st = kv_rows_check(v, type, v_row, v_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
+  return hip_status(bmx::launch_kv4_write(*cache, k, v, type, k_row, k_head, v_row, v_head, (int)rows, max_new, (hipStream_t)stream));
+}
+
+int bmx_kv4_read(const bmx_kv4_cache* cache, void* k, void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head,
+                 int64_t rows, int max_new, void* stream) {
+  int st = kv_check(cache, type, rows, &max_new);
+  if (st != BMX_OK || rows == 0) return st;
+  if ((st = kv_rows_check(k, type, k_row, k_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
+  if ((st = kv_rows_check(v, type, v_row, v_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
+  return hip_status(bmx::launch_kv4_read(*cache, k, v, type, k_row, k_head, v_row, v_head, (int)rows, max_new, (hipStream_t)stream));
+}
+
+int bmx_kv4_attention(const bmx_kv4_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
+                      int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+  return kv_attention(cache, q, type, q_row, q_head, q_heads, rows, max_new, scale, causal, window, out, out_row, out_head, lse,
+                      workspace, workspace_bytes, stream, false);
+}
+
+int bmx_fresh_kv4_attention(const bmx_kv4_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
+                            int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                            void* workspace, size_t workspace_bytes, void* stream) {
   return kv_attention(cache, q, type, q_row, q_head, q_heads, rows, max_new, scale, causal, window, out, out_row, out_head, lse,
                       workspace, workspace_bytes, stream, true);
 }

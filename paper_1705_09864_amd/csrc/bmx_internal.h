@@ -264,6 +264,21 @@ hipError_t launch_kv_attention(const bmx_kv_cache& c, const void* q, int type, i
 // What any call of at most max_new new rows a sequence (0: any) needs, and what one of exactly so many does.
 size_t kv_attention_workspace(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new);
 size_t kv_attention_workspace_of_call(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new);
+// kv_pages.hip: which pages are whose.  rotary.hip: heads rotated by position.
+hipError_t launch_kv_resize(const int32_t* change, int sequences, int32_t* table, int64_t table_ld, int table_width, int32_t* lengths, int32_t* pool,
+                            int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int rows, hipStream_t s);
+hipError_t launch_rotary(const void* x, int type, int64_t x_row, int64_t x_head, int heads, int dim, int rows, const int32_t* positions, const double* freq,
+                         int rot, bool interleaved, float factor, bool inverse, void* out, int64_t out_row, int64_t out_head, hipStream_t s);
+// kv4_cache.hip, kv4_attention.hip: the cache of 4 bits and the attention over it, as those of 8.
+hipError_t launch_kv4_write(const bmx_kv4_cache& c, const void* k, const void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row,
+                            int64_t v_head, int rows, int max_new, hipStream_t s);
+hipError_t launch_kv4_read(const bmx_kv4_cache& c, void* k, void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head,
+                           int rows, int max_new, hipStream_t s);
+hipError_t launch_kv4_attention(const bmx_kv4_cache& c, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int rows,
+                                int max_new, float scale, bool causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                                void* workspace, bool fresh, hipStream_t s);
+size_t kv4_attention_workspace(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new);
+size_t kv4_attention_workspace_of_call(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new);
 
 // The same convolution on the GEMM kernel (filters = A rows streamed through SGPRs, im2col
 // rows gathered per chunk): for K that does not fit the stationary kernel or grids with too

@@ -61,13 +61,74 @@ __device__ static inline void load_eight(const void* p, int64_t at, int left, bo
   }
 }
 
-// A sequence's rows and positions (lengths and starts come from device memory).
-__device__ static inline KvSpan kv_span(const bmx_kv_cache& c, int seq, int rows, int max_new) {
+// N consecutive values, as they lie in memory at an address of an element.
+template <int TYPE, int N>
+struct Run {
+  static constexpr int kDwords = N * (TYPE == BMX_F32 ? 4 : 2) / 4;
+  struct __attribute__((packed, aligned(TYPE == BMX_F32 ? 4 : 2))) Raw {
+    uint32_t w[kDwords];
+  };
+  uint32_t w[kDwords];
+
+  __device__ static size_t bytes(int64_t at) { return at * (TYPE == BMX_F32 ? 4 : 2); }
+  // `left` of them are there, the others are 0
+  __device__ void load(const void* p, int64_t at, int left) {
+    if (left >= N) {
+      const Raw r = *reinterpret_cast<const Raw*>(static_cast<const char*>(p) + bytes(at));
+#pragma unroll
+      for (int i = 0; i < kDwords; ++i) w[i] = r.w[i];
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if constexpr (TYPE == BMX_F32) {
+          w[j] = j < left ? static_cast<const uint32_t*>(p)[at + j] : 0;
+        } else {
+          const uint32_t h = j < left ? static_cast<const uint16_t*>(p)[at + j] : 0;
+          w[j / 2] = j % 2 ? w[j / 2] | h << 16 : h;
+        }
+      }
+    }
+  }
+  __device__ void store(void* p, int64_t at, int left) const {
+    if (left >= N) {
+      Raw r;
+#pragma unroll
+      for (int i = 0; i < kDwords; ++i) r.w[i] = w[i];
+      *reinterpret_cast<Raw*>(static_cast<char*>(p) + bytes(at)) = r;
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if (j >= left) continue;
+        if constexpr (TYPE == BMX_F32) static_cast<uint32_t*>(p)[at + j] = w[j];
+        else static_cast<uint16_t*>(p)[at + j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
+      }
+    }
+  }
+  __device__ float get(int j) const {
+    if constexpr (TYPE == BMX_F32) {
+      const uint32_t x = w[j];
+      return __builtin_bit_cast(float, x);
+    } else {
+      const uint32_t h = w[j / 2] >> (16 * (j % 2)) & 0xffff;
+      return TYPE == BMX_F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)h) : bf16_float(h);
+    }
+  }
+  __device__ void set2(int j, float a, float b) {  // values j (even) and j + 1
+    if constexpr (TYPE == BMX_F32) w[j] = __builtin_bit_cast(uint32_t, a), w[j + 1] = __builtin_bit_cast(uint32_t, b);
+    else if constexpr (TYPE == BMX_F16) w[j / 2] = f16_bits(a) | f16_bits(b) << 16;
+    else w[j / 2] = bf16_bits(a) | bf16_bits(b) << 16;
+  }
+};
+
+// A sequence's rows and positions (lengths and starts come from device memory); Cache: bmx_kv_cache or bmx_kv4_cache.
+template <class Cache>
+__device__ static inline KvSpan kv_span(const Cache& c, int seq, int rows, int max_new) {
   const int each = c.starts ? 0 : rows / c.sequences, begin = c.starts ? c.starts[seq] : seq * each, end = c.starts ? c.starts[seq + 1] : begin + each;
   return kv_span_of(begin, end, c.lengths[seq], rows, max_new, c.table_width);
 }
 // The page at place `at` of a sequence's row of the table; negative where there is none.
-__device__ static inline int kv_page(const bmx_kv_cache& c, int seq, int at) {
+template <class Cache>
+__device__ static inline int kv_page(const Cache& c, int seq, int at) {
   const int p = c.table[seq * c.table_ld + at];
   return p < c.num_pages ? p : -1;
 }
@@ -78,6 +139,10 @@ __device__ static inline int kv_key_at(int row, int t, int d) {
   return d / 64 * 64 + 64 <= row ? base + d % 64 / 16 * 256 + t % 16 * 16 + d % 16 : base + d % 32 / 8 * 128 + t % 16 * 8 + d % 8;
 }
 __device__ static inline int kv_value_at(int t, int d) { return d / 16 * 1024 + t % 16 / 4 * 256 + d % 16 * 16 + t / 16 * 4 + t % 4; }
+// Bytes that a token's head takes in a page of 4 bits, and where its value d lies there: the low half of a byte if d is even.
+__host__ __device__ static inline int kv4_row_bytes(int dim) { return (dim + 31) / 32 * 16; }
+__device__ static inline int kv4_key_at(int row, int t, int d) { return t * row + d / 2; }
+__device__ static inline int kv4_value_at(int t, int d) { return d / 32 * 1024 + t % 16 / 4 * 256 + d % 32 / 2 * 16 + t / 16 * 4 + t % 4; }
 
 // Memory as a buffer of so many bytes.  A read whose lane_at is behind its end gives zeros and moves nothing; what the hardware compares with the end
 // need not hold `at`, so lane_at alone says whether there is anything to read (kNowhere added: there is not).

@@ -35,6 +35,12 @@
 #pragma weak bmx_kv_read
 #pragma weak bmx_kv_attention
 #pragma weak bmx_fresh_kv_attention
+#pragma weak bmx_kv_resize
+#pragma weak bmx_rotary
+#pragma weak bmx_kv4_write
+#pragma weak bmx_kv4_read
+#pragma weak bmx_kv4_attention
+#pragma weak bmx_fresh_kv4_attention
 
 namespace {
 
@@ -556,28 +562,50 @@ bmx_kv_cache cache_of(PyObject* p, PyObject* s, PyObject* t, PyObject* n, PyObje
           as_int(seqs), as_int(table->size(1)), as_int(pages->size(0)), as_int(pages->size(1)), as_int(dim), (int)(64 / blocks)};
 }
 
-FUNCTION(kv_write, 9) {  // k, v, pages, scales, table, lengths, starts, max_new, stream
+// The same of a cache of 4 bits.
+bmx_kv4_cache cache4_of(PyObject* p, PyObject* s, PyObject* t, PyObject* n, PyObject* at_, int64_t dim) {
+  T pages = required(p, at::kByte, 4, "cache pages", true), scales = required(s, at::kBFloat16, 5, "cache scales", true);
+  T table = required(t, kI32, 2, "cache table"), lengths = required(n, kI32, 1, "cache lengths", true);
+  T starts = tensor(at_, kI32, "cache starts", true);
+  const int64_t seqs = lengths->size(0);
+  if (dim <= 0 || dim > 256) check_status(BMX_ERR_SHAPE, "cache");
+  shape(pages, {pages->size(0), pages->size(1), 2, 64 * ((dim + 31) / 32 * 16)}, "cache pages");
+  shape(scales, {pages->size(0), pages->size(1), 2, 64, 2}, "cache scales");
+  shape(table, {seqs, table->size(1)}, "cache table");
+  if (starts) shape(starts, {seqs + 1}, "cache starts");
+  return {ptr<uint8_t>(pages), ptr<uint16_t>(scales), ptr<int32_t>(table), ld(table), ptr<int32_t>(lengths), ptr<int32_t>(starts),
+          as_int(seqs), as_int(table->size(1)), as_int(pages->size(0)), as_int(pages->size(1)), as_int(dim)};
+}
+
+// The calls on either cache; of: what makes its description, name: the call's.
+template <class Of, class F>
+PyObject* write_rows(Args a, Of of, F f, const char* name) {
   T k = values(a[0], 3, "kv_write k");
   const at::ScalarType type = k->scalar_type();
   T v = values(a[1], 3, "kv_write v", &type);
-  const bmx_kv_cache c = cache_of(a[2], a[3], a[4], a[5], a[6], k->size(2));
+  const auto c = of(a[2], a[3], a[4], a[5], a[6], k->size(2));
   shape(k, {k->size(0), c.heads, c.dim}, "kv_write k");
   shape(v, {k->size(0), c.heads, c.dim}, "kv_write v");
   const int max_new = small(a[7]);
   const hipStream_t s = stream_of(a[8]);
-  call("bmx_kv_write", bmx_kv_write, &c, k->data_ptr(), v->data_ptr(), type_of(type), k->stride(0), k->stride(1), v->stride(0),
-       v->stride(1), k->size(0), max_new, s);
+  call(name, f, &c, k->data_ptr(), v->data_ptr(), type_of(type), k->stride(0), k->stride(1), v->stride(0), v->stride(1), k->size(0), max_new, s);
   Py_RETURN_NONE;
 }
 
+FUNCTION(kv_write, 9) {  // k, v, pages, scales, table, lengths, starts, max_new, stream
+  return write_rows(a, cache_of, bmx_kv_write, "bmx_kv_write");
+}
+FUNCTION(kv4_write, 9) { return write_rows(a, cache4_of, bmx_kv4_write, "bmx_kv4_write"); }
+
 // pages, scales, table, lengths, dim, dtype, rows, starts, max_new, out_k, out_v, stream -> (k, v)
-FUNCTION(kv_read, 12) {
-  const bmx_kv_cache c = cache_of(a[0], a[1], a[2], a[3], a[7], integer(a[4]));
+template <class Of, class F>
+PyObject* read_rows(Args a, Of of, F f, const char* name) {
+  const auto c = of(a[0], a[1], a[2], a[3], a[7], integer(a[4]));
   if (!THPDtype_Check(a[5])) raise_value("%s: expected a torch.dtype, got %s", "kv_read dtype", Py_TYPE(a[5])->tp_name);
   const at::ScalarType type = reinterpret_cast<THPDtype*>(a[5])->scalar_type;
   if (type_of(type) < 0) raise_value("%s: %s, expected Float, Half or BFloat16", "kv_read dtype", c10::toString(type));
   const int64_t rows = integer(a[6]);
-  if (rows < 0) check_status(BMX_ERR_SHAPE, "bmx_kv_read");
+  if (rows < 0) check_status(BMX_ERR_SHAPE, name);
   T pages = &THPVariable_Unpack(a[0]), k, v;
   std::optional<Out> ok, ov;
   if (a[9] == Py_None) k = ok.emplace(Py_None, type, at::IntArrayRef({rows, c.heads, c.dim}), pages, "").t;
@@ -588,7 +616,7 @@ FUNCTION(kv_read, 12) {
   shape(v, {rows, c.heads, c.dim}, "kv_read out_v");
   const int max_new = small(a[8]);
   const hipStream_t s = stream_of(a[11]);
-  call("bmx_kv_read", bmx_kv_read, &c, k->data_ptr(), v->data_ptr(), type_of(type), k->stride(0), k->stride(1), v->stride(0), v->stride(1),
+  call(name, f, &c, k->data_ptr(), v->data_ptr(), type_of(type), k->stride(0), k->stride(1), v->stride(0), v->stride(1),
        rows, max_new, s);
   PyObject* r = PyTuple_New(2);
   if (!r) throw python_error();
@@ -600,12 +628,15 @@ FUNCTION(kv_read, 12) {
   }
   return r;
 }
+FUNCTION(kv_read, 12) { return read_rows(a, cache_of, bmx_kv_read, "bmx_kv_read"); }
+FUNCTION(kv4_read, 12) { return read_rows(a, cache4_of, bmx_kv4_read, "bmx_kv4_read"); }
 
 // q, pages, scales, table, lengths, starts, max_new, scale, causal, window, lse, out, workspace, stream -> out or (out, lse)
-FUNCTION(kv_attention, 14) {
+template <class Of, class F>
+PyObject* attention(Args a, Of of, F f, F f_fresh, int op, const char* name) {
   T q = values(a[0], 3, "kv_attention q");
   const at::ScalarType type = q->scalar_type();
-  const bmx_kv_cache c = cache_of(a[1], a[2], a[3], a[4], a[5], q->size(2));
+  const auto c = of(a[1], a[2], a[3], a[4], a[5], q->size(2));
   const int64_t rows = q->size(0);
   const int heads = as_int(q->size(1)), window = small(a[9]);
   int max_new = small(a[6]);
@@ -621,14 +652,80 @@ FUNCTION(kv_attention, 14) {
   const int64_t most = c.starts ? max_new ? std::min<int64_t>(max_new, rows) : rows : rows / std::max(c.sequences, 1);
   Workspace ws;
   const bool fresh = !ws.given(a[12]);
-  if (fresh) ws.allocate(BMX_OP_KV_ATTENTION, {c.sequences, c.table_width, c.heads, heads, c.dim, most, rows}, q, s);
-  call("bmx_kv_attention", fresh ? bmx_fresh_kv_attention : bmx_kv_attention, &c, q->data_ptr(), type_of(type), q->stride(0),
+  if (fresh) ws.allocate(op, {c.sequences, c.table_width, c.heads, heads, c.dim, most, rows}, q, s);
+  call(name, fresh ? f_fresh : f, &c, q->data_ptr(), type_of(type), q->stride(0),
        q->stride(1), heads, rows, max_new, (float)scale, (int)truth(a[8]), window, out->data_ptr(), out->stride(0), out->stride(1),
        lse ? ptr<float>(lse->t) : nullptr, ws.p, ws.bytes, s);
   PyObject* o;
   if (made) o = made->result();
   else Py_INCREF(o = a[11]);
   return lse ? Py_BuildValue("NN", o, lse->result()) : o;
+}
+FUNCTION(kv_attention, 14) { return attention(a, cache_of, bmx_kv_attention, bmx_fresh_kv_attention, BMX_OP_KV_ATTENTION, "bmx_kv_attention"); }
+FUNCTION(kv4_attention, 14) {
+  return attention(a, cache4_of, bmx_kv4_attention, bmx_fresh_kv4_attention, BMX_OP_KV4_ATTENTION, "bmx_kv4_attention");
+}
+
+// A vector of so many numbers: the caller's, or a new one.
+struct Numbers {
+  std::optional<Out> made;
+  T t = nullptr;
+  PyObject* given = nullptr;
+  Numbers(PyObject* o, at::ScalarType type, int64_t n, T like, const char* what) {
+    if (o == Py_None) {
+      t = made.emplace(Py_None, type, at::IntArrayRef({n}), like, "").t;
+    } else {
+      t = required(o, type, 1, what, true);
+      shape(t, {n}, what);
+      Py_INCREF(given = o);
+    }
+  }
+  ~Numbers() { Py_XDECREF(given); }
+  PyObject* result() {
+    if (made) return made->result();
+    PyObject* o = given;
+    given = nullptr;
+    return o;
+  }
+};
+
+// change, table, lengths, pool, rows, starts, positions, slots, stream -> (starts, positions, slots)
+FUNCTION(kv_resize, 9) {
+  T change = required(a[0], kI32, 1, "kv_resize change", true), table = required(a[1], kI32, 2, "kv_resize table");
+  T lengths = required(a[2], kI32, 1, "kv_resize lengths", true), pool = required(a[3], kI32, 1, "kv_resize pool", true);
+  const int64_t seqs = lengths->size(0), rows = integer(a[4]);
+  shape(change, {seqs}, "kv_resize change");
+  shape(table, {seqs, table->size(1)}, "kv_resize table");
+  if (pool->size(0) < 2) raise_value("%s: expected 2 numbers and one for each page, got %s", "kv_resize pool", std::to_string(pool->size(0)).c_str());
+  if (rows < 0) check_status(BMX_ERR_SHAPE, "bmx_kv_resize");
+  Numbers starts(a[5], kI32, seqs + 1, lengths, "kv_resize starts"), positions(a[6], kI32, rows, lengths, "kv_resize positions");
+  Numbers slots(a[7], at::kLong, rows, lengths, "kv_resize slots");
+  const hipStream_t s = stream_of(a[8]);
+  call("bmx_kv_resize", bmx_kv_resize, ptr<int32_t>(change), as_int(seqs), ptr<int32_t>(table), ld(table), as_int(table->size(1)), ptr<int32_t>(lengths),
+       ptr<int32_t>(pool), as_int(pool->size(0) - 2), ptr<int32_t>(starts.t), ptr<int32_t>(positions.t), ptr<int64_t>(slots.t), rows, s);
+  return Py_BuildValue("NNN", starts.result(), positions.result(), slots.result());
+}
+
+// x, positions, freq, interleaved, factor, inverse, out, stream -> out
+FUNCTION(rotary, 8) {
+  T x = values(a[0], 3, "rotary x");
+  const at::ScalarType type = x->scalar_type();
+  T positions = required(a[1], kI32, 1, "rotary positions", true), freq = required(a[2], at::kDouble, 1, "rotary freq", true);
+  shape(positions, {x->size(0)}, "rotary positions");
+  const double factor = PyFloat_AsDouble(a[4]);
+  if (factor == -1.0 && PyErr_Occurred()) throw python_error();
+  std::optional<Out> made;
+  T out;
+  if (a[6] == Py_None) out = made.emplace(Py_None, type, x->sizes(), x, "").t;
+  else out = values(a[6], 3, "rotary out", &type);
+  shape(out, x->sizes(), "rotary out");
+  const hipStream_t s = stream_of(a[7]);
+  call("bmx_rotary", bmx_rotary, x->data_ptr(), type_of(type), x->stride(0), x->stride(1), as_int(x->size(1)), as_int(x->size(2)), x->size(0),
+       ptr<int32_t>(positions), ptr<double>(freq), as_int(2 * freq->size(0)), (int)truth(a[3]), (float)factor, (int)truth(a[5]), out->data_ptr(),
+       out->stride(0), out->stride(1), s);
+  if (made) return made->result();
+  Py_INCREF(a[6]);
+  return a[6];
 }
 
 PyObject* set_error(PyObject*, PyObject* cls) {
@@ -644,7 +741,7 @@ PyMethodDef methods[] = {ENTRY(binarize_pack), ENTRY(unpack_pm1), ENTRY(xnor_gem
                          ENTRY(pack_conv_weights), ENTRY(binary_conv2d), ENTRY(pack_nchw), ENTRY(binary_conv2d_packed),
                          ENTRY(binary_conv2d_bits), ENTRY(quant_gemm), ENTRY(alpha_mean_abs),
                          ENTRY(w4_quantize), ENTRY(w4_dequantize), ENTRY(w4_fc), ENTRY(kv_write), ENTRY(kv_read),
-                         ENTRY(kv_attention),
+                         ENTRY(kv_attention), ENTRY(kv_resize), ENTRY(rotary), ENTRY(kv4_write), ENTRY(kv4_read), ENTRY(kv4_attention),
                          {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bmx_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

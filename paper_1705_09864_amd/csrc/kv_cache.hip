@@ -16,65 +16,6 @@
 namespace bmx {
 namespace {
 
-// N consecutive values, as they lie in memory at an address of an element.
-template <int TYPE, int N>
-struct Run {
-  static constexpr int kDwords = N * (TYPE == BMX_F32 ? 4 : 2) / 4;
-  struct __attribute__((packed, aligned(TYPE == BMX_F32 ? 4 : 2))) Raw {
-    uint32_t w[kDwords];
-  };
-  uint32_t w[kDwords];
-
-  __device__ static size_t bytes(int64_t at) { return at * (TYPE == BMX_F32 ? 4 : 2); }
-  // `left` of them are there, the others are 0
-  __device__ void load(const void* p, int64_t at, int left) {
-    if (left >= N) {
-      const Raw r = *reinterpret_cast<const Raw*>(static_cast<const char*>(p) + bytes(at));
-#pragma unroll
-      for (int i = 0; i < kDwords; ++i) w[i] = r.w[i];
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if constexpr (TYPE == BMX_F32) {
-          w[j] = j < left ? static_cast<const uint32_t*>(p)[at + j] : 0;
-        } else {
-          const uint32_t h = j < left ? static_cast<const uint16_t*>(p)[at + j] : 0;
-          w[j / 2] = j % 2 ? w[j / 2] | h << 16 : h;
-        }
-      }
-    }
-  }
-  __device__ void store(void* p, int64_t at, int left) const {
-    if (left >= N) {
-      Raw r;
-#pragma unroll
-      for (int i = 0; i < kDwords; ++i) r.w[i] = w[i];
-      *reinterpret_cast<Raw*>(static_cast<char*>(p) + bytes(at)) = r;
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if (j >= left) continue;
-        if constexpr (TYPE == BMX_F32) static_cast<uint32_t*>(p)[at + j] = w[j];
-        else static_cast<uint16_t*>(p)[at + j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
-      }
-    }
-  }
-  __device__ float get(int j) const {
-    if constexpr (TYPE == BMX_F32) {
-      const uint32_t x = w[j];
-      return __builtin_bit_cast(float, x);
-    } else {
-      const uint32_t h = w[j / 2] >> (16 * (j % 2)) & 0xffff;
-      return TYPE == BMX_F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)h) : bf16_float(h);
-    }
-  }
-  __device__ void set2(int j, float a, float b) {  // values j (even) and j + 1
-    if constexpr (TYPE == BMX_F32) w[j] = __builtin_bit_cast(uint32_t, a), w[j + 1] = __builtin_bit_cast(uint32_t, b);
-    else if constexpr (TYPE == BMX_F16) w[j / 2] = f16_bits(a) | f16_bits(b) << 16;
-    else w[j / 2] = bf16_bits(a) | bf16_bits(b) << 16;
-  }
-};
-
 __device__ inline float finite(float a) { return a < INFINITY ? a : 0.0f; }  // of a size: neither infinite nor NaN
 
 // (the instruction itself: in C++ the conversion of a NaN or of too large a number has no result)

@@ -42,4 +42,20 @@ __host__ __device__ static inline int64_t kv_pages_of(int max_new) { return ((in
 __host__ __device__ static inline int kv_pages_to(int end) { return end > 0 ? (end - 1) / kPage + 1 : 0; }
 __host__ __device__ static inline bool kv_all_in(int t0, int n, int low, int high) { return t0 >= low && high >= n && t0 <= high - n; }
 
+// A sequence of `tokens` tokens that is to have `change` more (or fewer): its pages now and then, and the rows that are new.  fits: neither number of
+// tokens is below 0 or more than the table has room for.
+struct KvChange {
+  bool fits;
+  int pages, pages_then, tokens_then, more;
+};
+__host__ __device__ static inline KvChange kv_change_of(int tokens, int change, int table_width) {
+  KvChange c = {};
+  const int64_t then = (int64_t)tokens + change, most = (int64_t)table_width * kPage;
+  c.fits = tokens >= 0 && tokens <= most && then >= 0 && then <= most && then <= 0x7fffffff;
+  if (!c.fits) return c;
+  c.pages = kv_pages_to(tokens), c.pages_then = kv_pages_to((int)then), c.tokens_then = (int)then;
+  c.more = change > 0 ? change : 0;
+  return c;
+}
+
 }  // namespace bmx

@@ -27,4 +27,8 @@ int bmx_lazy_quant_gemm(const float* a, int64_t lda, int bits_a, const float* w,
 int bmx_fresh_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
                            int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
                            void* workspace, size_t workspace_bytes, void* stream);
+// The same over the cache of 4 bits.
+int bmx_fresh_kv4_attention(const bmx_kv4_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
+                            int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
+                            void* workspace, size_t workspace_bytes, void* stream);
 }

@@ -1,0 +1,156 @@
+// Heads rotated by their tokens' positions: values a and b of a pair j of a token at position p become
+//   a' = f (a cos t - b sin t), b' = f (b cos t + a sin t),  t = p freq_j,
+// pairs of neighbours, or of a value and the one half of the rotated part behind it.
+// The angle is taken in 64 bits as a part of a turn, p (freq_j / 2 pi) less the nearest whole number: in 32 bits a position of 10^6 would leave 4
+// digits of it.  What is left is at most half a turn, exact enough in 32 bits, and goes by quarters to |t| <= pi / 4, where the series of sine and cosine end
+// below fp32's last bit with a^9 and a^10.
+//
+// Bound by the heads' bytes, in and out once.  A workgroup takes ROWS tokens: a thread makes an angle's sine and cosine, which all heads of the token
+// share, into LDS, while its first values are on their way; then 16 bytes of each side of the pairs a step.
+#include "bmx_internal.h"
+#include "few_bits.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace bmx {
+namespace {
+
+struct Args {
+  const void* x;
+  int64_t x_row, x_head;
+  void* out;
+  int64_t out_row, out_head;
+  const int32_t* positions;
+  const double* freq;
+  int heads, dim, half;  // half: pairs
+  int rows;
+  float cos_by, sin_by;
+  bool copy;  // values behind the rotated part go to another place
+};
+
+// Sine and cosine of t turns, |t| <= 1/2.
+__device__ inline void turn(float t, float* s, float* c) {
+  const float n = rintf(4.0f * t), a = (t - 0.25f * n) * 6.2831853071795865f, b = a * a;
+  const float si = a + a * b * (-1.0f / 6 + b * (1.0f / 120 + b * (-1.0f / 5040 + b * (1.0f / 362880))));
+  const float co = 1.0f + b * (-0.5f + b * (1.0f / 24 + b * (-1.0f / 720 + b * (1.0f / 40320 + b * (-1.0f / 3628800)))));
+  const int q = (int)n;  // -2 to 2
+  const float u = q & 1 ? co : si, v = q & 1 ? si : co;
+  *s = q & 2 ? -u : u;
+  *c = (q + 1) & 2 ? -v : v;
+}
+
+// A value, as Run has several.
+template <int TYPE>
+struct Single {
+  float v;
+  __device__ void load(const void* p, int64_t at, int) { v = load_one<TYPE>(p, at); }
+  __device__ float get(int) const { return v; }
+};
+
+// PAIR: neighbours.  N: values of a step on each side (halves) or in all (neighbours); rows and heads lie so that N of them are one access where N > 2.
+template <int TYPE, bool PAIR, int N>
+__global__ __launch_bounds__(256) void rotary_kernel(Args a, int rows_each, int head_groups) {
+  constexpr int PAIRS = PAIR ? N / 2 : N;
+  extern __shared__ float2 table[];  // [row][pair]
+  const int row0 = blockIdx.x / head_groups * rows_each, rows = min(rows_each, a.rows - row0), group = blockIdx.x % head_groups;
+  const int head0 = (int)((int64_t)group * a.heads / head_groups), heads = (int)((int64_t)(group + 1) * a.heads / head_groups) - head0;
+  const int steps = a.half / PAIRS, items = rows * heads * steps;
+  using V = std::conditional_t<N == 1, Single<TYPE>, Run<TYPE, N == 1 ? 2 : N>>;
+  const auto place = [&](int e, int* row, int* j, int* head) {
+    *j = e % steps * PAIRS;
+    *head = e / steps % heads + head0;
+    *row = e / steps / heads;
+  };
+  const auto load = [&](int e, V* u, V* w) {
+    int row, j, head;
+    place(e, &row, &j, &head);
+    const int64_t at = (int64_t)(row0 + row) * a.x_row + head * a.x_head + (PAIR ? 2 * j : j);
+    u->load(a.x, at, N);
+    if constexpr (!PAIR) w->load(a.x, at + a.half, N);
+  };
+  V u, w;
+  if ((int)threadIdx.x < items) load(threadIdx.x, &u, &w);
+  for (int e = threadIdx.x; e < rows * a.half; e += 256) {
+    const double t = (double)a.positions[row0 + e / a.half] * (a.freq[e % a.half] * 0.15915494309189533577);
+    float s, c;
+    turn((float)(t - rint(t)), &s, &c);
+    table[e] = float2{c * a.cos_by, s * a.sin_by};
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < items; e += 256) {
+    if (e != (int)threadIdx.x) load(e, &u, &w);
+    int row, j, head;
+    place(e, &row, &j, &head);
+    const int64_t at = (int64_t)(row0 + row) * a.out_row + head * a.out_head + (PAIR ? 2 * j : j);
+    const float2* f = table + row * a.half + j;
+    [[maybe_unused]] V p, q;
+    if constexpr (PAIR) {
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        const float x = u.get(i), y = u.get(i + 1);
+        p.set2(i, x * f[i / 2].x - y * f[i / 2].y, y * f[i / 2].x + x * f[i / 2].y);
+      }
+      p.store(a.out, at, N);
+    } else if constexpr (N == 1) {
+      const float x = u.get(0), y = w.get(0);
+      store_one<TYPE>(a.out, at, x * f[0].x - y * f[0].y);
+      store_one<TYPE>(a.out, at + a.half, y * f[0].x + x * f[0].y);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        const float x0 = u.get(i), y0 = w.get(i), x1 = u.get(i + 1), y1 = w.get(i + 1);
+        p.set2(i, x0 * f[i].x - y0 * f[i].y, x1 * f[i + 1].x - y1 * f[i + 1].y);
+        q.set2(i, y0 * f[i].x + x0 * f[i].y, y1 * f[i + 1].x + x1 * f[i + 1].y);
+      }
+      p.store(a.out, at, N);
+      q.store(a.out, at + a.half, N);
+    }
+  }
+  if (a.copy) {
+    constexpr int M = N > 2 ? N : 1;
+    const int from = 2 * a.half, each = (a.dim - from) / M;
+    for (int e = threadIdx.x; e < rows * heads * each; e += 256) {
+      const int row = row0 + e / each / heads, head = head0 + e / each % heads, d = from + e % each * M;
+      if constexpr (M == 1) {
+        store_one<TYPE>(a.out, row * a.out_row + head * a.out_head + d, load_one<TYPE>(a.x, row * a.x_row + head * a.x_head + d));
+      } else {
+        Run<TYPE, M> v;
+        v.load(a.x, row * a.x_row + head * a.x_head + d, M);
+        v.store(a.out, row * a.out_row + head * a.out_head + d, M);
+      }
+    }
+  }
+}
+
+template <int TYPE, bool PAIR>
+void launch(const Args& a, hipStream_t s) {
+  constexpr int SIZE = TYPE == BMX_F32 ? 4 : 2, WIDE = 16 / SIZE, NARROW = PAIR ? 2 : 1;
+  const auto whole = [](int64_t n) { return n % WIDE == 0; };
+  const bool wide = (PAIR ? whole(2 * a.half) : whole(a.half)) && (!a.copy || whole(a.dim - 2 * a.half));
+  const int n = wide ? WIDE : NARROW, pairs = PAIR ? n / 2 : n;
+  const int64_t per_row = (int64_t)a.heads * (a.half / pairs);
+  // rows of a workgroup: four steps a thread, as long as the chip is filled; heads of few rows are dealt out to several workgroups
+  int64_t rows_each = std::max<int64_t>(std::min<int64_t>({4 * 256 / per_row, a.rows / 1024, 4096 / a.half, 64}), 1);
+  int64_t groups = std::max<int64_t>(std::min<int64_t>({(per_row + 255) / 256, a.heads, (1024 + a.rows - 1) / a.rows}), 1);
+  if (rows_each > 1) groups = 1;
+  const dim3 grid((uint32_t)(ceil_div(a.rows, rows_each) * groups));
+  const auto kern = wide ? rotary_kernel<TYPE, PAIR, WIDE> : rotary_kernel<TYPE, PAIR, NARROW>;
+  launch_kernel(kern, grid, dim3(256), rows_each * a.half * sizeof(float2), s, a, (int)rows_each, (int)groups);
+  note_kernel("rotary_kernel<%d,%d,%d> grid %u block 256", TYPE, PAIR, n, grid.x);
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const void* x, int type, int64_t x_row, int64_t x_head, int heads, int dim, int rows, const int32_t* positions, const double* freq,
+                         int rot, bool interleaved, float factor, bool inverse, void* out, int64_t out_row, int64_t out_head, hipStream_t s) {
+  const Args a = {x, x_row, x_head, out, out_row, out_head, positions, freq, heads, dim, rot / 2, rows, factor, inverse ? -factor : factor,
+                  out != x && rot < dim};
+  const auto f = type == BMX_F32 ? (interleaved ? launch<BMX_F32, true> : launch<BMX_F32, false>)
+               : type == BMX_F16 ? (interleaved ? launch<BMX_F16, true> : launch<BMX_F16, false>)
+                                 : (interleaved ? launch<BMX_BF16, true> : launch<BMX_BF16, false>);
+  f(a, s);
+  return launch_error();
+}
+
+}  // namespace bmx

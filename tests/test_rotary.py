@@ -1,0 +1,168 @@
+"""Heads rotated by position against the definition in 64 bits, each pair as a complex number."""
+import numpy as np
+import pytest
+import torch
+
+from paper_1705_09864_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+
+
+def turned(x, positions, freq, interleaved, factor, inverse):
+    x, rot = x.double().cpu().numpy(), 2 * freq.numel()
+    angle = positions.cpu().numpy().astype(np.float64)[:, None] * freq.cpu().numpy()[None]
+    by = factor * np.exp((-1j if inverse else 1j) * angle)[:, None]
+    a, b = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    z = (x[..., a] + 1j * x[..., b]) * by
+    out = x.copy()
+    out[..., a], out[..., b] = z.real, z.imag
+    return torch.from_numpy(out)
+
+
+def check(got, x, positions, freq, interleaved=False, factor=1.0, inverse=False):
+    """A result is a sum of two products with a sine and a cosine that are each off by at most 4 * 2^-24 (the angle in fp32 2^-24 of at most half a turn brought to an
+    eighth, the series' steps, the factor), and has two roundings itself, all relative to the pair's size: 6 * 2^-24 of that times sqrt(2); then the
+    type's own rounding, and half of its smallest number."""
+    want = turned(x, positions, freq, interleaved, factor, inverse)
+    got, x = got.double().cpu(), x.double().cpu()
+    rot = 2 * freq.numel()
+    half = rot // 2
+    size = torch.zeros_like(x)
+    if interleaved:
+        size[..., :rot] = (x[..., 0:rot:2].square() + x[..., 1:rot:2].square()).sqrt().repeat_interleave(2, -1)
+    else:
+        size[..., :rot] = torch.cat(2 * [(x[..., :half].square() + x[..., half:rot].square()).sqrt()], -1)
+    return got, want, abs(factor) * size * 6 * 2.0**-24 * 2**0.5
+
+
+def agrees(got, *args, **named):
+    g, want, off = check(got, *args, **named)
+    info = torch.finfo(got.dtype)
+    off = off + (want.abs() + off) * info.eps / 2 * (got.dtype != torch.float32) + info.smallest_normal * info.eps
+    bad = (g - want).abs() > off
+    assert not bool(bad.any()), (float((g - want).abs().max()), bad.nonzero()[:3].tolist())
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rows,heads,dim,rot", [(1, 1, 2, 2), (5, 3, 64, 64), (7, 2, 80, 32), (3, 5, 96, 90), (2, 1, 7, 4), (33, 4, 128, 128), (1500, 2, 64, 64),
+                                                (4, 40, 128, 128), (2, 3, 256, 256), (9, 1, 33, 32), (3000, 1, 16, 6), (2, 72, 256, 200), (1, 1000, 4, 4), (1, 2, 255, 254)])
+def test_sizes(kind, interleaved, rows, heads, dim, rot):
+    g = torch.Generator(device="cuda").manual_seed(rows + dim)
+    x = torch.randn((rows, heads, dim), device="cuda", generator=g).to(kind)
+    positions = torch.randint(0, 5000, (rows,), device="cuda", generator=g, dtype=torch.int32)
+    freq = B.rotary_frequencies(rot)
+    agrees(B.rotary(x, positions, freq, interleaved), x, positions, freq, interleaved)
+    agrees(B.rotary(x, positions, freq, interleaved, 1.3, True), x, positions, freq, interleaved, 1.3, True)
+    before = x.clone()
+    assert B.rotary(x, positions, freq, interleaved, out=x) is x
+    agrees(x, before, positions, freq, interleaved)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,rot", [(128, 128), (80, 32), (66, 64), (32, 6)])
+def test_strides(kind, interleaved, dim, rot):
+    """Parts of a projection's rows, on odd elements, heads in any order and apart; what lies between is left as it was."""
+    g = torch.Generator(device="cuda").manual_seed(dim)
+    rows, heads = 11, 3
+    freq, positions = B.rotary_frequencies(rot), torch.arange(rows, dtype=torch.int32, device="cuda") * 7
+    for off, gap, turn in ((0, 0, False), (1, 5, False), (3, 0, True), (8, 8, True), (2, 6, False)):
+        def view(t):
+            v = t[off:off + rows * heads * (dim + gap)].view((heads, rows, dim + gap) if turn else (rows, heads, dim + gap))
+            return (v.transpose(0, 1) if turn else v)[..., :dim]
+        n = off + rows * heads * (dim + gap) + 9
+        base = torch.randn((n,), device="cuda", generator=g).to(kind)
+        dest = torch.full((n,), 5.0, device="cuda").to(kind)
+        x, out = view(base), view(dest)
+        keep = torch.ones((n,), dtype=torch.bool, device="cuda")
+        view(keep).fill_(False)
+        B.rotary(x, positions, freq, interleaved, out=out)
+        agrees(out, x, positions, freq, interleaved)
+        assert bool((dest[keep] == 5).all())
+        was = base.clone()
+        B.rotary(x, positions, freq, interleaved, out=x)
+        agrees(x, view(was), positions, freq, interleaved)
+        assert torch.equal(base[keep], was[keep])
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_far_positions(kind):
+    """As exact at the ends of 32 bits: the product of position and angle has 53 bits, so at 2^31 a pair of frequency 1 is off by 2^31 * 2^-52 radians, below fp32's."""
+    positions = torch.tensor([0, 1, -1, 131071, 10**6, -10**6, 2**31 - 1, -2**31], dtype=torch.int32, device="cuda")
+    x = torch.randn((8, 2, 64), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(kind)
+    freq = B.rotary_frequencies(64)
+    agrees(B.rotary(x, positions, freq), x, positions, freq)
+    freq = torch.linspace(0, 3.2, 32, dtype=torch.float64, device="cuda")
+    got, want, off = check(B.rotary(x, positions, freq), x, positions, freq)
+    assert bool(((got - want).abs() <= off + want.abs() * torch.finfo(kind).eps / 2 + 8 * 2.0**31 * 2.0**-52).all())
+
+
+def test_angles_of_every_part_of_a_turn():
+    """Quarters and eighths of a turn and what lies beside them."""
+    turns = torch.cat([torch.arange(-32, 33, dtype=torch.float64) / 16 + d for d in (0, 2.0**-26, -2.0**-26, 2.0**-60)])
+    freq = turns.cuda() * 2 * np.pi
+    x = torch.randn((3, 2, 2 * turns.numel() if 2 * turns.numel() <= 256 else 256), device="cuda")
+    for part in freq.split(128):
+        y = x[..., :2 * part.numel()].contiguous()
+        agrees(B.rotary(y, torch.tensor([1, -1, 3], dtype=torch.int32, device="cuda"), part), y, torch.tensor([1, -1, 3]), part)
+
+
+def test_inverse_is_the_gradients_way():
+    """<g, R x> = <R' g, x> for every g and x, and the difference quotient of <g, R x> along a direction: R is linear, so any step gives it.  fp32: a sum of n products
+    each off by at most 6 * 2^-24 * sqrt(2) of its pair's sizes (see check), summed in 64 bits."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows, heads, dim, rot = 6, 3, 40, 32
+    x, y, d = (torch.randn((rows, heads, dim), device="cuda", generator=g) for _ in range(3))
+    positions, freq = torch.arange(rows, dtype=torch.int32, device="cuda") * 100, B.rotary_frequencies(rot)
+    for interleaved in (False, True):
+        def f(x):
+            return float((y.double() * B.rotary(x, positions, freq, interleaved, 1.1).double()).sum())
+        grad = B.rotary(y, positions, freq, interleaved, 1.1, True).double()
+        bound = 2 * 1.1 * 9 * 2.0**-24 * float(y.double().norm()) * float(x.double().norm())
+        assert abs(f(x) - float((grad * x.double()).sum())) <= bound
+        both = x + 0.5 * d
+        slope = (f(both) - f(x)) / 0.5
+        step = float((grad * ((both - x).double() / 0.5)).sum())
+        assert abs(slope - step) <= 2 * (2 * 1.1 * 9 * 2.0**-24 * float(y.double().norm()) * float(both.double().norm())) / 0.5
+        # there and back is factor^2
+        back = B.rotary(B.rotary(x, positions, freq, interleaved, 1.1), positions, freq, interleaved, 1.1, True)
+        turned_part = torch.ones_like(x)
+        turned_part[..., :rot] *= 1.21
+        assert float((back - x * turned_part).abs().max()) <= 1.21 * 2 * 9 * 2.0**-24 * float(x.abs().max()) * 2**0.5
+
+
+def test_what_is_not_finite_stays_in_its_pair():
+    x = torch.ones((2, 2, 12), device="cuda")
+    x[0, 0, 3], x[1, 1, 0], x[0, 1, 11] = float("nan"), float("inf"), float("inf")
+    positions, freq = torch.tensor([5, 9], dtype=torch.int32, device="cuda"), B.rotary_frequencies(8)
+    out = B.rotary(x, positions, freq)
+    bad = ~torch.isfinite(out)
+    assert {tuple(t) for t in bad.nonzero().tolist()} == {(0, 0, 3), (0, 0, 7), (1, 1, 0), (1, 1, 4), (0, 1, 11)}
+    assert float(out[0, 1, 11]) == float("inf")
+
+
+def test_captured_and_replayed():
+    x = torch.randn((9, 4, 64), device="cuda")
+    positions, freq, out = torch.zeros((9,), dtype=torch.int32, device="cuda"), B.rotary_frequencies(64), torch.empty_like(x)
+    B.rotary(x, positions, freq, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.rotary(x, positions, freq, out=out)
+    for k in range(4):
+        positions.fill_(k * 1000)
+        x.normal_()
+        graph.replay()
+        agrees(out, x, positions, freq)
+
+
+def test_frequencies():
+    f = B.rotary_frequencies(8, 10000.0, device="cpu")
+    assert torch.allclose(f, torch.tensor([1, 0.1, 0.01, 0.001], dtype=torch.float64))
+    assert torch.allclose(B.rotary_frequencies(8, stretch=4, device="cpu"), f / 4)
+    # 0.01 turns 3.2 times over 2000, 0.001 a third of one, the others more than four times
+    part = B.rotary_frequencies(8, stretch=4, trained=2000, slow=1, fast=4, device="cpu")
+    keep = (0.01 * 2000 / (2 * np.pi) - 1) / 3
+    assert torch.allclose(part, torch.tensor([1, 0.1, 0.01 * keep + 0.0025 * (1 - keep), 0.00025], dtype=torch.float64))
