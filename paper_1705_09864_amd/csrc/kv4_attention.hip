@@ -24,6 +24,14 @@
 namespace bmx {
 namespace {
 
+using f32x16 = float __attribute__((ext_vector_type(16)));
+template <bool F16>
+__device__ inline f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
 __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
@@ -31,18 +39,20 @@ __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
 template <int TYPE>
 constexpr float kZero = TYPE == BMX_F32 ? 8.0f : -16.0f;
 // The bits of 16.0 in both halves, in a register: beside a literal v_and_or_b32 takes no other, and would fall into two instructions.
+template <int TYPE>
 __device__ inline uint32_t sixteen() {
-  uint32_t x = 0x41804180;
+  uint32_t x = TYPE == BMX_F16 ? 0x4C004C00 : 0x41804180;
   asm volatile("" : "+v"(x));
   return x;
 }
-// The levels in fields I and I + 4 of a dword, as operands.
+// The levels in fields I and I + 4 of a dword, as operands: f16 or bf16 by the type.
 template <int TYPE, int I>
 __device__ inline uint32_t two_levels(uint32_t w, uint32_t sixteens) {
-  constexpr int shift = 4 * I - 3;  // onto the mantissa's highest four bits
+  constexpr int shift = 4 * I - (TYPE == BMX_F16 ? 6 : 3);  // onto the mantissa's highest four bits
+  constexpr uint32_t m = TYPE == BMX_F16 ? 0x03C003C0 : 0x00780078;
   uint32_t x;
-  if constexpr (shift < 0) x = ((w << -shift) & 0x00780078) | sixteens;
-  else x = ((w >> shift) & 0x00780078) | sixteens;
+  if constexpr (shift < 0) x = ((w << -shift) & m) | sixteens;
+  else x = ((w >> shift) & m) | sixteens;
   if constexpr (TYPE == BMX_F32) x = upper_halves(__builtin_bit_cast(float, x << 16) - 24.0f, __builtin_bit_cast(float, x & 0xffff0000u) - 24.0f);
   return x;
 }
@@ -60,31 +70,40 @@ __device__ inline void pair(float a, float b, uint32_t (&part)[PARTS]) {
     }
   }
 }
+// The larger of x and that of the lane 32 away.
+__device__ inline float max_32(float x) {
+  const auto two = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a = two[0], b = two[1];
+  return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
 __device__ inline float or_zero(float x) { return x == -INFINITY ? 0.0f : x; }
 
 struct Args {
   const void* q;
   int64_t q_row, q_head;
   JoinTo to;
-  int rows, max_new, window;
+  int rows, max_new, window, prompt_splits;
+  int few;  // sequences of more rows than this are the other kernel's
   bool causal, aligned;
   float scale;
 };
 
 constexpr int kWaves = kJoinWaves;
 constexpr int kCounters = 16384;  // of the workspace's head; what needs more than these has rows enough not to be split
+constexpr int kLeastPages = 16;   // of a split of many rows
+constexpr int kLeastTiles = 128;  // of 128 rows for the kernel for many
 constexpr int64_t kMostTiles = 65535;  // of 16 rows: a launch's second dimension
 
 template <int TYPE, int DC>
 __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cache c, Args a) {
   constexpr int QP = TYPE == BMX_F32 ? 3 : TYPE == BMX_F16 ? 2 : 1, PP = TYPE == BMX_F32 ? 3 : 2;
-  constexpr int ROW = DC * 32, BYTES = DC * 16, LINE = ROW + 4;
+  constexpr int ROW = DC * 32, BYTES = DC * 16, LINE = ROW + 4, LEVEL = TYPE == BMX_F32 ? BMX_F32 : BMX_BF16;
   __shared__ JoinLds<ROW> lds;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16;
   const int head = blockIdx.x % c.heads, split = blockIdx.x / c.heads, seq = blockIdx.z;
   const KvSpan s = kv_span(c, seq, a.rows, a.max_new);
   const int r0 = blockIdx.y * 16, share = a.to.share;
-  if (r0 >= s.count * share) return;
+  if (r0 >= s.count * share || s.count * share > a.few) return;
   // what any, and what every one of the 16 rows sees: positions [low, high)
   const int tok0 = r0 / share, tok1 = min((r0 + 15) / share, s.count - 1);
   const int high_any = a.causal ? min(s.first + tok1 + 1, s.length) : s.length, high_all = a.causal ? min(s.first + tok0 + 1, s.length) : s.length;
@@ -169,7 +188,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
     all *= factor;
   }
 
-  const uint32_t sixteens = sixteen();
+  const uint32_t sixteens = sixteen<LEVEL>();
   float m = -INFINITY, l = 0.0f, rest = 0.0f;  // rest: sum of p_t (d_t + kZero c_t), over this lane's tokens
   f32x4 o[DC][2] = {};  // of each 32 values, the even ones and the odd ones
   while (page >= 0) {
@@ -183,7 +202,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
 #pragma unroll
       for (int i = 0; i < DC; ++i) {
         const uint32_t w = k[u][i];
-        const u32x4 x = {two_levels<TYPE, 0>(w, sixteens), two_levels<TYPE, 1>(w, sixteens), two_levels<TYPE, 2>(w, sixteens), two_levels<TYPE, 3>(w, sixteens)};
+        const u32x4 x = {two_levels<LEVEL, 0>(w, sixteens), two_levels<LEVEL, 1>(w, sixteens), two_levels<LEVEL, 2>(w, sixteens), two_levels<LEVEL, 3>(w, sixteens)};
 #pragma unroll
         for (int part = 0; part < QP; ++part) z = mfma(x, q[part][i], z);
       }
@@ -246,8 +265,8 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t y0 = v[i][2 * h], y1 = v[i][2 * h + 1];
-          const u32x4 x = odd ? u32x4{two_levels<TYPE, 1>(y0, sixteens), two_levels<TYPE, 3>(y0, sixteens), two_levels<TYPE, 1>(y1, sixteens), two_levels<TYPE, 3>(y1, sixteens)}
-                              : u32x4{two_levels<TYPE, 0>(y0, sixteens), two_levels<TYPE, 2>(y0, sixteens), two_levels<TYPE, 0>(y1, sixteens), two_levels<TYPE, 2>(y1, sixteens)};
+          const u32x4 x = odd ? u32x4{two_levels<LEVEL, 1>(y0, sixteens), two_levels<LEVEL, 3>(y0, sixteens), two_levels<LEVEL, 1>(y1, sixteens), two_levels<LEVEL, 3>(y1, sixteens)}
+                              : u32x4{two_levels<LEVEL, 0>(y0, sixteens), two_levels<LEVEL, 2>(y0, sixteens), two_levels<LEVEL, 0>(y1, sixteens), two_levels<LEVEL, 2>(y1, sixteens)};
 #pragma unroll
           for (int part = 0; part < PP; ++part) o[i][odd] = mfma(x, w[part][h], o[i][odd]);
         }
@@ -272,30 +291,341 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
   join_rows<TYPE, ROW>(lds, a.to, c.dim, s.row0, head, r0, min(s.count * share - r0, 16), unit, split, used);
 }
 
+// Many rows: 128 of one head of the cache per workgroup, 32 a wave, over all pages that any of them sees.  A page's levels come into LDS once for
+// the four waves, as 16-bit floats in the order of the 32 x 32 x 16 products' operands, its scales and offsets as floats (a wave brings in a quarter of it, a page ahead, and
+// converts it on its way), and a lane has one row's scores of 16 of 32 tokens, which again are those of its own column of P^T.  Rows of V^T are a block's 16
+// even values, then its odd ones.
+// SPLIT: tiles of rows fewer than the chip holds workgroups at once, whose pages are split and joined as above.
+template <int TYPE, int DC, bool SPLIT>
+__global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv4_cache c, Args a) {
+  static_assert(TYPE != BMX_F32, "");
+  constexpr int BYTES = DC * 16, NS = DC * 2, KN = (DC + 3) / 4;  // NS: steps of 16 values; KN: what a wave brings in of keys, and of values, by 64 lanes
+  __shared__ u32x4 lds[2][2][NS * 128];                           // [buffer][keys, values]
+  __shared__ f32x4 of_token[2][4][16];                            // [buffer][keys' scale and offset, values'][token / 4]
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
+  const int head = SPLIT ? blockIdx.x % c.heads : blockIdx.x, split = SPLIT ? blockIdx.x / c.heads : 0, seq = blockIdx.z;
+  const KvSpan s = kv_span(c, seq, a.rows, a.max_new);
+  const int share = a.to.share, rows = s.count * share;
+  const int r0 = ((rows + 127) / 128 - 1 - (int)blockIdx.y) * 128;  // (the last rows, which see most, first)
+  if (r0 < 0 || rows <= a.few) return;
+  const auto first_seen = [&](int token) { return a.window ? max(max(s.first + token, 0) - a.window + 1, 0) : 0; };
+  const auto end_seen = [&](int token) { return a.causal ? min(s.first + token + 1, s.length) : s.length; };
+  const auto token_of = [&](int r) { return min(r, rows - 1) / share; };
+  // what any row of the workgroup sees; what any, and every row of this wave does; what this lane's row does
+  const int low_group = first_seen(token_of(r0)), high_group = end_seen(token_of(r0 + 127));
+  const int r_wave = r0 + wave * 32, r = r_wave + lane % 32, token = token_of(r);
+  const int low_any = first_seen(token_of(r_wave)), low_all = first_seen(token_of(r_wave + 31));
+  const int high_all = end_seen(token_of(r_wave)), high_any = r_wave < rows ? end_seen(token_of(r_wave + 31)) : 0;
+  const int low = first_seen(token), high = end_seen(token);
+
+  const int64_t page_bytes = (int64_t)c.heads * 2 * kPage * BYTES;
+  const float factor = a.scale * 1.4426950408889634f;
+  const uint32_t sixteens = sixteen<TYPE>(), sixteens_v = sixteen<BMX_BF16>();
+  u32x4 kr[KN], vr[KN][2];
+  uint32_t pair_in = 0;  // waves 0 and 1: a token's scale and offset, of keys and of values
+  int begin = low_group / kPage, last = kv_pages_to(high_group), used = 1;
+  if constexpr (SPLIT) {  // this split's pages: as many for the rows that see few as for those that see most, which then are in fewer splits
+    const int pages = max(last - begin, 0), most_pages = kv_pages_to(s.length) - first_seen(token_of((rows - 1) / 128 * 128)) / kPage;
+    const int per = max((max(most_pages, pages) + a.prompt_splits - 1) / a.prompt_splits, kLeastPages);
+    used = max((pages + per - 1) / per, 1);
+    if (split >= used) return;
+    last = begin + min(pages, (split + 1) * per);
+    begin += split * per;
+  }
+  const int none = c.num_pages > 0 ? 0 : kNowhere;
+  // the first page from `pg` on that is there, on its way into registers
+  const auto fetch = [&](int pg) {
+    int page = -1;
+    for (; pg < last; ++pg) {
+      page = kv_page(c, seq, pg);
+      if (page >= 0) break;
+    }
+    // (behind the last page: page 0 once more, which nobody uses)
+    const Rsrc r = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)head * 2 * kPage * BYTES, 2 * kPage * BYTES);
+    const Rsrc rs = buffer(c.scales + ((int64_t)max(page, 0) * c.heads + head) * 4 * kPage, 8 * kPage);
+    if (wave < 2) pair_in = load4(rs, threadIdx.x * 4 + none, 0);
+#pragma unroll
+    for (int n = 0; n < KN; ++n) {
+      const int i = min(lane / 16 + 4 * n, DC - 1), block = min(wave + 4 * n, DC - 1);
+      kr[n] = load16(r, lane % 16 * BYTES + i * 16 + none, wave * 16 * BYTES);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) vr[n][g] = load16(r, lane / 16 % 2 * 256 + lane % 16 * 16 + none, kPage * BYTES + block * 1024 + g * 512);
+    }
+    return pg;
+  };
+  const auto convert = [&](int buf) {
+    // keys: 32 values of token 16 wave + lane % 16; values: of a block a pair's even ones or its odd ones, every other four tokens
+#pragma unroll
+    for (int n = 0; n < KN; ++n) {
+      const int i = lane / 16 + 4 * n;
+      if (i < DC) {
+        u32x4* to = &lds[buf][0][(wave / 2 * NS + 2 * i) * 64 + wave % 2 * 16 + lane % 16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = kr[n][j];
+          to[j / 2 * 64 + j % 2 * 32] = u32x4{two_levels<TYPE, 0>(w, sixteens), two_levels<TYPE, 1>(w, sixteens), two_levels<TYPE, 2>(w, sixteens), two_levels<TYPE, 3>(w, sixteens)};
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < KN; ++n) {
+      if (wave + 4 * n >= DC) break;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t x = vr[n][0][u] >> (h * 4), y = vr[n][1][u] >> (h * 4);
+        lds[buf][1][(u * DC + wave + 4 * n) * 64 + lane / 16 % 2 * 32 + h * 16 + lane % 16] =
+            u32x4{two_levels<BMX_BF16, 0>(x, sixteens_v), two_levels<BMX_BF16, 2>(x, sixteens_v), two_levels<BMX_BF16, 0>(y, sixteens_v), two_levels<BMX_BF16, 2>(y, sixteens_v)};
+      }
+    }
+    if (wave < 2) {
+      const float scale = bf16_float(pair_in), offset = __builtin_bit_cast(float, pair_in & 0xffff0000u) - 16.0f * scale;
+      float* to = reinterpret_cast<float*>(of_token[buf][2 * wave]) + lane;
+      to[0] = wave ? scale : scale * factor;
+      to[64] = offset;
+    }
+  };
+  int pg = fetch(begin);
+
+  u32x4 q[NS];
+  float all = 0.0f;
+  {
+    const int64_t base = (s.row0 + token) * a.q_row + (head * share + min(r, rows - 1) % share) * a.q_head;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const int d = 16 * i + 8 * h;
+      float x[8];
+      load_eight<TYPE>(a.q, base + d, c.dim - d, a.aligned, x);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        q[i][j] = TYPE == BMX_F16 ? f16_bits(x[j]) | f16_bits(x[4 + j]) << 16 : upper_halves(x[j], x[4 + j]);
+        all += x[j] + x[4 + j];
+      }
+    }
+    all += __shfl_xor(all, 32);
+    all *= factor;
+  }
+  if (pg < last) convert(0);
+  __syncthreads();
+
+  // (what LDS holds does not come into registers all at once: there are not as many)
+  const auto fence = [](bool here) {
+    if (DC > 2 && here) __builtin_amdgcn_sched_barrier(0);
+  };
+  float m = -INFINITY, l = 0.0f, rest = 0.0f;
+  f32x16 o[DC] = {};
+  for (int buf = 0; pg < last; buf ^= 1) {
+    const int next = fetch(pg + 1), t0 = pg * kPage;
+    if (t0 < high_any && t0 + kPage - 1 >= low_any) {
+      f32x16 z[2] = {};
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) z[t] = mfma32<TYPE == BMX_F16>(lds[buf][0][(t * NS + i) * 64 + lane], q[i], z[t]);
+        fence(i % 4 == 3);
+      }
+      const bool whole = kv_all_in(t0, kPage, low_all, high_all);
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 scale = of_token[buf][0][t * 8 + j * 2 + h], offset = of_token[buf][1][t * 8 + j * 2 + h];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) z[t][4 * j + i] = z[t][4 * j + i] * scale[i] + all * offset[i];
+          fence(j % 2);
+        }
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const int t = t0 + i / 4 * 8 + 4 * h + i % 4;
+          z[i / 16][i % 16] = t < high && t >= low ? z[i / 16][i % 16] : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) top = fmaxf(top, z[i / 16][i % 16]);
+      top = max_32(top);
+      const float m_new = fmaxf(m, top), m_at = or_zero(m_new), shrink = __builtin_amdgcn_exp2f(m - m_at);
+      m = m_new;
+      u32x4 w[2][4];  // [part][16 tokens]
+      float sum = 0.0f, more = 0.0f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        f32x4 scale = of_token[buf][2][u * 2 + h], offset = of_token[buf][3][u * 2 + h];
+        if (!whole) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {  // (a token that the row does not see may have any)
+            const int t = t0 + u * 8 + 4 * h + i;
+            const bool sees = t < high && t >= low;
+            scale[i] = sees ? scale[i] : 0.0f, offset[i] = sees ? offset[i] : 0.0f;
+          }
+        }
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = __builtin_amdgcn_exp2f(z[u / 4][u % 4 * 4 + i] - m_at);
+          sum += e;
+          more += e * offset[i];
+          x[i] = e * scale[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t part[2];
+          pair<2>(x[i], x[i + 2], part);
+          w[0][u / 2][u % 2 * 2 + i] = part[0], w[1][u / 2][u % 2 * 2 + i] = part[1];
+        }
+        fence(u % 2);
+      }
+      l = l * shrink + sum;
+      rest = rest * shrink + more;
+      if (__any(shrink != 1.0f)) {  // (most pages hold no new maximum)
+#pragma unroll
+        for (int n = 0; n < DC; ++n) o[n] *= shrink;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int n = 0; n < DC; ++n) {
+          const u32x4 x = lds[buf][1][(u * DC + n) * 64 + lane];
+          o[n] = mfma32<false>(x, w[1][u], mfma32<false>(x, w[0][u], o[n]));
+          fence(n % 4 == 3);
+        }
+    }
+    if (next < last) convert(buf ^ 1);
+    pg = next;
+    __syncthreads();
+  }
+  l += __shfl_xor(l, 32);
+  rest += __shfl_xor(rest, 32);
+  if (SPLIT && used > 1) {  // the parts: each lane's numbers at the same place in all of them
+    const int64_t unit = ((int64_t)seq * gridDim.y + r0 / 128) * c.heads + head;
+    constexpr int PART = 64 * (DC * 16 + 2);
+    float* at = a.to.parts + (unit * a.prompt_splits * 4 + wave) * PART + lane * 2;
+    if (r_wave < rows) {
+      float* to = at + (int64_t)split * 4 * PART;
+#pragma unroll
+      for (int n = 0; n < DC; ++n)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) put(to + (n * 8 + i) * 128, o[n][2 * i] + rest, o[n][2 * i + 1] + rest);
+      put(to + DC * 1024, m, l);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's numbers are there
+    __shared__ uint32_t place;
+    __syncthreads();
+    if (threadIdx.x == 0) place = __hip_atomic_fetch_add(a.to.arrived + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (place != (uint32_t)used - 1) return;
+    if (threadIdx.x == 0) __hip_atomic_store(a.to.arrived + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (r_wave >= rows) return;
+    m = -INFINITY, l = 0.0f, rest = 0.0f;
+    for (int p = 0; p < used; ++p) {
+      const float* from = at + (int64_t)p * 4 * PART;
+      const u32x2 x = get(from + DC * 1024);
+      constexpr int N = DC <= 4 ? DC : 2;
+      const uint32_t x0 = x[0], x1 = x[1];
+      const float m_part = __builtin_bit_cast(float, x0), m_new = fmaxf(m, m_part), m_at = or_zero(m_new);
+      const float f = __builtin_amdgcn_exp2f(m - m_at), f_part = __builtin_amdgcn_exp2f(m_part - m_at);
+      l = l * f + __builtin_bit_cast(float, x1) * f_part;
+      m = m_new;
+#pragma unroll
+      for (int n0 = 0; n0 < DC; n0 += N) {
+        u32x2 y[N * 8];  // (every read at once: each is a trip to memory)
+#pragma unroll
+        for (int i = 0; i < N * 8; ++i)
+          if (n0 * 8 + i < DC * 8) y[i] = get(from + (n0 * 8 + i) * 128);
+#pragma unroll
+        for (int n = n0; n < n0 + N && n < DC; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t v = y[(n - n0) * 8 + i / 2][i % 2];
+            o[n][i] = (p == 0 ? 0.0f : o[n][i] * f) + __builtin_bit_cast(float, v) * f_part;
+          }
+      }
+    }
+  }
+  if (r >= rows) return;
+  int right = 8 * h, mine = r;
+  asm("" : "+v"(right), "+v"(mine));  // (places are counted anew: kept from where the queries were read, they would be registers through the whole loop)
+  const int64_t to = s.row0 + mine / share;
+  const int to_head = head * share + mine % share;
+  const int64_t at = to * a.to.out_row + to_head * a.to.out_head;
+  const float share_of = 1.0f / l;  // (a row that sees nothing is zeros)
+#pragma unroll
+  for (int n = 0; n < DC; ++n)
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      const int d = n * 32 + i * 4 + right;  // eight values from here on
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[2 * j] = l == 0.0f ? 0.0f : (o[n][i + j] + rest) * share_of;
+        x[2 * j + 1] = l == 0.0f ? 0.0f : (o[n][8 + i + j] + rest) * share_of;
+      }
+      if (d + 8 <= c.dim) {
+        Run<TYPE, 8> y;
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) y.set2(j, x[j], x[j + 1]);
+        y.store(a.to.out, at + d, 8);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (d + j < c.dim) store_one<TYPE>(a.to.out, at + d + j, x[j]);
+      }
+    }
+  if (a.to.lse && h == 0)
+    a.to.lse[to * a.to.q_heads + to_head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
 // What a call needs: tiles of rows, splits, and bytes of the workspace.
 struct Plan {
-  int64_t units, tiles;
-  int splits, part_rows;
+  int64_t units, tiles, prompt_tiles;  // prompt_tiles: of 128 rows, 0 where they are too few to fill the chip
+  int splits, part_rows, few, prompt_splits;
   size_t bytes;
 };
-Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new) {
+Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new, int type) {
   Plan p;
-  const int64_t rows = max_new * (q_heads / heads);
+  int64_t rows = max_new * (q_heads / heads);
+  p.few = 0x7fffffff;
+  p.prompt_tiles = 0;
+  if (type != BMX_F32 && ceil_div(rows, 128) * heads * sequences >= kLeastTiles && rows > 64) {
+    p.prompt_tiles = ceil_div(rows, 128);
+    p.few = 64;
+    rows = 64;
+  }
+  const size_t line = (kv4_row_bytes((int)dim) * 2 + 4) * 4;
   p.tiles = ceil_div(rows, 16);
   p.units = sequences * heads * p.tiles;
   p.part_rows = (int)std::min<int64_t>(rows, 16);
   // one workgroup for each of the chip's 256 CUs, but four pages of the longest sequence for each at least
   p.splits = (int)std::max<int64_t>(std::min({ceil_div(256, std::max<int64_t>(p.units, 1)), ceil_div(table_width, 4), (int64_t)kMostSplits}), 1);
   if (p.units > kCounters) p.splits = 1;
-  p.bytes = p.splits == 1 ? 0 : kCounters * 4 + (size_t)p.units * p.splits * p.part_rows * (kv4_row_bytes((int)dim) * 2 + 4) * 4;
+  p.bytes = p.splits == 1 ? 0 : kCounters * 4 + (size_t)p.units * p.splits * p.part_rows * line;
+  p.prompt_splits = 1;
+  if (p.prompt_tiles) {
+    const int64_t units = p.prompt_tiles * heads * sequences;
+    // as many workgroups as the chip holds at once, two a CU up to 128 values and one beyond, of 16 pages each at least
+    p.prompt_splits = (int)std::max<int64_t>(std::min<int64_t>((dim <= 128 ? 512 : 256) / units, table_width / kLeastPages), 1);
+    if (p.prompt_splits > 1) p.bytes = std::max(p.bytes, kCounters * 4 + (size_t)units * p.prompt_splits * 128 * line);
+  }
   return p;
 }
 
 template <int TYPE, int DC>
 void launch(const bmx_kv4_cache& c, const Args& a, const Plan& p, hipStream_t s) {
-  const dim3 grid(c.heads * p.splits, (uint32_t)p.tiles, c.sequences);
-  launch_kernel(kv4_attention_kernel<TYPE, DC>, grid, dim3(kWaves * 64), 0, s, c, a);
-  note_kernel("kv4_attention_kernel<%d,%d> grid %ux%ux%u block %d", TYPE, DC, grid.x, grid.y, grid.z, kWaves * 64);
+  // (rows of sequences as long as each other are all many or all few)
+  if (!p.prompt_tiles || (c.starts && c.sequences > 1)) {
+    const dim3 grid(c.heads * p.splits, (uint32_t)p.tiles, c.sequences);
+    launch_kernel(kv4_attention_kernel<TYPE, DC>, grid, dim3(kWaves * 64), 0, s, c, a);
+    note_kernel("kv4_attention_kernel<%d,%d> grid %ux%ux%u block %d", TYPE, DC, grid.x, grid.y, grid.z, kWaves * 64);
+  }
+  if constexpr (TYPE != BMX_F32) {
+    if (p.prompt_tiles) {
+      const dim3 grid(c.heads * p.prompt_splits, (uint32_t)p.prompt_tiles, c.sequences);
+      Args b = a;
+      if (!c.starts || c.sequences == 1) b.few = 0;
+      launch_kernel(p.prompt_splits > 1 ? kv4_prompt_kernel<TYPE, DC, true> : kv4_prompt_kernel<TYPE, DC, false>, grid, dim3(256), 0, s, c, b);
+      note_kernel("kv4_prompt_kernel<%d,%d,%d> grid %ux%ux%u block 256", TYPE, DC, p.prompt_splits > 1, grid.x, grid.y, grid.z);
+    }
+  }
 }
 template <int TYPE>
 void launch_typed(const bmx_kv4_cache& c, const Args& a, const Plan& p, hipStream_t s) {
@@ -313,14 +643,21 @@ size_t kv4_attention_workspace(int64_t sequences, int64_t table_width, int64_t h
   // The largest of the calls' bytes, which first grow with the rows and then, where rows fill the chip without splits, fall.  In closed form: of
   // `each` units a tile, and splits that bring t tiles to 256 workgroups, each * t * splits <= 255 + each * t while that is worth a split.
   const int64_t each = sequences * heads, rows = max_new > 0 ? std::min(max_new * (q_heads / heads), kMostTiles * 16) : kMostTiles * 16;
+  const size_t line = (kv4_row_bytes((int)dim) * 2 + 4) * 4;
+  size_t most = 0;
   if (each == 0) return 0;
   const int64_t units = each * std::min(ceil_div(rows, 16), 255 / each), splits = std::min<int64_t>(ceil_div(table_width, 4), kMostSplits);
-  if (units == 0 || splits <= 1) return 0;
-  return kCounters * 4 + std::min(units * splits, units + 255) * std::min<int64_t>(rows, 16) * (kv4_row_bytes((int)dim) * 2 + 4) * 4;
+  if (units > 0 && splits > 1) most = std::min(units * splits, units + 255) * std::min<int64_t>(rows, 16) * line;
+  const int64_t places = dim <= 128 ? 512 : 256, tiles = each * std::min(ceil_div(rows, 128), places / 2 / each);
+  if (rows > 64 && tiles >= kLeastTiles && table_width / kLeastPages > 1)
+    most = std::max<size_t>(most, std::min(places, tiles * (table_width / kLeastPages)) * 128 * line);
+  return most ? kCounters * 4 + most : 0;
 }
 
 size_t kv4_attention_workspace_of_call(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new) {
-  return plan(sequences, table_width, heads, q_heads, dim, max_new).bytes;
+  // (whatever the type)
+  return std::max(plan(sequences, table_width, heads, q_heads, dim, max_new, BMX_F32).bytes,
+                  plan(sequences, table_width, heads, q_heads, dim, max_new, BMX_F16).bytes);
 }
 
 hipError_t launch_kv4_attention(const bmx_kv4_cache& c, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int rows,
@@ -328,11 +665,12 @@ hipError_t launch_kv4_attention(const bmx_kv4_cache& c, const void* q, int type,
                                 void* workspace, bool fresh, hipStream_t s) {
   const int64_t size = type_bytes(type);
   const bool aligned = (uintptr_t)q % 16 == 0 && q_row * size % 16 == 0 && q_head * size % 16 == 0;
-  const Plan p = plan(c.sequences, c.table_width, c.heads, q_heads, c.dim, max_new);
+  const Plan p = plan(c.sequences, c.table_width, c.heads, q_heads, c.dim, max_new, type);
   uint32_t* arrived = static_cast<uint32_t*>(workspace);
   const Args a = {q, q_row, q_head, {out, out_row, out_head, lse, reinterpret_cast<float*>(arrived + kCounters), arrived, q_heads, q_heads / c.heads, p.splits, p.part_rows},
-                  rows, max_new, window, causal, aligned, scale};
-  if (fresh && p.splits > 1) launch_kernel(clear_kernel, dim3((uint32_t)ceil_div(p.units, 256)), dim3(256), 0, s, arrived);
+                  rows, max_new, window, p.prompt_splits, p.few, causal, aligned, scale};
+  const int64_t counters = std::max(p.splits > 1 ? p.units : 0, p.prompt_splits > 1 ? p.prompt_tiles * c.heads * c.sequences : 0);
+  if (fresh && counters) launch_kernel(clear_kernel, dim3((uint32_t)ceil_div(counters, 256)), dim3(256), 0, s, arrived);
   const auto f = type == BMX_F32 ? launch_typed<BMX_F32> : type == BMX_F16 ? launch_typed<BMX_F16> : launch_typed<BMX_BF16>;
   f(c, a, p, s);
   return launch_error();

@@ -281,12 +281,26 @@ def test_attention_of_many_rows(kind):
         attend(cache, share, new, kind, seed=3, causal=False)
 
 
+@pytest.mark.parametrize("kind", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("dim", [20, 32, 64, 80, 96, 128, 150, 192, 224, 255, 256])
+def test_prompts_split_and_not(kind, dim):
+    """Rows enough for the kernel of 128 rows: with pages split over workgroups (a long table and few tiles), and not; with few rows beside them."""
+    cache = Cache(4, dim, [2100], seed=dim)
+    for named in (dict(), dict(window=700), dict(causal=False)):
+        attend(cache, 8, [520], kind, seed=1, gap=dim % 3, **named)
+        assert "prompt" in B.last_kernel()
+    cache = Cache(4, dim, [900, 70, 500], seed=dim)
+    attend(cache, 8, [400, 3, 500], kind, seed=2, window=90)
+    attend(cache, 8, [400, 3, 9], kind, seed=3)
+
+
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("scale", [0.0, -0.3, 5.0, 1e-6])
 def test_attention_scales(kind, scale):
     cache = Cache(2, 64, [300, 70], seed=1)
     attend(cache, 2, [1, 1], kind, seed=1, scale=scale)
     attend(cache, 2, [150, 70], kind, seed=1, scale=scale)
+    attend(Cache(4, 64, [600], seed=1), 8, [600], kind, seed=2, scale=scale)
 
 
 @pytest.mark.parametrize("kind", TYPES)
