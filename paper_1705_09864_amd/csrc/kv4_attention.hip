@@ -57,6 +57,12 @@ __device__ inline uint32_t two_levels(uint32_t w, uint32_t sixteens) {
   return x;
 }
 
+// Two values rounded to bf16, by the one instruction.
+__device__ inline uint32_t two_bf16(float a, float b) {
+  using f32x2 = float __attribute__((ext_vector_type(2)));
+  using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
 // Two values as PARTS pairs of bf16: the bits of all but the last are cut off.
 template <int PARTS>
 __device__ inline void pair(float a, float b, uint32_t (&part)[PARTS]) {
@@ -66,53 +72,88 @@ __device__ inline void pair(float a, float b, uint32_t (&part)[PARTS]) {
       part[p] = upper_halves(a, b);
       a = lower_part(a), b = lower_part(b);
     } else {
-      part[p] = bf16_bits(a) | bf16_bits(b) << 16;
+      part[p] = two_bf16(a, b);
     }
   }
 }
-// The larger of x and that of the lane 32 away.
+// The larger of x and that of the lane 16, and 32, away.
+__device__ inline float max_16(float x) {
+  const auto two = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a = two[0], b = two[1];
+  return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
 __device__ inline float max_32(float x) {
   const auto two = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
   const uint32_t a = two[0], b = two[1];
   return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
+// Values changed in a branch, which stays one by it: the compiler would make selections of it, for all pages.
+template <class V>
+__device__ inline void apart(V& v) { asm volatile("" : "+v"(v)); }
 __device__ inline float or_zero(float x) { return x == -INFINITY ? 0.0f : x; }
+
+// By so much (of a logarithm of 2) a row's scores may pass the one that its weights are relative to, before they are taken relative to a larger one: weights have
+// fp32's range, and a row's results would otherwise be multiplied anew on every other page.
+constexpr float kGrowth = 8.0f;
 
 struct Args {
   const void* q;
   int64_t q_row, q_head;
   JoinTo to;
   int rows, max_new, window, prompt_splits;
+  int units, tiles;  // tiles of 16 rows, of all sequences and of one
+  Deal deal;         // of their pages; no extra parts: a tile's are all one workgroup's
   int few;  // sequences of more rows than this are the other kernel's
   bool causal, aligned;
   float scale;
 };
 
-constexpr int kWaves = kJoinWaves;
-constexpr int kCounters = 16384;  // of the workspace's head; what needs more than these has rows enough not to be split
+constexpr int kCounters = 16384;  // of the workspace's head
 constexpr int kLeastPages = 16;   // of a split of many rows
 constexpr int kLeastTiles = 128;  // of 128 rows for the kernel for many
+constexpr int64_t kPlaces = 512, kMostPlaces = 2048;
 constexpr int64_t kMostTiles = 65535;  // of 16 rows: a launch's second dimension
 
-template <int TYPE, int DC>
-__global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cache c, Args a) {
+// The 16 rows from r0 on of a sequence: what any, and what every one of them sees, positions [low, high).
+struct Seen {
+  int low_any, high_any, low_all, high_all;
+  __device__ Seen(const Args& a, const KvSpan& s, int r0) {
+    const int tok0 = r0 / a.to.share, tok1 = min((r0 + 15) / a.to.share, s.count - 1);
+    high_any = a.causal ? min(s.first + tok1 + 1, s.length) : s.length, high_all = a.causal ? min(s.first + tok0 + 1, s.length) : s.length;
+    low_any = a.window ? max(max(s.first + tok0, 0) - a.window + 1, 0) : 0, low_all = a.window ? max(max(s.first + tok1, 0) - a.window + 1, 0) : 0;
+  }
+  __device__ int pages() const { return max(kv_pages_to(high_any) - low_any / kPage, 0); }
+};
+
+// Rows from r0 on that are this kernel's.
+__device__ inline bool has_rows(const Args& a, const KvSpan& s, int r0) { return r0 < s.count * a.to.share && s.count * a.to.share <= a.few; }
+
+template <int TYPE, int DC, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void kv4_attention_kernel(bmx_kv4_cache c, Args a) {
   constexpr int QP = TYPE == BMX_F32 ? 3 : TYPE == BMX_F16 ? 2 : 1, PP = TYPE == BMX_F32 ? 3 : 2;
   constexpr int ROW = DC * 32, BYTES = DC * 16, LINE = ROW + 4, LEVEL = TYPE == BMX_F32 ? BMX_F32 : BMX_BF16;
-  __shared__ JoinLds<ROW> lds;
+  // (the queries' three parts and a page beside them leave no registers: 16 tokens after the other, scales of values when they are needed)
+  constexpr bool TIGHT = TYPE == BMX_F32 && DC > 4;
+  __shared__ JoinLds<ROW, WAVES> lds;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16;
-  const int head = blockIdx.x % c.heads, split = blockIdx.x / c.heads, seq = blockIdx.z;
+  const int head = blockIdx.x % c.heads, share = a.to.share;
+  Part part = {(int)(blockIdx.z * gridDim.y + blockIdx.y), 0, 1, 0, kAllPages};
+  if (a.deal.extra > 0) {
+    part = part_of(blockIdx.x / c.heads, a.units, a.deal, [&](int n) {
+      const KvSpan s = kv_span(c, n / a.tiles, a.rows, a.max_new);
+      const int r0 = n % a.tiles * 16;
+      return has_rows(a, s, r0) ? Seen(a, s, r0).pages() : -1;
+    });
+    if (part.unit < 0) return;
+  }
+  const int seq = part.unit / a.tiles, r0 = part.unit % a.tiles * 16;
   const KvSpan s = kv_span(c, seq, a.rows, a.max_new);
-  const int r0 = blockIdx.y * 16, share = a.to.share;
-  if (r0 >= s.count * share || s.count * share > a.few) return;
-  // what any, and what every one of the 16 rows sees: positions [low, high)
-  const int tok0 = r0 / share, tok1 = min((r0 + 15) / share, s.count - 1);
-  const int high_any = a.causal ? min(s.first + tok1 + 1, s.length) : s.length, high_all = a.causal ? min(s.first + tok0 + 1, s.length) : s.length;
-  const int low_any = a.window ? max(max(s.first + tok0, 0) - a.window + 1, 0) : 0, low_all = a.window ? max(max(s.first + tok1, 0) - a.window + 1, 0) : 0;
+  if (!has_rows(a, s, r0)) return;
+  const Seen seen(a, s, r0);
+  const int low_all = seen.low_all, high_all = seen.high_all;
   // this workgroup's pages
-  const int page0 = low_any / kPage, pages = max(kv_pages_to(high_any) - page0, 0);
-  const int per = pages <= 3 * kWaves ? pages : max((pages + a.to.splits - 1) / a.to.splits, kWaves), used = pages > 0 ? (pages + per - 1) / per : 1;
-  if (split >= used) return;
-  const int begin = page0 + split * per, count = max(min(per, pages - split * per) - wave + kWaves - 1, 0) / kWaves;  // (of this wave, kWaves apart)
+  const int pages = min(seen.pages() - part.split * part.per, part.per), begin = seen.low_any / kPage + part.split * part.per;
+  const int count = max(pages - wave + WAVES - 1, 0) / WAVES;  // (of this wave, WAVES apart)
 
   const int64_t page_bytes = (int64_t)c.heads * 2 * kPage * BYTES;
   int ids = -1, next = 0;  // the numbers of 64 pages, a lane each; the place of the next page
@@ -123,7 +164,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
   const auto load_keys = [&] {
     page = -1;
     for (; next < count; ++next) {
-      if (next % 64 == 0) ids = next + lane < count ? kv_page(c, seq, begin + wave + (next + lane) * kWaves) : -1;
+      if (next % 64 == 0) ids = next + lane < count ? kv_page(c, seq, begin + wave + (next + lane) * WAVES) : -1;
       page = __builtin_amdgcn_readlane(ids, next % 64);
       if (page >= 0) break;
     }
@@ -149,26 +190,30 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
 #pragma unroll
     for (int u = 0; u < 4; ++u) key_pairs[u] = load16(rs, g * 16 + none, u * 64);
   };
+  const auto load_value_pairs = [&] {
+    const Rsrc rs = buffer(c.scales + (((int64_t)max(page, 0) * c.heads + head) * 2 + 1) * 2 * kPage, 4 * kPage);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) value_pairs[u] = load16(rs, g * 16 + (page >= 0 ? 0 : kNowhere), u * 64);
+  };
   const auto load_values = [&] {
     const int none = page >= 0 ? 0 : kNowhere;
     const Rsrc r = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)(head * 2 + 1) * kPage * BYTES, kPage * BYTES);
 #pragma unroll
     for (int i = 0; i < DC; ++i) v[i] = load16(r, lane * 16 + none, i * 1024);
-    const Rsrc rs = buffer(c.scales + (((int64_t)max(page, 0) * c.heads + head) * 2 + 1) * 2 * kPage, 4 * kPage);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) value_pairs[u] = load16(rs, g * 16 + none, u * 64);
+    if (!TIGHT) load_value_pairs();
   };
   load_keys();
   load_values();
 
-  // this lane's row of queries
+  // this lane's row of queries, with the scale's sign
   const int r = r0 + lane % 16, token = min(r / share, s.count - 1), pos = s.first + token;
   const int high = a.causal ? min(pos + 1, s.length) : s.length, low = a.window ? max(max(pos, 0) - a.window + 1, 0) : 0;
-  const float factor = a.scale * 1.4426950408889634f;
+  const float factor = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 0x1p-126f);  // (0 times the score of a token that is not seen would be none)
   u32x4 q[QP][DC];
-  float all = 0.0f;  // the row's sum, times the factor
+  float all = 0.0f;  // the row's sum
   {
     const int64_t base = (s.row0 + token) * a.q_row + (head * share + r % share) * a.q_head;
+    const float sign = a.scale < 0.0f ? -1.0f : 1.0f;
 #pragma unroll
     for (int i = 0; i < DC; ++i) {
       const int d = 8 * (DC * g + i);
@@ -177,28 +222,31 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
 #pragma unroll
       for (int j = 0; j < 4; ++j) {  // (in the order of a dword's fields)
         uint32_t part[QP];
-        pair<QP>(x[j], x[4 + j], part);
-        all += x[j] + x[4 + j];
+        pair<QP>(sign * x[j], sign * x[4 + j], part);
+        all += sign * x[j] + sign * x[4 + j];
 #pragma unroll
         for (int p = 0; p < QP; ++p) q[p][i][j] = part[p];
       }
     }
     all += __shfl_xor(all, 16);
     all += __shfl_xor(all, 32);
-    all *= factor;
   }
 
   const uint32_t sixteens = sixteen<LEVEL>();
-  float m = -INFINITY, l = 0.0f, rest = 0.0f;  // rest: sum of p_t (d_t + kZero c_t), over this lane's tokens
+  // what the products of 16 + level begin with, so that they end as those of the levels
+  const float begin_at = TYPE == BMX_F32 ? 0.0f : -16.0f * all;
+  const f32x4 z0 = {begin_at, begin_at, begin_at, begin_at};
+  // held: the score, times log2 e, that the row's weights are relative to; rest: sum of p_t (d_t + kZero c_t), over this lane's tokens
+  float held = -INFINITY, l = 0.0f, rest = 0.0f;
   f32x4 o[DC][2] = {};  // of each 32 values, the even ones and the odd ones
   while (page >= 0) {
-    const int t0 = (begin + wave + at * kWaves) * kPage;
-    const bool whole = kv_all_in(t0, kPage, low_all, high_all);
+    const int t0 = (begin + wave + at * WAVES) * kPage;
+    const bool whole = __builtin_amdgcn_readfirstlane(kv_all_in(t0, kPage, low_all, high_all));
     float p[4][4];
     float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      f32x4 z = {};
+      f32x4 z = z0;
 #pragma unroll
       for (int i = 0; i < DC; ++i) {
         const uint32_t w = k[u][i];
@@ -209,10 +257,12 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t w = key_pairs[u][i];
-        const float ks = bf16_float(w), ko = __builtin_bit_cast(float, w & 0xffff0000u) + kZero<TYPE> * ks;
-        p[u][i] = z[i] * (factor * ks) + all * ko;
+        const float ks = bf16_float(w), ko = __builtin_bit_cast(float, w & 0xffff0000u);
+        p[u][i] = z[i] * ks + all * (TYPE == BMX_F32 ? ko + 8.0f * ks : ko);
       }
+      if (TIGHT) __builtin_amdgcn_sched_barrier(0);
     }
+    if (TIGHT) load_value_pairs();
     load_keys();
     if (!whole) {
 #pragma unroll
@@ -224,16 +274,28 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
           p[u][i] = sees ? p[u][i] : -INFINITY;
           value_pairs[u][i] = sees ? value_pairs[u][i] : 0;  // (those of a token that nobody has written may be anything)
         }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        apart(value_pairs[u]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) apart(p[u][i]);
+      }
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, p[u][i]);
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float m_new = fmaxf(m, top), m_at = or_zero(m_new), shrink = __builtin_amdgcn_exp2f(m - m_at);
-    m = m_new;
-    float sum = 0.0f, more = 0.0f;
+    top = max_32(max_16(top));
+    const float at_top = top * factor;
+    if (__any(at_top > held + kGrowth)) {  // (a row's first page, and few others)
+      const bool mine = at_top > held + kGrowth;
+      const float shrink = mine ? __builtin_amdgcn_exp2f(held - at_top) : 1.0f;
+      held = mine ? at_top : held;
+      l *= shrink, rest *= shrink;
+#pragma unroll
+      for (int i = 0; i < DC; ++i) o[i][0] *= shrink, o[i][1] *= shrink;
+    }
+    const float held_at = or_zero(held);
     u32x4 w[PP][2];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -242,9 +304,9 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
       for (int i = 0; i < 4; ++i) {
         const uint32_t y = value_pairs[u][i];
         const float vs = bf16_float(y), vo = __builtin_bit_cast(float, y & 0xffff0000u) + kZero<TYPE> * vs;
-        const float e = __builtin_amdgcn_exp2f(p[u][i] - m_at);
-        sum += e;
-        more += e * vo;
+        const float e = __builtin_amdgcn_exp2f(p[u][i] * factor - held_at);
+        l += e;
+        rest += e * vo;
         x[i] = e * vs;
       }
 #pragma unroll
@@ -254,14 +316,12 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
 #pragma unroll
         for (int n = 0; n < PP; ++n) w[n][u / 2][u % 2 * 2 + i] = part[n];
       }
+      if (TIGHT) __builtin_amdgcn_sched_barrier(0);
     }
-    l = l * shrink + sum;
-    rest = rest * shrink + more;
 #pragma unroll
-    for (int i = 0; i < DC; ++i) {
+    for (int i = 0; i < DC; ++i)
 #pragma unroll
-      for (int odd = 0; odd < 2; ++odd) {
-        o[i][odd] *= shrink;
+      for (int odd = 0; odd < 2; ++odd)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t y0 = v[i][2 * h], y1 = v[i][2 * h + 1];
@@ -270,8 +330,6 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
 #pragma unroll
           for (int part = 0; part < PP; ++part) o[i][odd] = mfma(x, w[part][h], o[i][odd]);
         }
-      }
-    }
     load_values();
   }
 
@@ -279,7 +337,7 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
   l += __shfl_xor(l, 32);
   rest += __shfl_xor(rest, 16);
   rest += __shfl_xor(rest, 32);
-  if (g == 0) lds.red_m[wave][lane] = m, lds.red_l[wave][lane] = l;
+  if (g == 0) lds.red_m[wave][lane] = held, lds.red_l[wave][lane] = l;
 #pragma unroll
   for (int i = 0; i < DC; ++i)
 #pragma unroll
@@ -287,8 +345,8 @@ __global__ __launch_bounds__(kWaves * 64) void kv4_attention_kernel(bmx_kv4_cach
       *reinterpret_cast<f32x4*>(&lds.red[(wave * 16 + lane % 16) * LINE + i * 32 + 8 * g + 2 * j]) =
           f32x4{o[i][0][j] + rest, o[i][1][j] + rest, o[i][0][j + 1] + rest, o[i][1][j + 1] + rest};
   __syncthreads();
-  const int64_t unit = ((int64_t)seq * gridDim.y + blockIdx.y) * c.heads + head;
-  join_rows<TYPE, ROW>(lds, a.to, c.dim, s.row0, head, r0, min(s.count * share - r0, 16), unit, split, used);
+  join_rows<TYPE, ROW, WAVES>(lds, a.to, c.dim, s.row0, head, r0, min(s.count * share - r0, 16), (int64_t)part.unit * c.heads + head,
+                              (int64_t)head * (a.units + a.deal.extra) + part.first, part.split, part.used);
 }
 
 // Many rows: 128 of one head of the cache per workgroup, 32 a wave, over all pages that any of them sees.  A page's levels come into LDS once for
@@ -301,7 +359,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
   static_assert(TYPE != BMX_F32, "");
   constexpr int BYTES = DC * 16, NS = DC * 2, KN = (DC + 3) / 4;  // NS: steps of 16 values; KN: what a wave brings in of keys, and of values, by 64 lanes
   __shared__ u32x4 lds[2][2][NS * 128];                           // [buffer][keys, values]
-  __shared__ f32x4 of_token[2][4][16];                            // [buffer][keys' scale and offset, values'][token / 4]
+  __shared__ f32x4 of_token[2][4][16];                            // [buffer][keys' scales and offsets, values'][token / 4]
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
   const int head = SPLIT ? blockIdx.x % c.heads : blockIdx.x, split = SPLIT ? blockIdx.x / c.heads : 0, seq = blockIdx.z;
   const KvSpan s = kv_span(c, seq, a.rows, a.max_new);
@@ -322,7 +380,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
   const float factor = a.scale * 1.4426950408889634f;
   const uint32_t sixteens = sixteen<TYPE>(), sixteens_v = sixteen<BMX_BF16>();
   u32x4 kr[KN], vr[KN][2];
-  uint32_t pair_in = 0;  // waves 0 and 1: a token's scale and offset, of keys and of values
+  uint32_t pair_in[2] = {};  // wave 0: a token's scale and offset, of keys and of values
   int begin = low_group / kPage, last = kv_pages_to(high_group), used = 1;
   if constexpr (SPLIT) {  // this split's pages: as many for the rows that see few as for those that see most, which then are in fewer splits
     const int pages = max(last - begin, 0), most_pages = kv_pages_to(s.length) - first_seen(token_of((rows - 1) / 128 * 128)) / kPage;
@@ -343,7 +401,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
     // (behind the last page: page 0 once more, which nobody uses)
     const Rsrc r = buffer(c.pages + max(page, 0) * page_bytes + (int64_t)head * 2 * kPage * BYTES, 2 * kPage * BYTES);
     const Rsrc rs = buffer(c.scales + ((int64_t)max(page, 0) * c.heads + head) * 4 * kPage, 8 * kPage);
-    if (wave < 2) pair_in = load4(rs, threadIdx.x * 4 + none, 0);
+    if (wave == 0) pair_in[0] = load4(rs, lane * 4 + none, 0), pair_in[1] = load4(rs, lane * 4 + none, 4 * kPage);
 #pragma unroll
     for (int n = 0; n < KN; ++n) {
       const int i = min(lane / 16 + 4 * n, DC - 1), block = min(wave + 4 * n, DC - 1);
@@ -353,7 +411,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
     }
     return pg;
   };
-  const auto convert = [&](int buf) {
+  const auto convert = [&](int buf, int pg) {
     // keys: 32 values of token 16 wave + lane % 16; values: of a block a pair's even ones or its odd ones, every other four tokens
 #pragma unroll
     for (int n = 0; n < KN; ++n) {
@@ -377,11 +435,21 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
             u32x4{two_levels<BMX_BF16, 0>(x, sixteens_v), two_levels<BMX_BF16, 2>(x, sixteens_v), two_levels<BMX_BF16, 0>(y, sixteens_v), two_levels<BMX_BF16, 2>(y, sixteens_v)};
       }
     }
-    if (wave < 2) {
-      const float scale = bf16_float(pair_in), offset = __builtin_bit_cast(float, pair_in & 0xffff0000u) - 16.0f * scale;
-      float* to = reinterpret_cast<float*>(of_token[buf][2 * wave]) + lane;
-      to[0] = wave ? scale : scale * factor;
-      to[64] = offset;
+    if (wave == 0) {
+      // Those of tokens that nobody has written may be anything, and count as 0.  One that is no finite number, of a value, is left to the score: a weight of 0
+      // times it would spoil the rows that do not see the token too.
+      float scale[2], offset[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t x = pg * kPage + lane < s.length ? pair_in[i] : 0;
+        scale[i] = bf16_float(x), offset[i] = __builtin_bit_cast(float, x & 0xffff0000u);
+      }
+      const bool none = !(fabsf(scale[1]) < INFINITY && fabsf(offset[1]) < INFINITY);
+      float* to = reinterpret_cast<float*>(of_token[buf]) + lane;
+      to[0] = scale[0] * factor;
+      to[64] = none ? NAN : offset[0] - 16.0f * scale[0];
+      to[128] = none ? 0.0f : scale[1];
+      to[192] = none ? 0.0f : offset[1] - 16.0f * scale[1];
     }
   };
   int pg = fetch(begin);
@@ -404,14 +472,15 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
     all += __shfl_xor(all, 32);
     all *= factor;
   }
-  if (pg < last) convert(0);
+  if (pg < last) convert(0, pg);
   __syncthreads();
 
   // (what LDS holds does not come into registers all at once: there are not as many)
   const auto fence = [](bool here) {
-    if (DC > 2 && here) __builtin_amdgcn_sched_barrier(0);
+    if ((DC == 3 || DC > 4 || (DC == 4 && (SPLIT || TYPE == BMX_F16))) && here) __builtin_amdgcn_sched_barrier(0);
   };
-  float m = -INFINITY, l = 0.0f, rest = 0.0f;
+  // held: the score that the row's weights are relative to; limit: from where on over it a score becomes the one
+  float held = 0.0f, limit = -INFINITY, l = 0.0f, rest = 0.0f;
   f32x16 o[DC] = {};
   for (int buf = 0; pg < last; buf ^= 1) {
     const int next = fetch(pg + 1), t0 = pg * kPage;
@@ -423,7 +492,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
         for (int t = 0; t < 2; ++t) z[t] = mfma32<TYPE == BMX_F16>(lds[buf][0][(t * NS + i) * 64 + lane], q[i], z[t]);
         fence(i % 4 == 3);
       }
-      const bool whole = kv_all_in(t0, kPage, low_all, high_all);
+      const bool whole = __builtin_amdgcn_readfirstlane(kv_all_in(t0, kPage, low_all, high_all));
       float top = -INFINITY;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -431,7 +500,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
         for (int j = 0; j < 4; ++j) {
           const f32x4 scale = of_token[buf][0][t * 8 + j * 2 + h], offset = of_token[buf][1][t * 8 + j * 2 + h];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) z[t][4 * j + i] = z[t][4 * j + i] * scale[i] + all * offset[i];
+          for (int i = 0; i < 4; ++i) z[t][4 * j + i] = z[t][4 * j + i] * scale[i] + (all * offset[i] - held);
           fence(j % 2);
         }
       if (!whole) {
@@ -440,29 +509,30 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
           const int t = t0 + i / 4 * 8 + 4 * h + i % 4;
           z[i / 16][i % 16] = t < high && t >= low ? z[i / 16][i % 16] : -INFINITY;
         }
+        apart(z[0]), apart(z[1]);
       }
 #pragma unroll
       for (int i = 0; i < 32; ++i) top = fmaxf(top, z[i / 16][i % 16]);
       top = max_32(top);
-      const float m_new = fmaxf(m, top), m_at = or_zero(m_new), shrink = __builtin_amdgcn_exp2f(m - m_at);
-      m = m_new;
-      u32x4 w[2][4];  // [part][16 tokens]
+      if (__any(top > limit)) {  // (a row's first page, and few others)
+        const bool mine = top > limit;
+        const float up = mine ? top : 0.0f, shrink = limit == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(-up);
+        held += up, limit = mine ? kGrowth : limit;
+        l *= shrink, rest *= shrink;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) z[t] -= up;
+#pragma unroll
+        for (int n = 0; n < DC; ++n) o[n] *= shrink;
+      }
       float sum = 0.0f, more = 0.0f;
+      u32x4 w[2][4];  // [part][16 tokens]
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        f32x4 scale = of_token[buf][2][u * 2 + h], offset = of_token[buf][3][u * 2 + h];
-        if (!whole) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {  // (a token that the row does not see may have any)
-            const int t = t0 + u * 8 + 4 * h + i;
-            const bool sees = t < high && t >= low;
-            scale[i] = sees ? scale[i] : 0.0f, offset[i] = sees ? offset[i] : 0.0f;
-          }
-        }
+        const f32x4 scale = of_token[buf][2][u * 2 + h], offset = of_token[buf][3][u * 2 + h];
         float x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float e = __builtin_amdgcn_exp2f(z[u / 4][u % 4 * 4 + i] - m_at);
+          const float e = __builtin_amdgcn_exp2f(z[u / 4][u % 4 * 4 + i]);
           sum += e;
           more += e * offset[i];
           x[i] = e * scale[i];
@@ -475,22 +545,22 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
         }
         fence(u % 2);
       }
-      l = l * shrink + sum;
-      rest = rest * shrink + more;
-      if (__any(shrink != 1.0f)) {  // (most pages hold no new maximum)
-#pragma unroll
-        for (int n = 0; n < DC; ++n) o[n] *= shrink;
-      }
+      l += sum, rest += more;
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int n = 0; n < DC; ++n) {
-          const u32x4 x = lds[buf][1][(u * DC + n) * 64 + lane];
-          o[n] = mfma32<false>(x, w[1][u], mfma32<false>(x, w[0][u], o[n]));
-          fence(n % 4 == 3);
+        for (int n0 = 0; n0 < DC; n0 += 4) {
+          u32x4 x[4];
+#pragma unroll
+          for (int n = 0; n < 4; ++n) x[n] = n0 + n < DC ? lds[buf][1][(u * DC + n0 + n) * 64 + lane] : u32x4{};
+#pragma unroll
+          for (int part = 0; part < 2; ++part)  // (no product waits for the one before)
+#pragma unroll
+            for (int n = 0; n < 4 && n0 + n < DC; ++n) o[n0 + n] = mfma32<false>(x[n], w[part][u], o[n0 + n]);
+          fence(true);
         }
     }
-    if (next < last) convert(buf ^ 1);
+    if (next < last) convert(buf ^ 1, next);
     pg = next;
     __syncthreads();
   }
@@ -506,7 +576,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
       for (int n = 0; n < DC; ++n)
 #pragma unroll
         for (int i = 0; i < 8; ++i) put(to + (n * 8 + i) * 128, o[n][2 * i] + rest, o[n][2 * i + 1] + rest);
-      put(to + DC * 1024, m, l);
+      put(to + DC * 1024, limit == -INFINITY ? limit : held, l);
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's numbers are there
     __shared__ uint32_t place;
@@ -516,7 +586,8 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
     if (place != (uint32_t)used - 1) return;
     if (threadIdx.x == 0) __hip_atomic_store(a.to.arrived + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (r_wave >= rows) return;
-    m = -INFINITY, l = 0.0f, rest = 0.0f;
+    float m = -INFINITY;
+    l = 0.0f, rest = 0.0f;
     for (int p = 0; p < used; ++p) {
       const float* from = at + (int64_t)p * 4 * PART;
       const u32x2 x = get(from + DC * 1024);
@@ -525,7 +596,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
       const float m_part = __builtin_bit_cast(float, x0), m_new = fmaxf(m, m_part), m_at = or_zero(m_new);
       const float f = __builtin_amdgcn_exp2f(m - m_at), f_part = __builtin_amdgcn_exp2f(m_part - m_at);
       l = l * f + __builtin_bit_cast(float, x1) * f_part;
-      m = m_new;
+      m = m_new, held = m_at;
 #pragma unroll
       for (int n0 = 0; n0 < DC; n0 += N) {
         u32x2 y[N * 8];  // (every read at once: each is a trip to memory)
@@ -572,15 +643,28 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
       }
     }
   if (a.to.lse && h == 0)
-    a.to.lse[to * a.to.q_heads + to_head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    a.to.lse[to * a.to.q_heads + to_head] = l == 0.0f ? -INFINITY : (held + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// What a call needs: tiles of rows, splits, and bytes of the workspace.
+// What a call needs: tiles of rows, parts of their pages, and bytes of the workspace.
 struct Plan {
   int64_t units, tiles, prompt_tiles;  // prompt_tiles: of 128 rows, 0 where they are too few to fill the chip
-  int splits, part_rows, few, prompt_splits;
+  int part_rows, few, prompt_splits;
+  Deal deal;
+  bool deep;  // workgroups of eight waves
   size_t bytes;
 };
+// How the pages of so many tiles are dealt out.  Up to 64 workgroups: over one a CU.  From there on, where lengths differ, 384, half of what the chip holds, with which
+// a part takes about as long as all bytes do; but not those that are no longer than others by less than a join takes.  Tiles that fill the chip are split where they
+// are far longer than the others only.  (Heads of 128 bf16, 8 of the cache, us with 256, 384, 512 workgroups: 16 sequences of up to 16000 tokens 51, 42, 45, unsplit 60; 48 of
+// up to 8000 71, 55, 64, unsplit 79; 32 of 2000 each 19.8, 19.7, 23.7; 16 of 4000 each, four new tokens 25, 28, 25; 64 of up to 4096 44.5, 45.7, 48.6, unsplit 44.)
+Deal deal_of(int64_t units, int64_t heads, int64_t table_width) {
+  if (units == 0 || units > kMostUnits || units * heads > kMostPlaces || table_width <= kWholePages || units * table_width >= 1 << 30) return {0, 0, 0};
+  const int64_t fill = units * heads, most = std::min<int64_t>(units * ceil_div(table_width, kLeastPart), kMostSplits) - 1;
+  const auto extra = [&](int64_t places) { return (int)std::min(ceil_div(places, heads) - 1, most); };
+  const Deal d = {extra(fill > 64 && fill < kPlaces ? 384 : 256), extra(256), fill < 256 ? 4 : 14};
+  return d.even > 0 ? d : Deal{0, 0, 0};
+}
 Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new, int type) {
   Plan p;
   int64_t rows = max_new * (q_heads / heads);
@@ -593,12 +677,11 @@ Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads
   }
   const size_t line = (kv4_row_bytes((int)dim) * 2 + 4) * 4;
   p.tiles = ceil_div(rows, 16);
-  p.units = sequences * heads * p.tiles;
+  p.units = sequences * p.tiles;
   p.part_rows = (int)std::min<int64_t>(rows, 16);
-  // one workgroup for each of the chip's 256 CUs, but four pages of the longest sequence for each at least
-  p.splits = (int)std::max<int64_t>(std::min({ceil_div(256, std::max<int64_t>(p.units, 1)), ceil_div(table_width, 4), (int64_t)kMostSplits}), 1);
-  if (p.units > kCounters) p.splits = 1;
-  p.bytes = p.splits == 1 ? 0 : kCounters * 4 + (size_t)p.units * p.splits * p.part_rows * line;
+  p.deal = deal_of(p.units, heads, table_width);
+  p.deep = p.deal.extra > 0 && p.units == 1 && table_width >= 16 * (p.deal.extra + 1);
+  p.bytes = p.deal.extra == 0 ? 0 : kCounters * 4 + (size_t)(p.units + p.deal.extra) * heads * p.part_rows * line;
   p.prompt_splits = 1;
   if (p.prompt_tiles) {
     const int64_t units = p.prompt_tiles * heads * sequences;
@@ -613,9 +696,13 @@ template <int TYPE, int DC>
 void launch(const bmx_kv4_cache& c, const Args& a, const Plan& p, hipStream_t s) {
   // (rows of sequences as long as each other are all many or all few)
   if (!p.prompt_tiles || (c.starts && c.sequences > 1)) {
-    const dim3 grid(c.heads * p.splits, (uint32_t)p.tiles, c.sequences);
-    launch_kernel(kv4_attention_kernel<TYPE, DC>, grid, dim3(kWaves * 64), 0, s, c, a);
-    note_kernel("kv4_attention_kernel<%d,%d> grid %ux%ux%u block %d", TYPE, DC, grid.x, grid.y, grid.z, kWaves * 64);
+    const dim3 grid = p.deal.extra ? dim3((uint32_t)(c.heads * (p.units + p.deal.extra))) : dim3(c.heads, (uint32_t)p.tiles, c.sequences);
+    int waves = 4;
+    auto kern = kv4_attention_kernel<TYPE, DC, 4>;
+    if constexpr (DC <= 4)  // (beyond 128 values eight waves' registers do not fit)
+      if (p.deep) kern = kv4_attention_kernel<TYPE, DC, 8>, waves = 8;
+    launch_kernel(kern, grid, dim3(waves * 64), 0, s, c, a);
+    note_kernel("kv4_attention_kernel<%d,%d,%d> grid %ux%ux%u block %d", TYPE, DC, waves, grid.x, grid.y, grid.z, waves * 64);
   }
   if constexpr (TYPE != BMX_F32) {
     if (p.prompt_tiles) {
@@ -640,14 +727,15 @@ __global__ void clear_kernel(uint32_t* p) { p[blockIdx.x * 256 + threadIdx.x] = 
 }  // namespace
 
 size_t kv4_attention_workspace(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new) {
-  // The largest of the calls' bytes, which first grow with the rows and then, where rows fill the chip without splits, fall.  In closed form: of
-  // `each` units a tile, and splits that bring t tiles to 256 workgroups, each * t * splits <= 255 + each * t while that is worth a split.
+  // The largest of the calls' bytes.  Of 16 rows a part: that of any number of tiles, of which each sequence has as many.
   const int64_t each = sequences * heads, rows = max_new > 0 ? std::min(max_new * (q_heads / heads), kMostTiles * 16) : kMostTiles * 16;
   const size_t line = (kv4_row_bytes((int)dim) * 2 + 4) * 4;
   size_t most = 0;
   if (each == 0) return 0;
-  const int64_t units = each * std::min(ceil_div(rows, 16), 255 / each), splits = std::min<int64_t>(ceil_div(table_width, 4), kMostSplits);
-  if (units > 0 && splits > 1) most = std::min(units * splits, units + 255) * std::min<int64_t>(rows, 16) * line;
+  for (int64_t tiles = 1; tiles <= std::min(ceil_div(rows, 16), (int64_t)kMostUnits); ++tiles) {
+    const int64_t extra = deal_of(sequences * tiles, heads, table_width).extra;
+    if (extra > 0) most = std::max<size_t>(most, (sequences * tiles + extra) * heads * std::min<int64_t>(rows, 16) * line);
+  }
   const int64_t places = dim <= 128 ? 512 : 256, tiles = each * std::min(ceil_div(rows, 128), places / 2 / each);
   if (rows > 64 && tiles >= kLeastTiles && table_width / kLeastPages > 1)
     most = std::max<size_t>(most, std::min(places, tiles * (table_width / kLeastPages)) * 128 * line);
@@ -667,9 +755,9 @@ hipError_t launch_kv4_attention(const bmx_kv4_cache& c, const void* q, int type,
   const bool aligned = (uintptr_t)q % 16 == 0 && q_row * size % 16 == 0 && q_head * size % 16 == 0;
   const Plan p = plan(c.sequences, c.table_width, c.heads, q_heads, c.dim, max_new, type);
   uint32_t* arrived = static_cast<uint32_t*>(workspace);
-  const Args a = {q, q_row, q_head, {out, out_row, out_head, lse, reinterpret_cast<float*>(arrived + kCounters), arrived, q_heads, q_heads / c.heads, p.splits, p.part_rows},
-                  rows, max_new, window, p.prompt_splits, p.few, causal, aligned, scale};
-  const int64_t counters = std::max(p.splits > 1 ? p.units : 0, p.prompt_splits > 1 ? p.prompt_tiles * c.heads * c.sequences : 0);
+  const Args a = {q, q_row, q_head, {out, out_row, out_head, lse, reinterpret_cast<float*>(arrived + kCounters), arrived, q_heads, q_heads / c.heads, p.part_rows},
+                  rows, max_new, window, p.prompt_splits, (int)p.units, (int)p.tiles, p.deal, p.few, causal, aligned, scale};
+  const int64_t counters = std::max(p.deal.extra ? p.units * c.heads : 0, p.prompt_splits > 1 ? p.prompt_tiles * c.heads * c.sequences : 0);
   if (fresh && counters) launch_kernel(clear_kernel, dim3((uint32_t)ceil_div(counters, 256)), dim3(256), 0, s, arrived);
   const auto f = type == BMX_F32 ? launch_typed<BMX_F32> : type == BMX_F16 ? launch_typed<BMX_F16> : launch_typed<BMX_BF16>;
   f(c, a, p, s);
