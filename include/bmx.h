@@ -389,7 +389,7 @@ typedef struct bmx_kv4_cache {
 /* Calls on it, with the arguments of the cache of 8 bits.
  * bmx_kv4_write: quantises the rows into the cache, at each sequence's last positions: o = the least of a token's head's values and s = (the largest - o) / 15,
  *   rounded to bf16 (a difference beyond fp32 counts as its largest number, one below 0, by o's rounding, as 0), levels round((x - o) / s), to the nearest, ties to even, 0 to 15, all 0 where s
- *   is 0.  Both are taken over finite values; infinity is level 15, -infinity and NaN level 0.  No other token changes.
+ *   < 2^-126.  Both are taken over finite values; infinity is level 15, -infinity and NaN level 0.  No other token changes.
  * bmx_kv4_read: the rows' values q * s + o, one rounding to fp32, then to the type; rows of tokens that are not there are zeros.
  * bmx_kv4_attention: as bmx_kv_attention; workspace by BMX_OP_KV4_ATTENTION with the same numbers.  Either cache's workspace may be any stream's own, not
  *   two streams' (nor two graphs' that run at once).  A row that sees a token whose scale or offset is no finite number has results that are none either. */

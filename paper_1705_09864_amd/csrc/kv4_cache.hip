@@ -22,9 +22,24 @@ __device__ inline uint32_t pair_of(float low, float high) {
 }
 __device__ inline float scale_of(uint32_t p) { return bf16_float(p & 0xffff); }
 __device__ inline float offset_of(uint32_t p) { return __builtin_bit_cast(float, p & 0xffff0000u); }
-// The level of x; 0 of a NaN and where s is 0.
-__device__ inline uint32_t level(float x, float s, float o) {
-  return s > 0.0f ? (uint32_t)fminf(fmaxf(rintf((x - o) / s), 0.0f), 15.0f) : 0;
+// (the instruction itself: it makes 0 of a NaN and of what is below 0, of which C++ has no conversion)
+__device__ inline uint32_t to_uint(float x) {
+  uint32_t i;
+  asm("v_cvt_u32_f32 %0, %1" : "=v"(i) : "v"(x));
+  return i;
+}
+// The level of x, r = 1 / s, or 0 where s is 0: the quotient's nearest whole number n, and with what is left of it the quotient again, n + (x - o - n s) / s, in which
+// a quotient halfway between two levels is just that (the remainder is exact, r off by half a bit at most), so that it goes to the even one as in a division.
+// Infinities: n stays 16, and what is left is infinite.
+__device__ inline uint32_t level(float x, float s, float o, float r) {
+  const float d = x - o, n = rintf(fminf(d * r, 16.0f));
+  return min(to_uint(rintf(__builtin_fmaf(__builtin_fmaf(-n, s, d), r, n))), 15u);
+}
+__device__ inline float inverse(float s) { return s >= 0x1p-126f ? 1.0f / s : 0.0f; }
+// The same in the low bits, for values and differences that are finite: whole numbers are the last bits of numbers from 2^23 on, where a sum rounds to them as rint does.
+__device__ inline uint32_t quick_level(float x, float s, float o, float r) {
+  const float d = x - o, t = __builtin_fmaf(d, r, 0x1p23f);
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(__builtin_fmaf(__builtin_fmaf(0x1p23f - t, s, d), r, t), 0x1p23f, 0x1p23f + 15.0f));
 }
 __device__ inline float value_of(uint32_t q, uint32_t p) { return __builtin_fmaf((float)q, scale_of(p), offset_of(p)); }
 
@@ -75,11 +90,19 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(bmx_kv4_cache c, const v
     const int e = threadIdx.x + 256 * i, t = e / CHUNKS, d = e % CHUNKS * 16, left = c.dim - d;
     const bool there = t >= p.t0 && t < p.t1 && d < c.dim;
     float low = INFINITY, high = -INFINITY;
+    bool odd = false;  // values that are infinite
     if (there) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
-        const float y = r[i].get(j);
-        if (left >= 16 || j < left) low = least(low, y), high = largest(high, y);
+        const float y = left >= 16 || j < left ? r[i].get(j) : NAN;  // (both pass over it)
+        low = fminf(low, y), high = fmaxf(high, y);
+      }
+      odd = low == -INFINITY || high == INFINITY;
+      if (odd) {
+        low = INFINITY, high = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (left >= 16 || j < left) low = least(low, r[i].get(j)), high = largest(high, r[i].get(j));
       }
     }
 #pragma unroll
@@ -87,10 +110,25 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(bmx_kv4_cache c, const v
     if (!there) continue;
     const uint32_t pair = pair_of(low, high);
     if (d == 0) p.pairs[t] = pair;
-    const float s = scale_of(pair), o = offset_of(pair);
+    const float s = scale_of(pair), o = offset_of(pair), of_s = inverse(s);
     uint32_t w[2] = {};
+    if (odd || high - low > 0x1p126f) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) w[j / 8] |= (left >= 16 || j < left ? level(r[i].get(j), s, o) : 0) << (4 * (j % 8));
+      for (int j = 0; j < 16; ++j) w[j / 8] |= level(r[i].get(j), s, o, of_s) << (4 * (j % 8));
+    } else {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        uint32_t b[4];  // two levels in the low byte
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          b[j] = quick_level(r[i].get(8 * n + 2 * j), s, o, of_s) | quick_level(r[i].get(8 * n + 2 * j + 1), s, o, of_s) << 4;
+        w[n] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
+      }
+    }
+    if (left < 16) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) w[j / 8] &= j < left ? 0xffffffffu : ~(15u << (4 * (j % 8)));
+    }
     if (which == 0) {
       *reinterpret_cast<u32x2*>(p.body + kv4_key_at(row, t, d)) = u32x2{w[0], w[1]};
     } else {
@@ -164,7 +202,8 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(bmx_kv4_cache c, const 
   for (int n = 0; n < 2; ++n) {
     const int d = 128 * n + 2 * lane;
     if (d >= c.dim) continue;
-    const uint32_t q = level(y[n][0], scale_of(pair), offset_of(pair)) | (d + 1 < c.dim ? level(y[n][1], scale_of(pair), offset_of(pair)) : 0) << 4;
+    const float sc = scale_of(pair), o = offset_of(pair), r = inverse(sc);
+    const uint32_t q = level(y[n][0], sc, o, r) | (d + 1 < c.dim ? level(y[n][1], sc, o, r) : 0) << 4;
     body[which ? kv4_value_at(t, d) : kv4_key_at(row, t, d)] = (uint8_t)q;
   }
 }
@@ -199,16 +238,24 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(bmx_kv4_cache c, void* k,
     }
   } else {
     // tokens 16 u + 4 wave + i, columns d and d + 1
+    u32x4 pairs[4] = {}, q[PAIRS] = {};
+    if (there) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) pairs[u] = *reinterpret_cast<const u32x4*>(p.pairs + 16 * u + 4 * wave);
+#pragma unroll
+      for (int n = 0; n < PAIRS; ++n) {
+        const int d = (lane + 64 * n) * 2;
+        if (d < c.dim) q[n] = *reinterpret_cast<const u32x4*>(p.body + d / 32 * 1024 + wave * 256 + d % 32 / 2 * 16);
+      }
+    }
 #pragma unroll
     for (int n = 0; n < PAIRS; ++n) {
       const int d = (lane + 64 * n) * 2;
       if (d >= c.dim) continue;
-      u32x4 q = {};
-      if (there) q = *reinterpret_cast<const u32x4*>(p.body + d / 32 * 1024 + wave * 256 + d % 32 / 2 * 16);
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
         const int t = j / 4 * 16 + 4 * wave + j % 4;
-        const uint32_t b = q[j / 4] >> (8 * (j % 4)), pair = there ? p.pairs[t] : 0;
+        const uint32_t b = q[n][j / 4] >> (8 * (j % 4)), pair = pairs[j / 4][j % 4];
         Run<TYPE, 2> x;
         x.set2(0, value_of(b & 15, pair), value_of(b >> 4 & 15, pair));
         if (t >= p.t0 && t < p.t1) x.store(v, p.base + t * x_row + d, c.dim - d);
