@@ -1,9 +1,9 @@
 // Which pages of a cache are whose, on the GPU: sequences grow by tokens or lose some, pages that they no longer reach go onto the stack of free
 // ones and those that they come to reach are taken from its top, and each new row learns its position and its place in the cache.
-// All of it follows from prefix sums over the sequences (pages given back, pages taken, new rows), so one workgroup does it; the rows' maps
-// of long prompts are a second launch of many.  In order of the sequences, pages given back first: the result does not depend on timing.
+// All of it follows from prefix sums over the sequences (pages given back, pages taken, new rows), which a workgroup makes in a microsecond.  In order of the
+// sequences, pages given back first: the result does not depend on timing.
 //
-// Bound by latency: a chain of the lengths, the sums, the stack and the table, each behind the one before.
+// Bound by latency: a chain of the lengths, the sums, the stack or the table, each behind the one before, with little code, which a launch reads from memory too.
 #include "bmx_internal.h"
 #include "few_bits.h"
 
@@ -22,175 +22,275 @@ struct Args {
   int32_t* positions;  // or null, like slots
   int64_t* slots;
   int sequences, table_width, num_pages, rows;
+  bool wide;  // positions and slots lie on 16 bytes
 };
 
-// The number of the first of n ascending numbers that is more than x, n if none is.
-__device__ inline int first_above(const int32_t* p, int n, int x) {
-  int low = 0, high = n;
-  while (low < high) {
-    const int mid = (low + high) / 2;
-    if (p[mid] > x) high = mid;
-    else low = mid + 1;
-  }
-  return low;
+// Sums of numbers that are not negative, 2^32 - 1 where they are more.
+__device__ inline uint32_t plus(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+template <int CTRL, int ROWS>
+__device__ inline uint32_t plus_lane(uint32_t x) { return plus(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false)); }
+// Those over the lanes up to each.
+__device__ inline uint32_t sums_to(uint32_t x) {
+  x = plus_lane<0x118, 0xf>(plus_lane<0x114, 0xf>(plus_lane<0x112, 0xf>(plus_lane<0x111, 0xf>(x))));  // a row of 16: 1, 2, 4, 8 to the left
+  return plus_lane<0x143, 0xc>(plus_lane<0x142, 0xa>(x));  // a row's last into the next, the second row's into the two behind it
 }
 
-// A row that is sequence i's, `at` rows behind its first, which stands at position `first`.
-__device__ inline void put_row(const Args& a, int r, int i, int pos) {
+// How many of n ascending numbers are not above x.
+template <class P>
+__device__ inline int not_above(const P p, int n, uint32_t x) {
+  int found = 0;
+  for (int by = 1 << (31 - __builtin_clz(n | 1)); by; by >>= 1)
+    if (found + by <= n && (uint32_t)p[found + by - 1] <= x) found += by;
+  return found;
+}
+
+__device__ inline void put_row(const Args& a, int r, int pos, int page) {
   if (a.positions) a.positions[r] = pos;
-  if (a.slots) a.slots[r] = pos < 0 ? -1 : (int64_t)a.table[i * a.table_ld + (pos >> kLogPage)] * kPage + (pos & (kPage - 1));
+  if (a.slots) a.slots[r] = pos < 0 ? -1 : (int64_t)page * kPage + (pos & (kPage - 1));
 }
 
-constexpr int kMostInOne = 4;  // rows a thread that the kernel itself maps
+constexpr int kMostInOne = 2;  // rows a thread up to which one workgroup does it all
+enum Part { kAll, kMoves, kState };
 
-// THREADS sequences at a time.  ONE: there are no more, and what a sequence needs stays in registers.
-template <int THREADS, bool ONE>
+// What all kernels begin with, THREADS sequences at a time: the sums, and whether everything has room.
+template <int THREADS>
+struct Sums {
+  static constexpr int WAVES = THREADS / 64;
+  uint32_t back_to[THREADS], take_to[THREADS], more_to[THREADS];  // of pages given back, pages taken, new rows: up to each sequence
+  int32_t pages_of[THREADS], first_of[THREADS];                   // its pages and tokens before the call
+  uint32_t of_wave[3][WAVES];
+  int first_bad;
+};
+
+// THREADS sequences or fewer; what one needs stays in registers.  kAll: one workgroup does everything.  Otherwise kMoves, any number of workgroups that move pages and map rows
+// between them, each on sums of its own, and behind it kState, one that brings lengths and pool up to date.
+// A page that is taken comes from the stack, or, if it is given back in this call, from where the table has it: pages go both ways at once.
+template <int THREADS, Part PART>
 __global__ __launch_bounds__(THREADS) void kv_resize_kernel(Args a) {
-  constexpr int WAVES = THREADS / 64;
-  __shared__ int32_t back_to[THREADS], take_to[THREADS], more_to[THREADS], pages_of[THREADS], first_of[THREADS];
-  __shared__ int64_t sums[3][WAVES];
-  __shared__ int first_bad;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  __shared__ Sums<THREADS> s;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, n = a.sequences;
   const int free = a.pool[0];
-  if (tid == 0) first_bad = 0x7fffffff;
-
+  if (tid == 0) s.first_bad = 0x7fffffff;
   KvChange c = {};
-  int tokens = 0;
-  const auto load = [&](int i) {
-    c = {};
-    if (i >= a.sequences) {
-      c.fits = true;
-      return;
-    }
-    tokens = a.lengths[i];
-    c = kv_change_of(tokens, a.change[i], a.table_width);
-  };
-  // each thread's sums up to its own numbers over the workgroup, and (in all) the workgroup's
-  const auto scan = [&](int64_t (&v)[3], int64_t (&all)[3]) {
-#pragma unroll
-    for (int k = 0; k < 3; ++k)
-      for (int o = 1; o < 64; o *= 2) {
-        const int64_t x = __shfl_up(v[k], o);
-        if (lane >= o) v[k] += x;
-      }
-    __syncthreads();  // (the sums of the step before are read)
-    if (lane == 63)
-      for (int k = 0; k < 3; ++k) sums[k][wave] = v[k];
-    __syncthreads();
-    for (int k = 0; k < 3; ++k) {
-      all[k] = 0;
-      for (int w = 0; w < WAVES; ++w) {
-        if (w == wave) v[k] += all[k];
-        all[k] += sums[k][w];
-      }
-    }
-  };
-  const auto mine = [&](int64_t (&v)[3]) { v[0] = max(c.pages - c.pages_then, 0), v[1] = max(c.pages_then - c.pages, 0), v[2] = c.more; };
-
-  // all pages that come back
-  int64_t v[3], all[3], back = 0;
-  for (int base = 0; base < a.sequences; base += THREADS) {
-    load(base + tid);
-    mine(v);
-    scan(v, all);
-    back += all[0];
+  c.fits = true;
+  if (tid < n) {
+    const int tokens = a.lengths[tid];
+    c = kv_change_of(tokens, a.change[tid], a.table_width);
+    s.pages_of[tid] = c.pages, s.first_of[tid] = tokens;
   }
-  // whether everything has room
-  const bool pool_is_one = free >= 0 && free <= a.num_pages && free + back <= a.num_pages;
-  int64_t before[3] = {};
-  const int64_t room = free + back;
-  for (int base = 0; base < a.sequences; base += THREADS) {
-    if (!ONE) {
-      load(base + tid);
-      mine(v);
-      scan(v, all);
-    }
-    if (!c.fits || before[1] + v[1] > room || before[2] + v[2] > a.rows) atomicMin(&first_bad, base + tid);
-    for (int k = 1; k < 3; ++k) before[k] += all[k];
+  uint32_t v[3] = {(uint32_t)max(c.pages - c.pages_then, 0), (uint32_t)max(c.pages_then - c.pages, 0), (uint32_t)c.more}, all[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    v[k] = sums_to(v[k]);
+    if (lane == 63) s.of_wave[k][wave] = v[k];
   }
   __syncthreads();
-  const int bad = first_bad;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const uint32_t to = sums_to(lane < Sums<THREADS>::WAVES ? s.of_wave[k][lane % Sums<THREADS>::WAVES] : 0);
+    all[k] = __builtin_amdgcn_readlane(to, 63);
+    if (wave > 0) v[k] = plus(v[k], __builtin_amdgcn_readlane(to, __builtin_amdgcn_readfirstlane(max(wave - 1, 0))));
+  }
+  const bool pool_is_one = free >= 0 && free <= a.num_pages && (int64_t)free + all[0] <= a.num_pages;
+  const uint32_t room = pool_is_one ? free + all[0] : 0, rows = a.rows;
+  s.back_to[tid] = v[0], s.take_to[tid] = v[1], s.more_to[tid] = v[2];
+  if (!c.fits || v[1] > room || v[2] > rows) atomicMin(&s.first_bad, tid);
+  __syncthreads();
+  const int bad = s.first_bad;
+  const bool refused = bad != 0x7fffffff || !pool_is_one;
+  if (PART != kMoves) {
+    if (tid == 0) a.pool[1] = !pool_is_one ? -1 : refused ? bad + 1 : 0;
+    if (!refused) {
+      if (tid == 0) a.pool[0] = (int)(room - all[1]);
+      if (tid < n) a.lengths[tid] = c.tokens_then;
+    }
+  }
+  if (PART == kState) return;
+  if (blockIdx.x == 0) {
+    if (tid == 0) a.starts[0] = 0;
+    if (tid < n) a.starts[tid + 1] = refused ? 0 : (int)v[2];
+  }
+  int32_t* const stack = a.pool + 2;
+  // the k-th page given back: where the table has it; the k-th taken: its number
+  const auto given = [&](uint32_t k) {
+    const int i = not_above(s.back_to, n, k);
+    return a.table + i * a.table_ld + s.pages_of[i] - 1 - (int)(k - (i ? s.back_to[i - 1] : 0));
+  };
+  const auto taken = [&](uint32_t k) { return room - 1 - k < (uint32_t)free ? stack[room - 1 - k] : *given(room - 1 - k - free); };
+  // Pages given back, pages taken and rows are one another's equals, and a thread has one of them at a time.  EACH rows behind one another to a thread: mostly of one
+  // sequence and one page.
+  constexpr int EACH = PART == kAll ? 1 : 4;
+  const uint64_t back = refused ? 0 : all[0], moves = back + (refused ? 0 : all[1]), items = moves + (rows + EACH - 1) / EACH;
+  for (uint64_t e = blockIdx.x * THREADS + tid; e < items; e += gridDim.x * THREADS) {
+    if (e < back) {
+      stack[free + e] = *given((uint32_t)e);
+      continue;
+    }
+    if (e < moves) {
+      const uint32_t k = (uint32_t)(e - back);
+      const int i = not_above(s.take_to, n, k);
+      a.table[i * a.table_ld + s.pages_of[i] + (int)(k - (i ? s.take_to[i - 1] : 0))] = taken(k);
+      continue;
+    }
+    const uint32_t r0 = (uint32_t)(e - moves) * EACH;
+    int i = refused ? n : not_above(s.more_to, n, r0), held = -1, page = 0, pos[EACH];
+    int64_t slot[EACH];
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const uint32_t r = r0 + j;
+      if (j > 0)
+        while (i < n && s.more_to[i] <= r) ++i, held = -1;
+      pos[j] = -1, slot[j] = -1;
+      if (i < n && r < rows) {
+        pos[j] = s.first_of[i] + (int)(r - (i ? s.more_to[i - 1] : 0));
+        const int at = pos[j] >> kLogPage, beyond = at - s.pages_of[i];  // (a new page is not read from the table, which other threads write)
+        if (at != held) page = beyond < 0 ? a.table[i * a.table_ld + at] : taken((i ? s.take_to[i - 1] : 0) + beyond);
+        held = at;
+        slot[j] = (int64_t)page * kPage + (pos[j] & (kPage - 1));
+      }
+    }
+    if (EACH == 4 && a.wide && r0 + EACH <= rows) {
+      struct __attribute__((aligned(16))) Four { int32_t x[4]; };
+      struct __attribute__((aligned(16))) Two { int64_t x[2]; };
+      if (a.positions) *reinterpret_cast<Four*>(a.positions + r0) = Four{pos[0], pos[1 % EACH], pos[2 % EACH], pos[3 % EACH]};
+      if (a.slots) {
+        reinterpret_cast<Two*>(a.slots + r0)[0] = Two{slot[0], slot[1 % EACH]};
+        reinterpret_cast<Two*>(a.slots + r0)[1] = Two{slot[2 % EACH], slot[3 % EACH]};
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) {
+        if (r0 + j >= rows) break;
+        if (a.positions) a.positions[r0 + j] = pos[j];
+        if (a.slots) a.slots[r0 + j] = slot[j];
+      }
+    }
+  }
+}
+
+// More sequences than threads: one workgroup over and over, the pages first all onto the stack and then from there; the rows' maps by kv_slots_kernel.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void kv_resize_many_kernel(Args a) {
+  __shared__ Sums<THREADS> s;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int free = a.pool[0];
+  if (tid == 0) s.first_bad = 0x7fffffff;
+  KvChange c = {};
+  int tokens = 0;
+  uint32_t v[3], all[3];
+  const auto sum = [&](int i) {
+    c = {};
+    c.fits = true;
+    if (i < a.sequences) {
+      tokens = a.lengths[i];
+      c = kv_change_of(tokens, a.change[i], a.table_width);
+    }
+    v[0] = max(c.pages - c.pages_then, 0), v[1] = max(c.pages_then - c.pages, 0), v[2] = c.more;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) v[k] = sums_to(v[k]);
+    __syncthreads();  // (what the step before left is read)
+    if (lane == 63)
+#pragma unroll
+      for (int k = 0; k < 3; ++k) s.of_wave[k][wave] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const uint32_t to = sums_to(lane < Sums<THREADS>::WAVES ? s.of_wave[k][lane % Sums<THREADS>::WAVES] : 0);
+      all[k] = __builtin_amdgcn_readlane(to, 63);
+      if (wave > 0) v[k] = plus(v[k], __builtin_amdgcn_readlane(to, __builtin_amdgcn_readfirstlane(max(wave - 1, 0))));
+    }
+  };
+  uint32_t back = 0;
+  for (int base = 0; base < a.sequences; base += THREADS) {
+    sum(base + tid);
+    back = plus(back, all[0]);
+  }
+  const bool pool_is_one = free >= 0 && free <= a.num_pages && (int64_t)free + back <= a.num_pages;
+  const uint32_t room = pool_is_one ? free + back : 0;
+  uint32_t taken = 0, rows = 0;
+  for (int base = 0; base < a.sequences; base += THREADS) {
+    sum(base + tid);
+    if (!c.fits || plus(taken, v[1]) > room || plus(rows, v[2]) > (uint32_t)a.rows) atomicMin(&s.first_bad, base + tid);
+    taken = plus(taken, all[1]), rows = plus(rows, all[2]);
+  }
+  __syncthreads();
+  const int bad = s.first_bad;
   if (bad != 0x7fffffff || !pool_is_one) {
     if (tid == 0) a.pool[1] = pool_is_one ? bad + 1 : -1;
     for (int i = tid; i <= a.sequences; i += THREADS) a.starts[i] = 0;
-    if (ONE && a.rows <= kMostInOne * THREADS)
-      for (int r = tid; r < a.rows; r += THREADS) put_row(a, r, 0, -1);
     return;
   }
-  const int64_t taken = before[1];
   if (tid == 0) {
     a.pool[0] = (int)(room - taken);
     a.pool[1] = 0;
     a.starts[0] = 0;
   }
   int32_t* const stack = a.pool + 2;
-  // pages back onto the stack, from there into the table
   for (int way = 0; way < 2; ++way) {
-    int64_t at = 0, rows = 0;  // pages and rows of the sequences before these
+    uint32_t at = 0, row = 0;  // pages and rows of the sequences before these
     for (int base = 0; base < a.sequences; base += THREADS) {
       const int n = min(a.sequences - base, THREADS);
-      if (!ONE) {
-        load(base + tid);
-        mine(v);
-        scan(v, all);
+      sum(base + tid);
+      uint32_t* const to = s.back_to;
+      to[tid] = way ? v[1] : v[0], s.pages_of[tid] = c.pages;
+      __syncthreads();
+      const uint32_t count = way ? all[1] : all[0];
+      for (uint32_t k = tid; k < count; k += THREADS) {
+        const int i = not_above(to, n, k), by = (int)(k - (i ? to[i - 1] : 0));
+        int32_t* const line = a.table + (base + i) * a.table_ld + s.pages_of[i];
+        if (way) line[by] = stack[room - 1 - at - k];
+        else stack[free + at + k] = line[-1 - by];
       }
-      if (!ONE || way == 0) {
-        back_to[tid] = (int)v[0], take_to[tid] = (int)v[1], more_to[tid] = (int)(rows + v[2]), pages_of[tid] = c.pages, first_of[tid] = tokens;
-        __syncthreads();
-      }
-      if (way == 0) {
-        for (int k = tid; k < all[0]; k += THREADS) {
-          const int i = first_above(back_to, n, k), from = i ? back_to[i - 1] : 0;
-          stack[free + at + k] = a.table[(base + i) * a.table_ld + pages_of[i] - 1 - (k - from)];
-        }
-        at += all[0];
-      } else {
-        for (int k = tid; k < all[1]; k += THREADS) {
-          const int i = first_above(take_to, n, k), from = i ? take_to[i - 1] : 0;
-          a.table[(base + i) * a.table_ld + pages_of[i] + (k - from)] = stack[room - 1 - at - k];
-        }
-        at += all[1];
+      at += count;
+      if (way) {
         if (base + tid < a.sequences) {
           a.lengths[base + tid] = c.tokens_then;
-          a.starts[base + tid + 1] = (int)(rows + v[2]);
+          a.starts[base + tid + 1] = (int)(row + v[2]);
         }
-        rows += all[2];
+        row += all[2];
       }
-      if (!ONE) __syncthreads();  // (the next sequences' sums come into the same memory)
     }
     __syncthreads();
-  }
-  if (ONE && a.rows <= kMostInOne * THREADS) {
-    for (int r = tid; r < a.rows; r += THREADS) {
-      const int i = first_above(more_to, a.sequences, r);
-      put_row(a, r, i, i < a.sequences ? first_of[i] + r - (i ? more_to[i - 1] : 0) : -1);
-    }
   }
 }
 
 __global__ __launch_bounds__(256) void kv_slots_kernel(Args a) {
   const int r = blockIdx.x * 256 + threadIdx.x;
   if (r >= a.rows) return;
-  const int i = first_above(a.starts + 1, a.sequences, r);
-  put_row(a, r, i, i < a.sequences ? a.lengths[i] - (a.starts[i + 1] - r) : -1);
+  const int i = not_above(a.starts + 1, a.sequences, r);
+  if (i == a.sequences) return put_row(a, r, -1, 0);
+  const int pos = a.lengths[i] - (a.starts[i + 1] - r);
+  put_row(a, r, pos, a.table[i * a.table_ld + (pos >> kLogPage)]);
 }
 
-template <int THREADS, bool ONE>
+template <int THREADS>
 void launch(const Args& a, hipStream_t s) {
-  launch_kernel(kv_resize_kernel<THREADS, ONE>, dim3(1), dim3(THREADS), 0, s, a);
-  note_kernel("kv_resize_kernel<%d,%d> grid 1 block %d", THREADS, ONE, THREADS);
-  if ((!ONE || a.rows > kMostInOne * THREADS) && a.rows > 0 && (a.positions || a.slots))
-    launch_kernel(kv_slots_kernel, dim3((uint32_t)ceil_div(a.rows, 256)), dim3(256), 0, s, a);
+  if (a.rows <= kMostInOne * THREADS) {
+    launch_kernel(kv_resize_kernel<THREADS, kAll>, dim3(1), dim3(THREADS), 0, s, a);
+    note_kernel("kv_resize_kernel<%d,%d> grid 1 block %d", THREADS, (int)kAll, THREADS);
+    return;
+  }
+  const uint32_t grid = (uint32_t)std::min<int64_t>(ceil_div(a.rows, 4 * THREADS) * 9 / 8 + 1, 512);  // (and some for pages)
+  launch_kernel(kv_resize_kernel<THREADS, kMoves>, dim3(grid), dim3(THREADS), 0, s, a);
+  launch_kernel(kv_resize_kernel<THREADS, kState>, dim3(1), dim3(THREADS), 0, s, a);
+  note_kernel("kv_resize_kernel<%d,%d> grid %u block %d", THREADS, (int)kMoves, grid, THREADS);
 }
 
 }  // namespace
 
 hipError_t launch_kv_resize(const int32_t* change, int sequences, int32_t* table, int64_t table_ld, int table_width, int32_t* lengths, int32_t* pool,
                             int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int rows, hipStream_t s) {
-  const Args a = {change, table, table_ld, lengths, pool, starts, positions, slots, sequences, table_width, num_pages, rows};
-  if (sequences <= 256) launch<256, true>(a, s);
-  else if (sequences <= 1024) launch<1024, true>(a, s);
-  else launch<1024, false>(a, s);
+  const Args a = {change, table, table_ld, lengths, pool, starts, positions, slots, sequences, table_width, num_pages, rows,
+                  (uintptr_t)positions % 16 == 0 && (uintptr_t)slots % 16 == 0};
+  if (sequences <= 256) {
+    launch<256>(a, s);
+  } else if (sequences <= 1024) {
+    launch<1024>(a, s);
+  } else {
+    launch_kernel(kv_resize_many_kernel<1024>, dim3(1), dim3(1024), 0, s, a);
+    note_kernel("kv_resize_many_kernel<1024> grid 1 block 1024");
+    if (rows > 0 && (positions || slots)) launch_kernel(kv_slots_kernel, dim3((uint32_t)ceil_div(rows, 256)), dim3(256), 0, s, a);
+  }
   return launch_error();
 }
 
