@@ -130,8 +130,10 @@ void launch(const Args& a, hipStream_t s) {
   const bool wide = (PAIR ? whole(2 * a.half) : whole(a.half)) && (!a.copy || whole(a.dim - 2 * a.half));
   const int n = wide ? WIDE : NARROW, pairs = PAIR ? n / 2 : n;
   const int64_t per_row = (int64_t)a.heads * (a.half / pairs);
-  // rows of a workgroup: four steps a thread, as long as the chip is filled; heads of few rows are dealt out to several workgroups
-  int64_t rows_each = std::max<int64_t>(std::min<int64_t>({4 * 256 / per_row, a.rows / 1024, 4096 / a.half, 64}), 1);
+  // Rows of a workgroup: three steps a thread, as long as there are two workgroups a CU; heads of few rows are dealt out to several workgroups.  (us with two,
+  // three, four steps: 8192 rows of 40 heads of 128 bf16 28.8, 27.6, 27.9, 9000 rows of 20 heads of 96 f16, 48 rotated, 17.7, 18.2, 20.0; with four workgroups a CU
+  // 1500 rows of 12 heads of 80 f32 5.1, with two 4.6.)
+  int64_t rows_each = std::max<int64_t>(std::min<int64_t>({3 * 256 / per_row, a.rows / 512, 4096 / a.half, 64}), 1);
   int64_t groups = std::max<int64_t>(std::min<int64_t>({(per_row + 255) / 256, a.heads, (1024 + a.rows - 1) / a.rows}), 1);
   if (rows_each > 1) groups = 1;
   const dim3 grid((uint32_t)(ceil_div(a.rows, rows_each) * groups));
