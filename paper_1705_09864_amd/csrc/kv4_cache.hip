@@ -36,10 +36,12 @@ __device__ inline uint32_t level(float x, float s, float o, float r) {
   return min(to_uint(rintf(__builtin_fmaf(__builtin_fmaf(-n, s, d), r, n))), 15u);
 }
 __device__ inline float inverse(float s) { return s >= 0x1p-126f ? 1.0f / s : 0.0f; }
-// The same in the low bits, for values and differences that are finite: whole numbers are the last bits of numbers from 2^23 on, where a sum rounds to them as rint does.
+// The same in the low bits, for values and differences that are finite: whole numbers are the last bits of numbers from 2^23 on, where a sum rounds to them as rint
+// does.  (The second quotient is rounded beside n first: beside 2^23 it would show which way r is off, and no two levels would be halfway between.)
 __device__ inline uint32_t quick_level(float x, float s, float o, float r) {
-  const float d = x - o, t = __builtin_fmaf(d, r, 0x1p23f);
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(__builtin_fmaf(__builtin_fmaf(0x1p23f - t, s, d), r, t), 0x1p23f, 0x1p23f + 15.0f));
+  const float d = x - o, n = __builtin_fmaf(d, r, 0x1p23f) - 0x1p23f;
+  const float t = __builtin_fmaf(__builtin_fmaf(-n, s, d), r, n);
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(t + 0x1p23f, 0x1p23f, 0x1p23f + 15.0f));
 }
 __device__ inline float value_of(uint32_t q, uint32_t p) { return __builtin_fmaf((float)q, scale_of(p), offset_of(p)); }
 

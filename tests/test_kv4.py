@@ -144,6 +144,29 @@ def test_write_and_read(kind, dim):
             at += m
 
 
+@pytest.mark.parametrize("kind,bits", [(torch.float32, 8), (torch.float16, 6), (torch.bfloat16, 3)])
+@pytest.mark.parametrize("new", [1, 70])
+def test_halfway_between_two_levels(kind, bits, new):
+    """Values that lie exactly between two levels go to the even one, whatever the scale (of so many bits that its multiples by a half are values of the type)."""
+    rng = np.random.default_rng(bits)
+    cache = Cache(2, 64, [new] * 40, seed=1)
+    step = np.ldexp(rng.integers(2**(bits - 1), 2**bits, (40 * new, 2)).astype(np.float64), rng.integers(-8, 3, (40 * new, 2)))
+    half = rng.integers(0, 31, (40 * new, 2, 64)) / 2
+    half[..., 5], half[..., 60] = 0, 15  # (the least and the largest)
+    x = torch.from_numpy(half * step[..., None]).cuda().to(kind)
+    assert bool((x.double().cpu() == torch.from_numpy(half * step[..., None])).all())
+    B.kv4_write(x, -x, *cache.args)
+    levels, scales = unpack(cache.pages, 64), cache.scales.float().cpu().numpy()
+    for i in range(40):
+        for t in range(new):
+            page, r = cache.table[i, t // 64], i * new + t
+            assert (scales[page, :, 0, t % 64, 0] == step[r]).all() and not scales[page, :, 0, t % 64, 1].any()
+            assert (levels[page, :, 0, t % 64] == np.rint(half[r])).all()
+            # (the least is -15 steps, rounded to bf16: exact where it has 8 bits)
+            if (bf16(-15 * step[r].astype(np.float32)) == -15 * step[r]).all():
+                assert (levels[page, :, 1, t % 64] == np.rint(15 - half[r])).all()
+
+
 def test_rows_that_are_not_finite():
     """Scales go by what is finite; infinity is the highest level, what is below or no number the lowest; a row of one value, and one without any."""
     for kind in TYPES:
