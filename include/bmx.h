@@ -392,7 +392,9 @@ typedef struct bmx_kv4_cache {
  *   < 2^-126.  Both are taken over finite values; infinity is level 15, -infinity and NaN level 0.  No other token changes.
  * bmx_kv4_read: the rows' values q * s + o, one rounding to fp32, then to the type; rows of tokens that are not there are zeros.
  * bmx_kv4_attention: as bmx_kv_attention; workspace by BMX_OP_KV4_ATTENTION with the same numbers.  Either cache's workspace may be any stream's own, not
- *   two streams' (nor two graphs' that run at once).  A row that sees a token whose scale or offset is no finite number has results that are none either. */
+ *   two streams' (nor two graphs' that run at once).  A row that sees a token whose scale or offset is no finite number has results that are none either,
+ *   or, where that makes a score of -infinity of a key, leaves the token out; other rows are as ever.  Results may be no numbers too where queries, scales or offsets are
+ *   beyond 2^100 (sums are fp32, of up to 31 times a scale). */
 int bmx_kv4_write(const bmx_kv4_cache* cache, const void* k, const void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row,
                   int64_t v_head, int64_t rows, int max_new, void* stream);
 int bmx_kv4_read(const bmx_kv4_cache* cache, void* k, void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head,

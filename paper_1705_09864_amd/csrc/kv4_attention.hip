@@ -101,8 +101,8 @@ struct Args {
   int64_t q_row, q_head;
   JoinTo to;
   int rows, max_new, window, prompt_splits;
-  int units, tiles;  // tiles of 16 rows, of all sequences and of one
-  Deal deal;         // of their pages; no extra parts: a tile's are all one workgroup's
+  Deal deal;         // of the pages of tiles of 16 rows; no extra parts: a tile's are all one workgroup's
+  int units, tiles;  // (for the deal) tiles of all sequences and of one
   int few;  // sequences of more rows than this are the other kernel's
   bool causal, aligned;
   float scale;
@@ -137,7 +137,8 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_attention_kernel(bmx_kv4_cache
   __shared__ JoinLds<ROW, WAVES> lds;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16;
   const int head = blockIdx.x % c.heads, share = a.to.share;
-  Part part = {(int)(blockIdx.z * gridDim.y + blockIdx.y), 0, 1, 0, kAllPages};
+  Part part = {0, 0, 1, 0, kAllPages};
+  int seq = blockIdx.z, r0 = blockIdx.y * 16;
   if (a.deal.extra > 0) {
     part = part_of(blockIdx.x / c.heads, a.units, a.deal, [&](int n) {
       const KvSpan s = kv_span(c, n / a.tiles, a.rows, a.max_new);
@@ -145,8 +146,8 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_attention_kernel(bmx_kv4_cache
       return has_rows(a, s, r0) ? Seen(a, s, r0).pages() : -1;
     });
     if (part.unit < 0) return;
+    seq = part.unit / a.tiles, r0 = part.unit % a.tiles * 16;
   }
-  const int seq = part.unit / a.tiles, r0 = part.unit % a.tiles * 16;
   const KvSpan s = kv_span(c, seq, a.rows, a.max_new);
   if (!has_rows(a, s, r0)) return;
   const Seen seen(a, s, r0);
@@ -756,7 +757,7 @@ hipError_t launch_kv4_attention(const bmx_kv4_cache& c, const void* q, int type,
   const Plan p = plan(c.sequences, c.table_width, c.heads, q_heads, c.dim, max_new, type);
   uint32_t* arrived = static_cast<uint32_t*>(workspace);
   const Args a = {q, q_row, q_head, {out, out_row, out_head, lse, reinterpret_cast<float*>(arrived + kCounters), arrived, q_heads, q_heads / c.heads, p.part_rows},
-                  rows, max_new, window, p.prompt_splits, (int)p.units, (int)p.tiles, p.deal, p.few, causal, aligned, scale};
+                  rows, max_new, window, p.prompt_splits, p.deal, p.deal.extra ? (int)p.units : 0, (int)p.tiles, p.few, causal, aligned, scale};
   const int64_t counters = std::max(p.deal.extra ? p.units * c.heads : 0, p.prompt_splits > 1 ? p.prompt_tiles * c.heads * c.sequences : 0);
   if (fresh && counters) launch_kernel(clear_kernel, dim3((uint32_t)ceil_div(counters, 256)), dim3(256), 0, s, arrived);
   const auto f = type == BMX_F32 ? launch_typed<BMX_F32> : type == BMX_F16 ? launch_typed<BMX_F16> : launch_typed<BMX_BF16>;

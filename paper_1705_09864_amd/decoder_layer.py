@@ -107,7 +107,7 @@ class FewBitAttention:
                 raise ValueError("x: expected the shape [rows, %d], got %r" % (self.hidden, list(x.shape)))
         elif x.dim() != 2 or tuple(x.shape) != (sum(new), self.hidden):
             raise ValueError("x: expected the shape [%d, %d], got %r" % (sum(new), self.hidden, list(x.shape)))
-        rows = B.w4_fc(x, *self.qkv, self.n_qkv).view(x.shape[0], -1, self.dim)
+        rows = B.w4_fc(x, *self.qkv, self.n_qkv).view(x.shape[0], self.heads + 2 * self.kv_heads, self.dim)
         if on_gpu:
             sequences = where.lengths.numel()
             starts, positions, _ = where.resize(new, x.shape[0])
@@ -127,7 +127,7 @@ class FewBitAttention:
         # (rows of no sequence are not written)
         out = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if on_gpu else None
         o = attention(q, *cache, starts=starts, max_new=most, out=out, workspace=self.workspace(sequences, where.table.shape[1], most))
-        return B.w4_fc(o.view(x.shape[0], -1), *self.out, self.n_out)
+        return B.w4_fc(o.view(x.shape[0], self.heads * self.dim), *self.out, self.n_out)
 
 
 def plain(x, w_qkv, w_out, heads, kv_heads, dim, freq=None, interleaved=False):

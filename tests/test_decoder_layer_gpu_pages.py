@@ -151,6 +151,18 @@ def test_against_the_layer_in_fp32():
         assert float((y - plain(x, w_qkv, w_out, 4, 2, 64)).norm() / want.norm()) > 0.35
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+def test_steps_without_rows(bits):
+    """Sequences that only lose tokens, and none that gain any."""
+    layer, g = make(2, 1, 64, 200, bits, freq=B.rotary_frequencies(64))
+    where, host = DevicePages(40, 2, 3), Pages(40, 2, 3)
+    layer.step(torch.randn((140, 200), device="cuda", generator=g).bfloat16(), where, gpu([70, 70]))
+    none = torch.zeros((0, 200), device="cuda").bfloat16()
+    assert layer.step(none, where, gpu([-70, -5])).shape == (0, 200)
+    assert where.refused() == 0 and where.lengths.tolist() == [0, 65] and where.pool[0].item() == 38
+    assert layer.step(none, host, [0, 0]).shape == (0, 200) and host.tokens == [0, 0]
+
+
 def test_what_does_not_fit():
     with pytest.raises(ValueError, match="bits"):
         make(2, 1, 64, 200, 5)

@@ -347,6 +347,49 @@ def test_values_of_uneven_sizes(kind):
         check_attention(cache, q, new, out)
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("new", [[1] * 5, [4] * 5, [30, 0, 1, 300, 2]])
+def test_scales_that_are_no_numbers(kind, new):
+    """A token's scale or offset that is infinite or no number spoils the rows that see the token (an infinite one of a key may make a score of -infinity), and no others."""
+    lengths = [70, 300, 130, 400, 200]
+    clean = Cache(4, 64, lengths, seed=9)
+    q = torch.randn((sum(new), 32, 64), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(kind)
+    want = B.kv4_attention(q, *clean.args, starts=starts_of(new), window=50)
+    for which in (0, 1):
+        for part, value in ((0, float("nan")), (1, float("nan")), (0, float("inf")), (1, float("-inf"))):
+            cache = Cache(4, 64, lengths, seed=9)
+            spoilt = [(0, 5), (1, 260), (2, 129), (3, 120), (4, 100)]
+            for i, t in spoilt:
+                cache.scales[int(cache.table[i, t // 64]), :, which, t % 64, part] = value
+            out = B.kv4_attention(q, *cache.args, starts=starts_of(new), window=50)
+            at = 0
+            for (i, t), n, m in zip(spoilt, lengths, new):
+                pos = torch.arange(n - m, n, device="cuda")
+                sees = (t <= pos) & (t > pos - 50)
+                rows, same = out[at:at + m], want[at:at + m]
+                assert (which == 0 and value != value) <= (not bool(torch.isfinite(rows[sees]).any()))
+                assert which == 0 or not bool(torch.isfinite(rows[sees]).all(-1).any())
+                assert torch.equal(rows[~sees], same[~sees])
+                at += m
+
+
+def test_many_sequences_of_unknown_rows():
+    """More tiles of rows, of all sequences together, than 32 bits have room for their numbers: starts alone say how few there are."""
+    sequences, rows = 40000, 60000
+    pages, scales = B.kv4_cache(3, 1, 32)
+    pages.random_(0, 256)
+    scales.copy_(torch.tensor([0.2, -1.5], device="cuda"))
+    table = torch.ones((sequences, 1), dtype=torch.int32, device="cuda")
+    lengths = torch.full((sequences,), 64, dtype=torch.int32, device="cuda")
+    starts = torch.zeros((sequences + 1,), dtype=torch.int32, device="cuda")
+    starts[sequences:] = 3
+    q = torch.randn((rows, 16, 32), device="cuda")
+    out = torch.full_like(q, 7)
+    B.kv4_attention(q, pages, scales, table, lengths, starts=starts, max_new=900, out=out)
+    alone = B.kv4_attention(q[:3], pages, scales, table[:1], lengths[:1])
+    assert torch.equal(out[:3], alone) and bool((out[3:] == 7).all())
+
+
 def test_tokens_that_are_not_there():
     """Places of the table outside the pages: their tokens count for nothing."""
     for kind in TYPES:
