@@ -137,19 +137,21 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_attention_kernel(bmx_kv4_cache
   __shared__ JoinLds<ROW, WAVES> lds;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16;
   const int head = blockIdx.x % c.heads, share = a.to.share;
-  Part part = {0, 0, 1, 0, kAllPages};
+  Part part = {0, 0, 1, 0, kAllPages, {}};
   int seq = blockIdx.z, r0 = blockIdx.y * 16;
   if (a.deal.extra > 0) {
     part = part_of(blockIdx.x / c.heads, a.units, a.deal, [&](int n) {
       const KvSpan s = kv_span(c, n / a.tiles, a.rows, a.max_new);
       const int r0 = n % a.tiles * 16;
-      return has_rows(a, s, r0) ? Seen(a, s, r0).pages() : -1;
+      return UnitPages{has_rows(a, s, r0) ? Seen(a, s, r0).pages() : -1, s};
     });
     if (part.unit < 0) return;
     seq = part.unit / a.tiles, r0 = part.unit % a.tiles * 16;
+  } else {
+    part.span = kv_span(c, seq, a.rows, a.max_new);
+    if (!has_rows(a, part.span, r0)) return;
   }
-  const KvSpan s = kv_span(c, seq, a.rows, a.max_new);
-  if (!has_rows(a, s, r0)) return;
+  const KvSpan s = part.span;
   const Seen seen(a, s, r0);
   const int low_all = seen.low_all, high_all = seen.high_all;
   // this workgroup's pages

@@ -35,6 +35,11 @@ __device__ inline int sums_to(int x) {
 struct Part {
   int unit, split, used, first;  // the unit's part `split` of `used`; first: the number of its first part among all; unit < 0: none
   int per;                       // pages of a part
+  KvSpan span;                   // of the unit's sequence
+};
+struct UnitPages {
+  int pages;  // below 0 where it has no rows, fewer than 2^30
+  KvSpan span;
 };
 constexpr int kAllPages = 0x7fffffff, kMostUnits = 256;
 constexpr int kWholePages = 12, kLeastPart = 4;  // (pages that a single unit keeps in one part, and that any part has at least)
@@ -43,47 +48,46 @@ constexpr int kWholePages = 12, kLeastPart = 4;  // (pages that a single unit ke
 struct Deal {
   int extra, even, slack;
 };
-// pages_of(n): the n-th unit's pages, below 0 where it has no rows, all of them fewer than 2^30.
+// pages_of(n): the n-th unit's pages.
 template <class F>
 __device__ inline Part part_of(int slot, int units, const Deal& deal, F pages_of) {
   const int lane = threadIdx.x % 64;
   if (units == 1) {
-    const int pages = pages_of(0), per = max((pages + deal.extra) / (deal.extra + 1), pages <= kWholePages ? pages : kLeastPart), used = pages > 0 ? (pages + per - 1) / per : 1;
-    return {pages >= 0 && slot < used ? 0 : -1, slot, used, 0, used == 1 ? kAllPages : per};
+    const UnitPages u = pages_of(0);
+    const int pages = u.pages, per = max((pages + deal.extra) / (deal.extra + 1), pages <= kWholePages ? pages : kLeastPart), used = pages > 0 ? (pages + per - 1) / per : 1;
+    return {pages >= 0 && slot < used ? 0 : -1, slot, used, 0, used == 1 ? kAllPages : per, u.span};
   }
-  constexpr int EACH = kMostUnits / 64;
-  int pages[EACH], mine = 0;
-  const int each = (units + 63) / 64;
-#pragma unroll
-  for (int j = 0; j < EACH; ++j) {
-    const int n = lane * each + j;
-    pages[j] = j < each && n < units ? pages_of(n) : -1;
-    mine += max(pages[j], 0);
+  // 64 units at a time, a lane each (rolled up: the code of a launch comes from memory too)
+  UnitPages u = {-1, {}};
+  const auto load = [&](int base) {
+    u.pages = -1;
+    if (base + lane < units) u = pages_of(base + lane);
+  };
+  int all = 0, longest = 0;
+#pragma unroll 1
+  for (int base = 0; base < units; base += 64) {
+    load(base);
+    longest = max(longest, u.pages);
+    all += __builtin_amdgcn_readlane(sums_to(max(u.pages, 0)), 63);
   }
-  const int all = __builtin_amdgcn_readlane(sums_to(mine), 63);
-  bool long_one = false;  // by a quarter longer than the mean
-#pragma unroll
-  for (int j = 0; j < EACH; ++j) long_one |= (float)pages[j] * units > 1.25f * all;
-  const int extra = __any(long_one) ? deal.extra : deal.even, per = max((all + extra - 1) / extra, kLeastPart);
-  int parts[EACH], sum = 0;
-#pragma unroll
-  for (int j = 0; j < EACH; ++j) {
-    parts[j] = pages[j] < 0 ? 0 : pages[j] <= per + deal.slack ? 1 : (pages[j] - 1) / per + 1;
-    sum += parts[j];
+  const int extra = __any((float)longest * units > 1.25f * all) ? deal.extra : deal.even, per = max((all + extra - 1) / extra, kLeastPart);
+  int first = 0;
+#pragma unroll 1
+  for (int base = 0; base < units; base += 64) {
+    if (units > 64) load(base);
+    const int parts = u.pages < 0 ? 0 : u.pages <= per + deal.slack ? 1 : (u.pages - 1) / per + 1;
+    const int to = first + sums_to(parts);
+    const uint64_t has = __ballot(slot < to);
+    if (has) {
+      const int who = __builtin_ctzll(has);
+      const auto of_lane = [&](int x) { return __builtin_amdgcn_readlane(x, who); };
+      const int used = of_lane(parts), from = of_lane(to) - used;
+      return {base + who, slot - from, used, from, used == 1 ? kAllPages : per,
+              {of_lane(u.span.row0), of_lane(u.span.count), of_lane(u.span.first), of_lane(u.span.length)}};
+    }
+    first = __builtin_amdgcn_readlane(to, 63);
   }
-  const int to = sums_to(sum);
-  Part p = {-1, 0, 0, to - sum, per};
-#pragma unroll
-  for (int j = 0; j < EACH; ++j) {
-    if (slot >= p.first && slot < p.first + parts[j] && p.unit < 0) p.unit = lane * each + j, p.split = slot - p.first, p.used = parts[j];
-    if (p.unit < 0) p.first += parts[j];
-  }
-  const uint64_t has = __ballot(p.unit >= 0);
-  if (has == 0) return {-1, 0, 0, 0, 0};
-  const int who = __builtin_ctzll(has);
-  const int used = __builtin_amdgcn_readlane(p.used, who);
-  return {__builtin_amdgcn_readlane(p.unit, who), __builtin_amdgcn_readlane(p.split, who), used, __builtin_amdgcn_readlane(p.first, who),
-          used == 1 ? kAllPages : per};
+  return {-1, 0, 0, 0, 0, {}};
 }
 
 constexpr int kMostSplits = 128;  // workgroups that share rows

@@ -288,7 +288,7 @@ hipError_t launch_kv_resize(const int32_t* change, int sequences, int32_t* table
     launch<1024>(a, s);
   } else {
     launch_kernel(kv_resize_many_kernel<1024>, dim3(1), dim3(1024), 0, s, a);
-    note_kernel("kv_resize_many_kernel<1024> grid 1 block 1024");
+    note_kernel("kv_resize_many_kernel<%d> grid 1 block %d", 1024, 1024);
     if (rows > 0 && (positions || slots)) launch_kernel(kv_slots_kernel, dim3((uint32_t)ceil_div(rows, 256)), dim3(256), 0, s, a);
   }
   return launch_error();
