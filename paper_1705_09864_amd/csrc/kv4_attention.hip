@@ -14,7 +14,9 @@
 //
 // Bound by the cache's bytes: a wave goes over pages of its own (8.5 KB at 128 values a head) with its queries, running maxima, sums and results in
 // registers, and requests the next page's keys as soon as this one's are used up, its values as soon as these are.  Where rows x heads are few, a sequence's
-// pages are split over workgroups too, and joined by the last of them (kv_join.h).
+// pages are split over workgroups too, and joined by the last of them (kv_join.h).  64 sequences of 8192 tokens stream at 5.3 TB/s; 131072 tokens of one,
+// 8 heads of the cache of 128: 35.2 us, 4.1 TB/s (vector ALU 52 % of the time, matrix cores 15 %; the rest are the first pages and the join); 64 of 0 to 4096: 44.2 us,
+// 3.2 TB/s, as long as the longest takes; 100 tokens of 8 heads of 64: 6.3 us, a launch and five trips to memory.
 #include "bmx_internal.h"
 #include "few_bits.h"
 #include "kv_join.h"
@@ -94,6 +96,7 @@ __device__ inline float or_zero(float x) { return x == -INFINITY ? 0.0f : x; }
 
 // By so much (of a logarithm of 2) a row's scores may pass the one that its weights are relative to, before they are taken relative to a larger one: weights have
 // fp32's range, and a row's results would otherwise be multiplied anew on every other page.
+// (2048 new tokens of 4096 347 us without it, 323 with.)
 constexpr float kGrowth = 8.0f;
 
 struct Args {
@@ -109,8 +112,10 @@ struct Args {
 };
 
 constexpr int kCounters = 16384;  // of the workspace's head
-constexpr int kLeastPages = 16;   // of a split of many rows
-constexpr int kLeastTiles = 128;  // of 128 rows for the kernel for many
+constexpr int kLeastPages = 16;  // of a split of many rows (8: level)
+// Tiles of 128 rows for the kernel for many: where fewer are level goes by lengths that only the device knows (us in tiles of 16 rows, of 128, 32 heads on 8 of 128 bf16:
+// 256 new tokens of 768 15.8, 29.9, of 4352 50, 53, of 16640 164, 127; 512 of 512 19.6, 22.0, of 4608 96, 74, of 16896 317, 225; 16 sequences of 64 new of 512 41, 24).
+constexpr int kLeastTiles = 128;
 constexpr int64_t kPlaces = 512, kMostPlaces = 2048;
 constexpr int64_t kMostTiles = 65535;  // of 16 rows: a launch's second dimension
 
@@ -356,7 +361,11 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_attention_kernel(bmx_kv4_cache
 // the four waves, as 16-bit floats in the order of the 32 x 32 x 16 products' operands, its scales and offsets as floats (a wave brings in a quarter of it, a page ahead, and
 // converts it on its way), and a lane has one row's scores of 16 of 32 tokens, which again are those of its own column of P^T.  Rows of V^T are a block's 16
 // even values, then its odd ones.
-// SPLIT: tiles of rows fewer than the chip holds workgroups at once, whose pages are split and joined as above.
+// SPLIT: tiles of rows fewer than the chip holds workgroups at once, whose pages are split and joined as above (32 heads on 8 of 128 bf16: 512 new tokens of 4608 74 us,
+// unsplit 148, of 16896 225, 522; 1024 of 5120 138, 164; 4 sequences of 128 new of 4224 70, 135).
+//
+// Bound by issue: two sequences of 2048 new tokens of 4096, 32 heads on 8 of 128 bf16, 319 us, 650 TFLOP/s by the formula's products (a third of those made are the
+// weights' lower parts).  Vector ALU 63 % of the time, matrix cores 48 %, two waves a SIMD.  Two tiles of 32 rows a wave, one wave a SIMD: 464 us.
 template <int TYPE, int DC, bool SPLIT>
 __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv4_cache c, Args a) {
   static_assert(TYPE != BMX_F32, "");
@@ -478,7 +487,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
   if (pg < last) convert(0, pg);
   __syncthreads();
 
-  // (what LDS holds does not come into registers all at once: there are not as many)
+  // (what LDS holds does not come into registers all at once: there are not as many, and they would spill; where the compiler keeps to them by itself, 347 us without, 356 with)
   const auto fence = [](bool here) {
     if ((DC == 3 || DC > 4 || (DC == 4 && (SPLIT || TYPE == BMX_F16))) && here) __builtin_amdgcn_sched_barrier(0);
   };

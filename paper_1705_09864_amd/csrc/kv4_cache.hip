@@ -4,7 +4,8 @@
 // Levels are chosen against the rounded pair, by fp32 quotients.  No token's levels depend on another's, so none is ever written again, and a byte
 // belongs to one token.
 //
-// Bound by the bytes of rows and levels.
+// Bound by the bytes of rows and levels: 13364 tokens of 8 heads of 128 f16 written in 20.2 us (69 MB, 3.4 TB/s: rows, then a token's least and largest, a barrier for
+// the values' order, then levels), read in 16.1 (4.3 TB/s).  A few tokens by latency: 64 in 2.9 us, 4007 read in 8.5 to 10 (21 MB).
 #include "bmx_internal.h"
 #include "few_bits.h"
 
@@ -279,6 +280,8 @@ auto pick_read(int dim) {
 
 hipError_t launch_kv4_write(const bmx_kv4_cache& c, const void* k, const void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row,
                             int64_t v_head, int rows, int max_new, hipStream_t s) {
+  // (us of a call and a read of one token, a wave a token, pages whole: 64 sequences of 2 new tokens 7.1, 11.0, 8 9.9, 11.5, 16 13.5, 12.0, 32 19.5, 13.1; 8 of 8 6.1, 6.8,
+  // 16 6.3, 6.8, 64 8.6, 7.4)
   if (max_new <= 8) {
     const dim3 grid((uint32_t)(c.sequences * max_new), (c.heads * 2 + 3) / 4);
     const auto kern = type == BMX_F32 ? kv4_append_kernel<BMX_F32> : type == BMX_F16 ? kv4_append_kernel<BMX_F16> : kv4_append_kernel<BMX_BF16>;

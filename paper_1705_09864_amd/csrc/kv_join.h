@@ -42,7 +42,7 @@ struct UnitPages {
   KvSpan span;
 };
 constexpr int kAllPages = 0x7fffffff, kMostUnits = 256;
-constexpr int kWholePages = 12, kLeastPart = 4;  // (pages that a single unit keeps in one part, and that any part has at least)
+constexpr int kWholePages = 12, kLeastPart = 4;  // (pages that a single unit keeps in one part, and that any part has at least; 6 or 8: level)
 // How they are dealt out: parts beyond one for each unit, the most there are (1 or more) and those aimed at where the units are of about a size; pages that a unit's only
 // part may have more than others'.
 struct Deal {
