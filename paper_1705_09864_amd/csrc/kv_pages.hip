@@ -56,37 +56,42 @@ __device__ inline void put_row(const Args& a, int r, int pos, int page) {
 constexpr int kMostInOne = 4;
 enum Part { kAll, kMoves, kState };
 
-// What all kernels begin with, THREADS sequences at a time: the sums, and whether everything has room.
-template <int THREADS>
+// What all kernels begin with, EACH sequences a thread at a time: the sums, and whether everything has room.
+template <int THREADS, int EACH = 1>
 struct Sums {
-  static constexpr int WAVES = THREADS / 64;
-  uint32_t back_to[THREADS], take_to[THREADS], more_to[THREADS];  // of pages given back, pages taken, new rows: up to each sequence
-  int32_t pages_of[THREADS], first_of[THREADS];                   // its pages and tokens before the call
+  static constexpr int WAVES = THREADS / 64, MANY = THREADS * EACH;
+  uint32_t back_to[MANY], take_to[MANY], more_to[MANY];  // of pages given back, pages taken, new rows: up to each sequence
+  int32_t pages_of[MANY], first_of[MANY];                // its pages and tokens before the call
   uint32_t of_wave[3][WAVES];
   int first_bad;
 };
 
-// THREADS sequences or fewer; what one needs stays in registers.  kAll: one workgroup does everything.  Otherwise kMoves, any number of workgroups that move pages and map rows
+// THREADS times SEQS sequences or fewer, SEQS behind one another to a thread; what one needs stays in registers.  kAll: one workgroup does everything.  Otherwise kMoves, any number of workgroups that move pages and map rows
 // between them, each on sums of its own, and behind it kState, one that brings lengths and pool up to date.
 // A page that is taken comes from the stack, or, if it is given back in this call, from where the table has it: pages go both ways at once.
-template <int THREADS, Part PART>
+template <int THREADS, int SEQS, Part PART>
 __global__ __launch_bounds__(THREADS) void kv_resize_kernel(Args a) {
-  __shared__ Sums<THREADS> s;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, n = a.sequences;
+  __shared__ Sums<THREADS, SEQS> s;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, n = a.sequences, mine = tid * SEQS;
   const int free = a.pool[0];
   if (tid == 0) s.first_bad = 0x7fffffff;
-  KvChange c = {};
-  c.fits = true;
-  if (tid < n) {
-    const int tokens = a.lengths[tid];
-    c = kv_change_of(tokens, a.change[tid], a.table_width);
-    s.pages_of[tid] = c.pages, s.first_of[tid] = tokens;
+  KvChange c[SEQS] = {};
+  uint32_t v[3] = {}, all[3];  // of this thread's sequences, then of all before them
+#pragma unroll
+  for (int j = 0; j < SEQS; ++j) {
+    c[j].fits = true;
+    if (mine + j < n) {
+      const int tokens = a.lengths[mine + j];
+      c[j] = kv_change_of(tokens, a.change[mine + j], a.table_width);
+      s.pages_of[mine + j] = c[j].pages, s.first_of[mine + j] = tokens;
+    }
+    v[0] = plus(v[0], max(c[j].pages - c[j].pages_then, 0)), v[1] = plus(v[1], max(c[j].pages_then - c[j].pages, 0)), v[2] = plus(v[2], c[j].more);
   }
-  uint32_t v[3] = {(uint32_t)max(c.pages - c.pages_then, 0), (uint32_t)max(c.pages_then - c.pages, 0), (uint32_t)c.more}, all[3];
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
-    v[k] = sums_to(v[k]);
-    if (lane == 63) s.of_wave[k][wave] = v[k];
+    const uint32_t to = sums_to(v[k]);
+    if (lane == 63) s.of_wave[k][wave] = to;
+    v[k] = __builtin_amdgcn_update_dpp(0, (int)to, 0x138, 0xf, 0xf, false);  // the lane's before this one
   }
   __syncthreads();
 #pragma unroll
@@ -97,8 +102,12 @@ __global__ __launch_bounds__(THREADS) void kv_resize_kernel(Args a) {
   }
   const bool pool_is_one = free >= 0 && free <= a.num_pages && (int64_t)free + all[0] <= a.num_pages;
   const uint32_t room = pool_is_one ? free + all[0] : 0, rows = a.rows;
-  s.back_to[tid] = v[0], s.take_to[tid] = v[1], s.more_to[tid] = v[2];
-  if (!c.fits || v[1] > room || v[2] > rows) atomicMin(&s.first_bad, tid);
+#pragma unroll
+  for (int j = 0; j < SEQS; ++j) {
+    v[0] = plus(v[0], max(c[j].pages - c[j].pages_then, 0)), v[1] = plus(v[1], max(c[j].pages_then - c[j].pages, 0)), v[2] = plus(v[2], c[j].more);
+    s.back_to[mine + j] = v[0], s.take_to[mine + j] = v[1], s.more_to[mine + j] = v[2];
+    if (!c[j].fits || v[1] > room || v[2] > rows) atomicMin(&s.first_bad, mine + j);
+  }
   __syncthreads();
   const int bad = s.first_bad;
   const bool refused = bad != 0x7fffffff || !pool_is_one;
@@ -106,13 +115,15 @@ __global__ __launch_bounds__(THREADS) void kv_resize_kernel(Args a) {
     if (tid == 0) a.pool[1] = !pool_is_one ? -1 : refused ? bad + 1 : 0;
     if (!refused) {
       if (tid == 0) a.pool[0] = (int)(room - all[1]);
-      if (tid < n) a.lengths[tid] = c.tokens_then;
+#pragma unroll
+      for (int j = 0; j < SEQS; ++j)
+        if (mine + j < n) a.lengths[mine + j] = c[j].tokens_then;
     }
   }
   if (PART == kState) return;
   if (blockIdx.x == 0) {
     if (tid == 0) a.starts[0] = 0;
-    if (tid < n) a.starts[tid + 1] = refused ? 0 : (int)v[2];
+    for (int i = tid; i < n; i += THREADS) a.starts[i + 1] = refused ? 0 : (int)s.more_to[i];
   }
   int32_t* const stack = a.pool + 2;
   // the k-th page given back: where the table has it; the k-th taken: its number
@@ -172,7 +183,7 @@ __global__ __launch_bounds__(THREADS) void kv_resize_kernel(Args a) {
   }
 }
 
-// More sequences than threads: one workgroup over and over, the pages first all onto the stack and then from there; the rows' maps by kv_slots_kernel.
+// More than 4096 sequences: one workgroup over and over (3000 with a token each 23 us, 8.9 with four to a thread), the pages first all onto the stack and then from there; the rows' maps by kv_slots_kernel.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void kv_resize_many_kernel(Args a) {
   __shared__ Sums<THREADS> s;
@@ -267,17 +278,17 @@ __global__ __launch_bounds__(256) void kv_slots_kernel(Args a) {
   put_row(a, r, pos, a.table[i * a.table_ld + (pos >> kLogPage)]);
 }
 
-template <int THREADS>
+template <int THREADS, int SEQS>
 void launch(const Args& a, hipStream_t s) {
   if (a.rows <= kMostInOne * THREADS) {
-    launch_kernel(kv_resize_kernel<THREADS, kAll>, dim3(1), dim3(THREADS), 0, s, a);
-    note_kernel("kv_resize_kernel<%d,%d> grid 1 block %d", THREADS, (int)kAll, THREADS);
+    launch_kernel(kv_resize_kernel<THREADS, SEQS, kAll>, dim3(1), dim3(THREADS), 0, s, a);
+    note_kernel("kv_resize_kernel<%d,%d,%d> grid 1 block %d", THREADS, SEQS, (int)kAll, THREADS);
     return;
   }
   const uint32_t grid = (uint32_t)std::min<int64_t>(ceil_div(a.rows, 4 * THREADS) * 9 / 8 + 1, 512);  // (and some for pages)
-  launch_kernel(kv_resize_kernel<THREADS, kMoves>, dim3(grid), dim3(THREADS), 0, s, a);
-  launch_kernel(kv_resize_kernel<THREADS, kState>, dim3(1), dim3(THREADS), 0, s, a);
-  note_kernel("kv_resize_kernel<%d,%d> grid %u block %d", THREADS, (int)kMoves, grid, THREADS);
+  launch_kernel(kv_resize_kernel<THREADS, SEQS, kMoves>, dim3(grid), dim3(THREADS), 0, s, a);
+  launch_kernel(kv_resize_kernel<THREADS, SEQS, kState>, dim3(1), dim3(THREADS), 0, s, a);
+  note_kernel("kv_resize_kernel<%d,%d,%d> grid %u block %d", THREADS, SEQS, (int)kMoves, grid, THREADS);
 }
 
 }  // namespace
@@ -287,9 +298,11 @@ hipError_t launch_kv_resize(const int32_t* change, int sequences, int32_t* table
   const Args a = {change, table, table_ld, lengths, pool, starts, positions, slots, sequences, table_width, num_pages, rows,
                   (uintptr_t)positions % 16 == 0 && (uintptr_t)slots % 16 == 0};
   if (sequences <= 256) {
-    launch<256>(a, s);
+    launch<256, 1>(a, s);
   } else if (sequences <= 1024) {
-    launch<1024>(a, s);
+    launch<1024, 1>(a, s);
+  } else if (sequences <= 4096) {
+    launch<1024, 4>(a, s);
   } else {
     launch_kernel(kv_resize_many_kernel<1024>, dim3(1), dim3(1024), 0, s, a);
     note_kernel("kv_resize_many_kernel<%d> grid 1 block %d", 1024, 1024);

@@ -101,6 +101,30 @@ def test_against_lists(sequences):
     assert refused >= 1 or sequences < 3
 
 
+@pytest.mark.parametrize("sequences", [4095, 4096, 4097, 6000])
+def test_thousands_of_sequences(sequences):
+    test_against_lists(sequences)
+
+
+@pytest.mark.parametrize("place", [0, 3, 1500, 4095])
+@pytest.mark.parametrize("rows", [3000, 9000])
+def test_one_of_many_refused(place, rows):
+    """Sequences that share a thread: the first that finds no room is named, and nothing changes; without it all have room."""
+    rng = np.random.default_rng(place)
+    want = Lists(4096, 3, 9000)
+    want.resize([int(n) for n in rng.integers(0, 100, 4096)], 1 << 20)
+    state = want.on_gpu()
+    change = [int(rng.integers(-n, 2)) for n in want.lengths]
+    change[place] = 64 * 3 + 1 - want.lengths[place]
+    expect = want.resize(change, rows)
+    assert want.status == place + 1
+    want.check(expect, B.kv_resize(ints(change), *state, rows), state)
+    change[place] = 0
+    expect = want.resize(change, rows)
+    assert want.status == 0
+    want.check(expect, B.kv_resize(ints(change), *state, rows), state)
+
+
 @pytest.mark.parametrize("rows", [0, 1, 1023, 1025, 4096, 4097, 70000])
 def test_maps_of_many_rows(rows):
     """The maps are made by the first launch, or by one of their own."""
