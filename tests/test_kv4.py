@@ -423,6 +423,20 @@ def test_far_pages_of_a_large_cache():
 
 
 @pytest.mark.parametrize("kind", TYPES)
+def test_a_prefix_shared_by_sequences(kind):
+    """Three sequences that begin with the same pages, read on a stream of their own behind the one that made them, one step and one prompt."""
+    for lengths, new in (([400, 130, 900], [1, 1, 1]), ([400, 300, 900], [200, 100, 150])):
+        cache = Cache(4, 64, lengths, seed=len(new))
+        cache.table[1:, :2] = cache.table[0, :2]
+        cache.args[2].copy_(torch.from_numpy(cache.table))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            attend(cache, 4, new, kind, seed=7)
+        torch.cuda.current_stream().wait_stream(side)
+
+
+@pytest.mark.parametrize("kind", TYPES)
 def test_workspace_kept_and_given(kind):
     """Calls of several sizes one after the other on one workspace give what each gives alone, and leave its counters at zero."""
     ws = torch.zeros((B.workspace_bytes(B.OP_KV4_ATTENTION, (4, 100, 2, 8, 64, 0)),), dtype=torch.uint8, device="cuda")
