@@ -363,26 +363,30 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_attention_kernel(bmx_kv4_cache
 // even values, then its odd ones.
 // SPLIT: tiles of rows fewer than the chip holds workgroups at once, whose pages are split and joined as above (32 heads on 8 of 128 bf16: 512 new tokens of 4608 74 us,
 // unsplit 148, of 16896 225, 522; 1024 of 5120 138, 164; 4 sequences of 128 new of 4224 70, 135).
+// GROUPS: two take turns, 256 rows a workgroup: while the four waves of one make products, those of the other, on the same SIMDs, make weights, with a barrier
+// wherever they change over.  So products of a page come a turn behind its weights, beside the next page's scores; the first group brings in keys, the second values.
 //
-// Bound by issue: two sequences of 2048 new tokens of 4096, 32 heads on 8 of 128 bf16, 319 us, 650 TFLOP/s by the formula's products (a third of those made are the
-// weights' lower parts).  Vector ALU 63 % of the time, matrix cores 48 %, two waves a SIMD.  Two tiles of 32 rows a wave, one wave a SIMD: 464 us.
-template <int TYPE, int DC, bool SPLIT>
-__global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv4_cache c, Args a) {
-  static_assert(TYPE != BMX_F32, "");
+// Bound by issue: two sequences of 2048 new tokens of 4096, 32 heads on 8 of 128 bf16, 282 us in two groups, 730 TFLOP/s by the formula's products (a third of those
+// made are the weights' lower parts), 319 in one.  Vector ALU 64 % of the time, matrix cores 54 % (63 and 48 in one group), two waves a SIMD; the products alone take
+// 221 us, the weights alone 200.  Two tiles of 32 rows a wave, one wave a SIMD: 464.
+template <int TYPE, int DC, bool SPLIT, int GROUPS>
+__global__ __launch_bounds__(GROUPS * 256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv4_cache c, Args a) {
+  static_assert(TYPE != BMX_F32 && !(SPLIT && GROUPS > 1) && (GROUPS == 1 || DC <= 4), "");
   constexpr int BYTES = DC * 16, NS = DC * 2, KN = (DC + 3) / 4;  // NS: steps of 16 values; KN: what a wave brings in of keys, and of values, by 64 lanes
-  __shared__ u32x4 lds[2][2][NS * 128];                           // [buffer][keys, values]
-  __shared__ f32x4 of_token[2][4][16];                            // [buffer][keys' scales and offsets, values'][token / 4]
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32;
+  constexpr int ROWS = GROUPS * 128, SLOTS = GROUPS + 1;
+  __shared__ u32x4 keys[2][NS * 128], values[SLOTS][NS * 128];
+  __shared__ f32x4 of_token[SLOTS][4][16];  // [slot][keys' scales and offsets, values'][token / 4]
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 32, group = wave / 4, part = wave % 4;
   const int head = SPLIT ? blockIdx.x % c.heads : blockIdx.x, split = SPLIT ? blockIdx.x / c.heads : 0, seq = blockIdx.z;
   const KvSpan s = kv_span(c, seq, a.rows, a.max_new);
   const int share = a.to.share, rows = s.count * share;
-  const int r0 = ((rows + 127) / 128 - 1 - (int)blockIdx.y) * 128;  // (the last rows, which see most, first)
+  const int r0 = ((rows + ROWS - 1) / ROWS - 1 - (int)blockIdx.y) * ROWS;  // (the last rows, which see most, first)
   if (r0 < 0 || rows <= a.few) return;
   const auto first_seen = [&](int token) { return a.window ? max(max(s.first + token, 0) - a.window + 1, 0) : 0; };
   const auto end_seen = [&](int token) { return a.causal ? min(s.first + token + 1, s.length) : s.length; };
   const auto token_of = [&](int r) { return min(r, rows - 1) / share; };
   // what any row of the workgroup sees; what any, and every row of this wave does; what this lane's row does
-  const int low_group = first_seen(token_of(r0)), high_group = end_seen(token_of(r0 + 127));
+  const int low_group = first_seen(token_of(r0)), high_group = end_seen(token_of(r0 + ROWS - 1));
   const int r_wave = r0 + wave * 32, r = r_wave + lane % 32, token = token_of(r);
   const int low_any = first_seen(token_of(r_wave)), low_all = first_seen(token_of(r_wave + 31));
   const int high_all = end_seen(token_of(r_wave)), high_any = r_wave < rows ? end_seen(token_of(r_wave + 31)) : 0;
@@ -391,7 +395,8 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
   const int64_t page_bytes = (int64_t)c.heads * 2 * kPage * BYTES;
   const float factor = a.scale * 1.4426950408889634f;
   const uint32_t sixteens = sixteen<TYPE>(), sixteens_v = sixteen<BMX_BF16>();
-  u32x4 kr[KN], vr[KN][2];
+  u32x4 in[KN][GROUPS == 1 ? 3 : 2];  // keys, and behind them values; of two groups the first brings in the keys, the second the values
+  constexpr int V0 = GROUPS == 1;
   uint32_t pair_in[2] = {};  // wave 0: a token's scale and offset, of keys and of values
   int begin = low_group / kPage, last = kv_pages_to(high_group), used = 1;
   if constexpr (SPLIT) {  // this split's pages: as many for the rows that see few as for those that see most, which then are in fewer splits
@@ -403,11 +408,17 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
     begin += split * per;
   }
   const int none = c.num_pages > 0 ? 0 : kNowhere;
+  [[maybe_unused]] int ids = -1;  // of two groups: 64 pages' numbers, a lane each
   // the first page from `pg` on that is there, on its way into registers
   const auto fetch = [&](int pg) {
     int page = -1;
     for (; pg < last; ++pg) {
-      page = kv_page(c, seq, pg);
+      if constexpr (GROUPS == 1) {
+        page = kv_page(c, seq, pg);
+      } else {
+        if ((pg - begin) % 64 == 0) ids = pg + lane < last ? kv_page(c, seq, pg + lane) : -1;
+        page = __builtin_amdgcn_readlane(ids, (pg - begin) % 64);
+      }
       if (page >= 0) break;
     }
     // (behind the last page: page 0 once more, which nobody uses)
@@ -416,35 +427,40 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
     if (wave == 0) pair_in[0] = load4(rs, lane * 4 + none, 0), pair_in[1] = load4(rs, lane * 4 + none, 4 * kPage);
 #pragma unroll
     for (int n = 0; n < KN; ++n) {
-      const int i = min(lane / 16 + 4 * n, DC - 1), block = min(wave + 4 * n, DC - 1);
-      kr[n] = load16(r, lane % 16 * BYTES + i * 16 + none, wave * 16 * BYTES);
+      const int i = min(lane / 16 + 4 * n, DC - 1), block = min(part + 4 * n, DC - 1);
+      if (GROUPS == 1 || group == 0) in[n][0] = load16(r, lane % 16 * BYTES + i * 16 + none, part * 16 * BYTES);
+      if (GROUPS == 1 || group == 1)
 #pragma unroll
-      for (int g = 0; g < 2; ++g) vr[n][g] = load16(r, lane / 16 % 2 * 256 + lane % 16 * 16 + none, kPage * BYTES + block * 1024 + g * 512);
+        for (int g = 0; g < 2; ++g) in[n][V0 + g] = load16(r, lane / 16 % 2 * 256 + lane % 16 * 16 + none, kPage * BYTES + block * 1024 + g * 512);
     }
     return pg;
   };
-  const auto convert = [&](int buf, int pg) {
-    // keys: 32 values of token 16 wave + lane % 16; values: of a block a pair's even ones or its odd ones, every other four tokens
+  const auto convert = [&](int buf, int slot, int pg) {
+    // keys: 32 values of token 16 part + lane % 16; values: of a block a pair's even ones or its odd ones, every other four tokens
+    if (GROUPS == 1 || group == 0) {
 #pragma unroll
-    for (int n = 0; n < KN; ++n) {
-      const int i = lane / 16 + 4 * n;
-      if (i < DC) {
-        u32x4* to = &lds[buf][0][(wave / 2 * NS + 2 * i) * 64 + wave % 2 * 16 + lane % 16];
+      for (int n = 0; n < KN; ++n) {
+        const int i = lane / 16 + 4 * n;
+        if (i < DC) {
+          u32x4* to = &keys[buf][(part / 2 * NS + 2 * i) * 64 + part % 2 * 16 + lane % 16];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t w = kr[n][j];
-          to[j / 2 * 64 + j % 2 * 32] = u32x4{two_levels<TYPE, 0>(w, sixteens), two_levels<TYPE, 1>(w, sixteens), two_levels<TYPE, 2>(w, sixteens), two_levels<TYPE, 3>(w, sixteens)};
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t w = in[n][0][j];
+            to[j / 2 * 64 + j % 2 * 32] = u32x4{two_levels<TYPE, 0>(w, sixteens), two_levels<TYPE, 1>(w, sixteens), two_levels<TYPE, 2>(w, sixteens), two_levels<TYPE, 3>(w, sixteens)};
+          }
         }
       }
     }
+    if (GROUPS == 1 || group == 1) {
 #pragma unroll
-    for (int n = 0; n < KN; ++n) {
-      if (wave + 4 * n >= DC) break;
+      for (int n = 0; n < KN; ++n) {
+        if (part + 4 * n >= DC) break;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const uint32_t x = vr[n][0][u] >> (h * 4), y = vr[n][1][u] >> (h * 4);
-        lds[buf][1][(u * DC + wave + 4 * n) * 64 + lane / 16 % 2 * 32 + h * 16 + lane % 16] =
-            u32x4{two_levels<BMX_BF16, 0>(x, sixteens_v), two_levels<BMX_BF16, 2>(x, sixteens_v), two_levels<BMX_BF16, 0>(y, sixteens_v), two_levels<BMX_BF16, 2>(y, sixteens_v)};
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t x = in[n][V0][u] >> (h * 4), y = in[n][V0 + 1][u] >> (h * 4);
+          values[slot][(u * DC + part + 4 * n) * 64 + lane / 16 % 2 * 32 + h * 16 + lane % 16] =
+              u32x4{two_levels<BMX_BF16, 0>(x, sixteens_v), two_levels<BMX_BF16, 2>(x, sixteens_v), two_levels<BMX_BF16, 0>(y, sixteens_v), two_levels<BMX_BF16, 2>(y, sixteens_v)};
+        }
       }
     }
     if (wave == 0) {
@@ -457,7 +473,7 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
         scale[i] = bf16_float(x), offset[i] = __builtin_bit_cast(float, x & 0xffff0000u);
       }
       const bool none = !(fabsf(scale[1]) < INFINITY && fabsf(offset[1]) < INFINITY);
-      float* to = reinterpret_cast<float*>(of_token[buf]) + lane;
+      float* to = reinterpret_cast<float*>(of_token[slot]) + lane;
       to[0] = scale[0] * factor;
       to[64] = none ? NAN : offset[0] - 16.0f * scale[0];
       to[128] = none ? 0.0f : scale[1];
@@ -484,97 +500,193 @@ __global__ __launch_bounds__(256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv
     all += __shfl_xor(all, 32);
     all *= factor;
   }
-  if (pg < last) convert(0, pg);
-  __syncthreads();
-
+  if (pg < last) convert(0, 0, pg);
   // (what LDS holds does not come into registers all at once: there are not as many, and they would spill; where the compiler keeps to them by itself, 347 us without, 356 with)
   const auto fence = [](bool here) {
     if ((DC == 3 || DC > 4 || (DC == 4 && (SPLIT || TYPE == BMX_F16))) && here) __builtin_amdgcn_sched_barrier(0);
   };
   // held: the score that the row's weights are relative to; limit: from where on over it a score becomes the one
   float held = 0.0f, limit = -INFINITY, l = 0.0f, rest = 0.0f;
-  f32x16 o[DC] = {};
-  for (int buf = 0; pg < last; buf ^= 1) {
-    const int next = fetch(pg + 1), t0 = pg * kPage;
-    if (t0 < high_any && t0 + kPage - 1 >= low_any) {
-      f32x16 z[2] = {};
+  f32x16 o[DC] = {}, z[2];
+  u32x4 w[2][4];  // [part][16 tokens]
+  const auto scores = [&](int buf) {
+    z[0] = z[1] = f32x16{};
 #pragma unroll
-      for (int i = 0; i < NS; ++i) {
+    for (int i = 0; i < NS; ++i) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) z[t] = mfma32<TYPE == BMX_F16>(lds[buf][0][(t * NS + i) * 64 + lane], q[i], z[t]);
-        fence(i % 4 == 3);
-      }
-      const bool whole = __builtin_amdgcn_readfirstlane(kv_all_in(t0, kPage, low_all, high_all));
-      float top = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x4 scale = of_token[buf][0][t * 8 + j * 2 + h], offset = of_token[buf][1][t * 8 + j * 2 + h];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) z[t][4 * j + i] = z[t][4 * j + i] * scale[i] + (all * offset[i] - held);
-          fence(j % 2);
-        }
-      if (!whole) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const int t = t0 + i / 4 * 8 + 4 * h + i % 4;
-          z[i / 16][i % 16] = t < high && t >= low ? z[i / 16][i % 16] : -INFINITY;
-        }
-        apart(z[0]), apart(z[1]);
-      }
-#pragma unroll
-      for (int i = 0; i < 32; ++i) top = fmaxf(top, z[i / 16][i % 16]);
-      top = max_32(top);
-      if (__any(top > limit)) {  // (a row's first page, and few others)
-        const bool mine = top > limit;
-        const float up = mine ? top : 0.0f, shrink = limit == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(-up);
-        held += up, limit = mine ? kGrowth : limit;
-        l *= shrink, rest *= shrink;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) z[t] -= up;
-#pragma unroll
-        for (int n = 0; n < DC; ++n) o[n] *= shrink;
-      }
-      float sum = 0.0f, more = 0.0f;
-      u32x4 w[2][4];  // [part][16 tokens]
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const f32x4 scale = of_token[buf][2][u * 2 + h], offset = of_token[buf][3][u * 2 + h];
-        float x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e = __builtin_amdgcn_exp2f(z[u / 4][u % 4 * 4 + i]);
-          sum += e;
-          more += e * offset[i];
-          x[i] = e * scale[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t part[2];
-          pair<2>(x[i], x[i + 2], part);
-          w[0][u / 2][u % 2 * 2 + i] = part[0], w[1][u / 2][u % 2 * 2 + i] = part[1];
-        }
-        fence(u % 2);
-      }
-      l += sum, rest += more;
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int n0 = 0; n0 < DC; n0 += 4) {
-          u32x4 x[4];
-#pragma unroll
-          for (int n = 0; n < 4; ++n) x[n] = n0 + n < DC ? lds[buf][1][(u * DC + n0 + n) * 64 + lane] : u32x4{};
-#pragma unroll
-          for (int part = 0; part < 2; ++part)  // (no product waits for the one before)
-#pragma unroll
-            for (int n = 0; n < 4 && n0 + n < DC; ++n) o[n0 + n] = mfma32<false>(x[n], w[part][u], o[n0 + n]);
-          fence(true);
-        }
+      for (int t = 0; t < 2; ++t) z[t] = mfma32<TYPE == BMX_F16>(keys[buf][(t * NS + i) * 64 + lane], q[i], z[t]);
+      fence(i % 4 == 3);
     }
-    if (next < last) convert(buf ^ 1, next);
-    pg = next;
+  };
+  // scales and offsets of four tokens, KEEP times: of two groups they are on their way while those before are used
+  constexpr int KEEP = 4;
+  [[maybe_unused]] f32x4 ks[KEEP][2];
+  const auto key_scales = [&](int slot, int j) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) ks[j % KEEP][i] = of_token[slot][i][j * 2 + h];
+  };
+  const auto weights = [&](int slot, int t0) {
+    [[maybe_unused]] f32x4 vs[KEEP][2];
+    const auto value_scales = [&](int u) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) vs[u % KEEP][i] = of_token[slot][2 + i][u * 2 + h];
+    };
+    const bool whole = __builtin_amdgcn_readfirstlane(kv_all_in(t0, kPage, low_all, high_all));
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = t * 4 + j;
+        if (GROUPS == 1) key_scales(slot, at);
+        else if (at + KEEP - 1 < 8) key_scales(slot, at + KEEP - 1);
+        else value_scales(at + KEEP - 9);
+        const f32x4 scale = ks[at % KEEP][0], offset = ks[at % KEEP][1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[t][4 * j + i] = z[t][4 * j + i] * scale[i] + (all * offset[i] - held);
+        fence(j % 2);
+        if (GROUPS == 2) __builtin_amdgcn_sched_barrier(0);
+      }
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const int t = t0 + i / 4 * 8 + 4 * h + i % 4;
+        z[i / 16][i % 16] = t < high && t >= low ? z[i / 16][i % 16] : -INFINITY;
+      }
+      apart(z[0]), apart(z[1]);
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, z[i / 16][i % 16]);
+    top = max_32(top);
+    if (__any(top > limit)) {  // (a row's first page, and few others)
+      const bool mine = top > limit;
+      const float up = mine ? top : 0.0f, shrink = limit == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(-up);
+      held += up, limit = mine ? kGrowth : limit;
+      l *= shrink, rest *= shrink;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) z[t] -= up;
+#pragma unroll
+      for (int n = 0; n < DC; ++n) o[n] *= shrink;
+    }
+    float sum = 0.0f, more = 0.0f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (GROUPS == 1) value_scales(u);
+      else if (u + KEEP - 1 < 8) value_scales(u + KEEP - 1);
+      const f32x4 scale = vs[u % KEEP][0], offset = vs[u % KEEP][1];
+      float x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = __builtin_amdgcn_exp2f(z[u / 4][u % 4 * 4 + i]);
+        sum += e;
+        more += e * offset[i];
+        x[i] = e * scale[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint32_t parts[2];
+        pair<2>(x[i], x[i + 2], parts);
+        w[0][u / 2][u % 2 * 2 + i] = parts[0], w[1][u / 2][u % 2 * 2 + i] = parts[1];
+      }
+      fence(u % 2);
+      if (GROUPS == 2) __builtin_amdgcn_sched_barrier(0);
+    }
+    l += sum, rest += more;
+  };
+  const auto products = [&](int slot) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int n0 = 0; n0 < DC; n0 += 4) {
+        u32x4 x[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) x[n] = n0 + n < DC ? values[slot][(u * DC + n0 + n) * 64 + lane] : u32x4{};
+#pragma unroll
+        for (int p = 0; p < 2; ++p)  // (no product waits for the one before)
+#pragma unroll
+          for (int n = 0; n < 4 && n0 + n < DC; ++n) o[n0 + n] = mfma32<false>(x[n], w[p][u], o[n0 + n]);
+        fence(true);
+      }
+  };
+  const auto sees = [&](int pg) { return pg * kPage < high_any && pg * kPage + kPage - 1 >= low_any; };
+  if constexpr (GROUPS == 1) {
     __syncthreads();
+    for (int buf = 0; pg < last; buf ^= 1) {
+      const int next = fetch(pg + 1);
+      if (sees(pg)) {
+        scores(buf);
+        weights(buf, pg * kPage);
+        products(buf);
+      }
+      if (next < last) convert(buf ^ 1, buf ^ 1, next);
+      pg = next;
+      __syncthreads();
+    }
+  } else {
+    // The second group is a phase behind the first, and both pass as many barriers.  Keys of the page after this one go where those of the page before were, in the first
+    // group's phase, which the second has read in the phase before; values, in the second's, where those of two pages before were, and scales, in the first's, likewise.
+    // What is brought in behind the last page is read by nobody.
+    const auto phase = [&] {
+      __builtin_amdgcn_sched_barrier(0);
+      __syncthreads();
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // Products of the page before, then scores of this one, in eight parts: each part's operands are on their way two parts before it.
+    const auto both = [&](int before, int buf, int slot, const auto& other) {
+      u32x4 x[3][DC];
+      const auto load = [&](int b) {
+#pragma unroll
+        for (int n = 0; n < DC; ++n) {
+          const int e = (b - 4) * DC + n;
+          x[b % 3][n] = b < 4 ? values[before][(b * DC + n) * 64 + lane] : keys[buf][(e % 2 * NS + e / 2) * 64 + lane];
+        }
+      };
+      load(0);
+      load(1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        if (b < 6) load(b + 2);
+        if (b >= 5) key_scales(slot, b - 5);
+        if (b < 4) {
+#pragma unroll
+          for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int n = 0; n < DC; ++n) o[n] = mfma32<false>(x[b % 3][n], w[p][b], o[n]);
+        } else {
+          if (b == 4) z[0] = z[1] = f32x16{};
+#pragma unroll
+          for (int n = 0; n < DC; ++n) {
+            const int e = (b - 4) * DC + n;
+            z[e % 2] = mfma32<TYPE == BMX_F16>(x[b % 3][n], q[e / 2], z[e % 2]);
+          }
+        }
+        if (b == 1) other();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    int next = fetch(pg + 1), before = 0, slot = 0, buf = 0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) w[u / 4][u % 4] = u32x4{};  // (before the first page: nothing of that page's own values, which are finite)
+    phase();
+    if (group == 1) phase();
+    for (; pg < last; buf ^= 1) {
+      const int after = slot == SLOTS - 1 ? 0 : slot + 1, t0 = pg * kPage;
+      const auto other = [&] {
+        convert(buf ^ 1, after, next);
+        pg = next;
+        next = fetch(next + 1);
+      };
+      __builtin_amdgcn_s_setprio(1);
+      both(before, buf, slot, other);
+      __builtin_amdgcn_s_setprio(0);
+      phase();
+      weights(slot, t0);
+      phase();
+      before = slot, slot = after;
+    }
+    products(before);
+    if (group == 0) phase();
   }
   l += __shfl_xor(l, 32);
   rest += __shfl_xor(rest, 32);
@@ -704,6 +816,17 @@ Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads
   return p;
 }
 
+// Whether prompts go to workgroups of two groups, one a CU, whose first reads nobody covers: where they have many pages, are alike and fill the rounds of the chip's
+// CUs.  (us in one group, in two, 32 heads on 8 of 128 bf16, sequences x new tokens of all: 2 x 1024 of 2048 103, 90, of 1536 78, 69; 4 x 1024 of 4096 359, 332, of 2048 169,
+// 165, of 1536 120, 123; 16 x 512 of 512 93, 106; 4 x 1024 of 1024 75, 84; 3 x 700 of 2700, a round of 256 and one of 8, 171, 181; 2 x 1600 of 4096 284, 257; 2 x 2048 of 2048 118,
+// 109, but one of these alone, in one round with the short ones, 78, 83; a window of 512 69, 73; 6 ragged ones 124, 129.)
+bool two_groups(const bmx_kv4_cache& c, const Args& a, const Plan& p) {
+  if (p.prompt_splits > 1 || (c.starts && c.sequences > 1)) return false;
+  const int64_t tiles = ceil_div(p.prompt_tiles, 2) * c.heads * c.sequences, rounds = ceil_div(tiles, 256);
+  const int64_t most = a.window ? std::min(c.table_width, a.window / kPage + 2) : c.table_width, mean = a.window || !a.causal ? most : most - a.max_new / (2 * kPage);
+  return 4 * tiles >= 3 * 256 * rounds && mean >= 16 && (rounds > 1 || 3 * mean >= 2 * most);
+}
+
 template <int TYPE, int DC>
 void launch(const bmx_kv4_cache& c, const Args& a, const Plan& p, hipStream_t s) {
   // (rows of sequences as long as each other are all many or all few)
@@ -718,11 +841,15 @@ void launch(const bmx_kv4_cache& c, const Args& a, const Plan& p, hipStream_t s)
   }
   if constexpr (TYPE != BMX_F32) {
     if (p.prompt_tiles) {
-      const dim3 grid(c.heads * p.prompt_splits, (uint32_t)p.prompt_tiles, c.sequences);
+      int groups = 1;
+      auto kern = p.prompt_splits > 1 ? kv4_prompt_kernel<TYPE, DC, true, 1> : kv4_prompt_kernel<TYPE, DC, false, 1>;
+      if constexpr (DC <= 4)
+        if (two_groups(c, a, p)) kern = kv4_prompt_kernel<TYPE, DC, false, 2>, groups = 2;
+      const dim3 grid(c.heads * p.prompt_splits, (uint32_t)ceil_div(p.prompt_tiles, groups), c.sequences);
       Args b = a;
       if (!c.starts || c.sequences == 1) b.few = 0;
-      launch_kernel(p.prompt_splits > 1 ? kv4_prompt_kernel<TYPE, DC, true> : kv4_prompt_kernel<TYPE, DC, false>, grid, dim3(256), 0, s, c, b);
-      note_kernel("kv4_prompt_kernel<%d,%d,%d> grid %ux%ux%u block 256", TYPE, DC, p.prompt_splits > 1, grid.x, grid.y, grid.z);
+      launch_kernel(kern, grid, dim3(256 * groups), 0, s, c, b);
+      note_kernel("kv4_prompt_kernel<%d,%d,%d,%d> grid %ux%ux%u block %d", TYPE, DC, p.prompt_splits > 1, groups, grid.x, grid.y, grid.z, 256 * groups);
     }
   }
 }

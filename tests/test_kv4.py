@@ -317,6 +317,51 @@ def test_prompts_split_and_not(kind, dim):
     attend(cache, 8, [400, 3, 9], kind, seed=3)
 
 
+@pytest.mark.parametrize("kind,dim,named", [(torch.bfloat16, 128, {}), (torch.float16, 128, {}), (torch.float16, 96, {}), (torch.bfloat16, 64, dict(causal=False)),
+                                            (torch.bfloat16, 20, {}), (torch.float16, 64, dict(window=1000)), (torch.bfloat16, 100, dict(scale=-0.05))])
+def test_prompts_in_two_groups(kind, dim, named):
+    """Prompts alike and long enough for workgroups whose halves take turns."""
+    cache = Cache(8, dim, [1536, 1500], seed=dim)
+    attend(cache, 4, [1000, 1000], kind, seed=2, gap=dim % 3, **named)
+    assert "prompt_kernel" in B.last_kernel() and "block 512" in B.last_kernel()
+
+
+@pytest.mark.parametrize("kind", [torch.float16, torch.bfloat16])
+def test_two_groups_and_pages_that_are_not_there(kind):
+    """More than 64 pages, some of them none, the first and the last among them."""
+    cache = Cache(16, 32, [4400], seed=6)
+    there = [np.ones(4400, bool)]
+    for place, none in ((0, -1), (2, cache.num_pages), (30, TOP), (31, -7), (63, -1), (64, -1), (67, 10**6), (68, -1)):
+        cache.table[0, place] = none
+        there[0][place * 64:place * 64 + 64] = False
+    q = torch.randn((1000, 64, 32), device="cuda").to(kind)
+    out = B.kv4_attention(q, *cache.args[:2], torch.from_numpy(cache.table).cuda(), cache.args[3])
+    assert "block 512" in B.last_kernel()
+    cache.table = np.where((cache.table >= 0) & (cache.table < cache.num_pages), cache.table, 0)
+    check_attention(cache, q, [1000], out, there=there)
+    # none at all, and no tokens
+    for table, lengths in ((torch.full_like(cache.args[2], -1), cache.args[3]), (cache.args[2], torch.zeros_like(cache.args[3]))):
+        out, lse = B.kv4_attention(q, *cache.args[:2], table, lengths, lse=True)
+        assert not bool(out.any()) and bool((lse == -float("inf")).all())
+
+
+@pytest.mark.parametrize("which", [0, 1])
+def test_scales_that_are_no_numbers_in_two_groups(which):
+    """A row that does not see the token is as ever, also where its wave's rows see nothing of the token's page."""
+    cache, q = Cache(8, 64, [1536, 1500], seed=4), torch.randn((2000, 32, 64), device="cuda").bfloat16()
+    want = B.kv4_attention(q, *cache.args)
+    for value in (float("nan"), float("inf")):
+        for part in (0, 1):
+            kept = cache.scales.clone()
+            cache.scales[int(cache.table[0, 1300 // 64]), :, which, 1300 % 64, part] = value
+            out = B.kv4_attention(q, *cache.args)
+            assert "block 512" in B.last_kernel()
+            assert torch.equal(out[:1300 - 536], want[:1300 - 536]) and torch.equal(out[1000:], want[1000:])
+            if which or value != value:
+                assert not bool(torch.isfinite(out[1300 - 536:1000]).all(-1).any())
+            cache.scales.copy_(kept)
+
+
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("scale", [0.0, -0.3, 5.0, 1e-6])
 def test_attention_scales(kind, scale):
