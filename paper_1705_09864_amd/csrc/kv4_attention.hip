@@ -367,7 +367,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_attention_kernel(bmx_kv4_cache
 // wherever they change over.  So products of a page come a turn behind its weights, beside the next page's scores; the first group brings in keys, the second values.
 //
 // Bound by issue: two sequences of 2048 new tokens of 4096, 32 heads on 8 of 128 bf16, 282 us in two groups, 730 TFLOP/s by the formula's products (a third of those
-// made are the weights' lower parts), 319 in one.  Vector ALU 64 % of the time, matrix cores 54 % (63 and 48 in one group), two waves a SIMD; the products alone take
+// made are the weights' lower parts), 319 in one.  Vector ALU 66 % of the time, matrix cores 56 % (63 and 48 in one group), two waves a SIMD; the products alone take
 // 221 us, the weights alone 200.  Two tiles of 32 rows a wave, one wave a SIMD: 464.
 template <int TYPE, int DC, bool SPLIT, int GROUPS>
 __global__ __launch_bounds__(GROUPS * 256, DC <= 4 ? 2 : 1) void kv4_prompt_kernel(bmx_kv4_cache c, Args a) {
