@@ -8,7 +8,8 @@
 // Bound by the heads' bytes, in and out once.  A workgroup takes ROWS tokens: a thread makes an angle's sine and cosine, which all heads of the token
 // share, into LDS, while its first values are on their way; then 16 bytes of each side of the pairs a step.  8192 tokens of 40 heads of 128 bf16:
 // 27.7 us, 168 MB at 6.1 TB/s (half of it is still in the last caches).  64 tokens: 2.7 us, a launch and two trips to memory.  1501 of 12 heads of 80 f32, pairs
-// of neighbours: 5.0 us, 2.3 TB/s.  Heads that no 16, 8 or 4 bytes reach (98 values of 16 bits, odd elements) go by pairs: 9 to 11 us where bytes take 3.3.
+// of neighbours: 5.0 us, 2.3 TB/s.  4000 of 20 heads of 98 bf16, which 16 bytes do not divide:
+// 9.2 us, 3.4 TB/s.
 #include "bmx_internal.h"
 #include "few_bits.h"
 
@@ -50,26 +51,30 @@ struct Single {
   __device__ float get(int) const { return v; }
 };
 
-// PAIR: neighbours.  N: values of a step on each side (halves) or in all (neighbours); rows and heads lie so that N of them are one access where N > 2.
-template <int TYPE, bool PAIR, int N>
+// Steps of N values that do not divide a head's: the last one begins earlier, and makes some values a second time, or, where those are overwritten in place, is a shorter one.
+enum Last { kWhole, kEarlier, kShorter };
+// PAIR: neighbours.  N: values of a step on each side (halves) or in all (neighbours).
+template <int TYPE, bool PAIR, int N, Last LAST>
 __global__ __launch_bounds__(256) void rotary_kernel(Args a, int rows_each, int head_groups) {
   constexpr int PAIRS = PAIR ? N / 2 : N;
   extern __shared__ float2 table[];  // [row][pair]
   const int row0 = blockIdx.x / head_groups * rows_each, rows = min(rows_each, a.rows - row0), group = blockIdx.x % head_groups;
   const int head0 = (int)((int64_t)group * a.heads / head_groups), heads = (int)((int64_t)(group + 1) * a.heads / head_groups) - head0;
-  const int steps = a.half / PAIRS, items = rows * heads * steps;
+  const int steps = LAST == kWhole ? a.half / PAIRS : (a.half + PAIRS - 1) / PAIRS, items = rows * heads * steps;
   using V = std::conditional_t<N == 1, Single<TYPE>, Run<TYPE, N == 1 ? 2 : N>>;
   const auto place = [&](int e, int* row, int* j, int* head) {
     *j = e % steps * PAIRS;
+    if (LAST == kEarlier) *j = min(*j, a.half - PAIRS);
     *head = e / steps % heads + head0;
     *row = e / steps / heads;
   };
+  const auto left = [&](int j) { return LAST != kShorter ? N : PAIR ? 2 * (a.half - j) : a.half - j; };
   const auto load = [&](int e, V* u, V* w) {
     int row, j, head;
     place(e, &row, &j, &head);
     const int64_t at = (int64_t)(row0 + row) * a.x_row + head * a.x_head + (PAIR ? 2 * j : j);
-    u->load(a.x, at, N);
-    if constexpr (!PAIR) w->load(a.x, at + a.half, N);
+    u->load(a.x, at, left(j));
+    if constexpr (!PAIR) w->load(a.x, at + a.half, left(j));
   };
   V u, w;
   if ((int)threadIdx.x < items) load(threadIdx.x, &u, &w);
@@ -93,7 +98,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(Args a, int rows_each, int 
         const float x = u.get(i), y = u.get(i + 1);
         p.set2(i, x * f[i / 2].x - y * f[i / 2].y, y * f[i / 2].x + x * f[i / 2].y);
       }
-      p.store(a.out, at, N);
+      p.store(a.out, at, left(j));
     } else if constexpr (N == 1) {
       const float x = u.get(0), y = w.get(0);
       store_one<TYPE>(a.out, at, x * f[0].x - y * f[0].y);
@@ -105,21 +110,21 @@ __global__ __launch_bounds__(256) void rotary_kernel(Args a, int rows_each, int 
         p.set2(i, x0 * f[i].x - y0 * f[i].y, x1 * f[i + 1].x - y1 * f[i + 1].y);
         q.set2(i, y0 * f[i].x + x0 * f[i].y, y1 * f[i + 1].x + x1 * f[i + 1].y);
       }
-      p.store(a.out, at, N);
-      q.store(a.out, at + a.half, N);
+      p.store(a.out, at, left(j));
+      q.store(a.out, at + a.half, left(j));
     }
   }
   if (a.copy) {
     constexpr int M = N > 2 ? N : 1;
-    const int from = 2 * a.half, each = (a.dim - from) / M;
+    const int from = 2 * a.half, each = LAST == kWhole ? (a.dim - from) / M : (a.dim - from + M - 1) / M;
     for (int e = threadIdx.x; e < rows * heads * each; e += 256) {
-      const int row = row0 + e / each / heads, head = head0 + e / each % heads, d = from + e % each * M;
+      const int row = row0 + e / each / heads, head = head0 + e / each % heads, at = from + e % each * M, d = LAST == kWhole || a.dim - from < M ? at : min(at, a.dim - M);
       if constexpr (M == 1) {
         store_one<TYPE>(a.out, row * a.out_row + head * a.out_head + d, load_one<TYPE>(a.x, row * a.x_row + head * a.x_head + d));
       } else {
         Run<TYPE, M> v;
-        v.load(a.x, row * a.x_row + head * a.x_head + d, M);
-        v.store(a.out, row * a.out_row + head * a.out_head + d, M);
+        v.load(a.x, row * a.x_row + head * a.x_head + d, LAST == kWhole ? M : a.dim - d);
+        v.store(a.out, row * a.out_row + head * a.out_head + d, LAST == kWhole ? M : a.dim - d);
       }
     }
   }
@@ -130,8 +135,12 @@ void launch(const Args& a, hipStream_t s) {
   constexpr int SIZE = TYPE == BMX_F32 ? 4 : 2, WIDE = 16 / SIZE, NARROW = PAIR ? 2 : 1;
   const auto whole = [](int64_t n) { return n % WIDE == 0; };
   const bool wide = (PAIR ? whole(2 * a.half) : whole(a.half)) && (!a.copy || whole(a.dim - 2 * a.half));
-  const int n = wide ? WIDE : NARROW, pairs = PAIR ? n / 2 : n;
-  const int64_t per_row = (int64_t)a.heads * (a.half / pairs);
+  // (us in steps of 16 bytes, of single pairs: 4000 rows of 20 heads of 98 bf16 9.2, 15.2, of 100 f16 7.8, 15.0; 8000 of 96, 50 rotated, 18.2, 31.0; with a shorter last step
+  // 10.7, 10.9 and 25.6, but 64 rows of 40 heads of 98 3.5, 2.9)
+  const bool fits = (PAIR ? 2 * a.half : a.half) >= WIDE, same = a.out == a.x;
+  const bool ragged = !wide && fits && (!same || (int64_t)a.rows * a.heads >= 16384);
+  const int n = wide || ragged ? WIDE : NARROW, pairs = PAIR ? n / 2 : n;
+  const int64_t per_row = (int64_t)a.heads * ceil_div(a.half, pairs);
   // Rows of a workgroup: three steps a thread, as long as there are two workgroups a CU; heads of few rows are dealt out to several workgroups.  (us with two,
   // three, four steps: 8192 rows of 40 heads of 128 bf16 28.8, 27.6, 27.9, 9000 rows of 20 heads of 96 f16, 48 rotated, 17.7, 18.2, 20.0; with four workgroups a CU
   // 1500 rows of 12 heads of 80 f32 5.1, with two 4.6.)
@@ -139,9 +148,12 @@ void launch(const Args& a, hipStream_t s) {
   int64_t groups = std::max<int64_t>(std::min<int64_t>({(per_row + 255) / 256, a.heads, (1024 + a.rows - 1) / a.rows}), 1);
   if (rows_each > 1) groups = 1;
   const dim3 grid((uint32_t)(ceil_div(a.rows, rows_each) * groups));
-  const auto kern = wide ? rotary_kernel<TYPE, PAIR, WIDE> : rotary_kernel<TYPE, PAIR, NARROW>;
-  launch_kernel(kern, grid, dim3(256), rows_each * a.half * sizeof(float2), s, a, (int)rows_each, (int)groups);
-  note_kernel("rotary_kernel<%d,%d,%d> grid %u block 256", TYPE, PAIR, n, grid.x);
+  const auto kern = wide      ? rotary_kernel<TYPE, PAIR, WIDE, kWhole>
+                    : !ragged ? rotary_kernel<TYPE, PAIR, NARROW, kWhole>
+                    : same    ? rotary_kernel<TYPE, PAIR, WIDE, kShorter>
+                              : rotary_kernel<TYPE, PAIR, WIDE, kEarlier>;
+  launch_kernel(kern, grid, dim3(256), (rows_each * a.half + (ragged ? WIDE : 0)) * sizeof(float2), s, a, (int)rows_each, (int)groups);
+  note_kernel("rotary_kernel<%d,%d,%d,%d> grid %u block 256", TYPE, PAIR, n, ragged ? (int)(same ? kShorter : kEarlier) : (int)kWhole, grid.x);
 }
 
 }  // namespace

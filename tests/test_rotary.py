@@ -62,6 +62,24 @@ def test_sizes(kind, interleaved, rows, heads, dim, rot):
 
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rows,heads,dim,rot", [(1700, 10, 98, 98), (700, 30, 41, 18), (300, 60, 40, 34), (20, 1000, 19, 16), (2000, 9, 100, 60), (5, 3, 255, 250)])
+def test_heads_that_steps_do_not_divide(kind, interleaved, rows, heads, dim, rot):
+    """Many heads and few, into new memory among other values, and in place."""
+    g = torch.Generator(device="cuda").manual_seed(rows + dim)
+    x = torch.randn((rows, heads, dim), device="cuda", generator=g).to(kind)
+    positions = torch.randint(-50, 5000, (rows,), device="cuda", generator=g, dtype=torch.int32)
+    freq = B.rotary_frequencies(rot)
+    whole = torch.full((rows, heads, dim + 3), 7.0, device="cuda").to(kind)
+    out = whole[..., 1:dim + 1]
+    B.rotary(x, positions, freq, interleaved, out=out)
+    agrees(out, x, positions, freq, interleaved)
+    assert bool((whole[..., [0, dim + 1, dim + 2]] == 7).all())
+    B.rotary(x, positions, freq, interleaved, out=x)
+    assert torch.equal(x, out)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("dim,rot", [(128, 128), (80, 32), (66, 64), (32, 6)])
 def test_strides(kind, interleaved, dim, rot):
     """Parts of a projection's rows, on odd elements, heads in any order and apart; what lies between is left as it was."""
