@@ -43,6 +43,14 @@ __device__ inline void turn(float t, float* s, float* c) {
   *c = (q + 1) & 2 ? -v : v;
 }
 
+// A pair's values, f: cosine and sine.  Fused by hand, and kept from the compiler's products that round to 16 bits at once: whatever step makes a value makes the same bits.
+__device__ inline float one(float r) {
+  asm("" : "+v"(r));
+  return r;
+}
+__device__ inline float first(float x, float y, float2 f) { return one(fmaf(x, f.x, -(y * f.y))); }
+__device__ inline float second(float x, float y, float2 f) { return one(fmaf(y, f.x, x * f.y)); }
+
 // A value, as Run has several.
 template <int TYPE>
 struct Single {
@@ -96,19 +104,19 @@ __global__ __launch_bounds__(256) void rotary_kernel(Args a, int rows_each, int 
 #pragma unroll
       for (int i = 0; i < N; i += 2) {
         const float x = u.get(i), y = u.get(i + 1);
-        p.set2(i, x * f[i / 2].x - y * f[i / 2].y, y * f[i / 2].x + x * f[i / 2].y);
+        p.set2(i, first(x, y, f[i / 2]), second(x, y, f[i / 2]));
       }
       p.store(a.out, at, left(j));
     } else if constexpr (N == 1) {
       const float x = u.get(0), y = w.get(0);
-      store_one<TYPE>(a.out, at, x * f[0].x - y * f[0].y);
-      store_one<TYPE>(a.out, at + a.half, y * f[0].x + x * f[0].y);
+      store_one<TYPE>(a.out, at, first(x, y, f[0]));
+      store_one<TYPE>(a.out, at + a.half, second(x, y, f[0]));
     } else {
 #pragma unroll
       for (int i = 0; i < N; i += 2) {
         const float x0 = u.get(i), y0 = w.get(i), x1 = u.get(i + 1), y1 = w.get(i + 1);
-        p.set2(i, x0 * f[i].x - y0 * f[i].y, x1 * f[i + 1].x - y1 * f[i + 1].y);
-        q.set2(i, y0 * f[i].x + x0 * f[i].y, y1 * f[i + 1].x + x1 * f[i + 1].y);
+        p.set2(i, first(x0, y0, f[i]), first(x1, y1, f[i + 1]));
+        q.set2(i, second(x0, y0, f[i]), second(x1, y1, f[i + 1]));
       }
       p.store(a.out, at, left(j));
       q.store(a.out, at + a.half, left(j));
