@@ -354,6 +354,9 @@ int bmx_kv_attention(const bmx_kv_cache* cache, const void* q, int type, int64_t
  * num_pages) gives -1 in the same way.  Kernels stay inside the buffers whatever the integers are.  One call at a time works on a pool. */
 int bmx_kv_resize(const int32_t* change, int sequences, int32_t* table, int64_t table_ld, int table_width, int32_t* lengths, int32_t* pool,
                   int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int64_t rows, void* stream);
+/* The same, where the calls behind it are given max_new (0: not known): a sequence that is to have more new tokens finds no room, for they would leave those out. */
+int bmx_kv_resize_most(const int32_t* change, int sequences, int32_t* table, int64_t table_ld, int table_width, int32_t* lengths, int32_t* pool,
+                       int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int64_t rows, int max_new, void* stream);
 
 /* Heads rotated by position: of each of `rows` rows of heads (element d of head h of row r at r*x_row + h*x_head + d) the first `rot` values, an even number up
  * to dim, are pairs (a, b) that become

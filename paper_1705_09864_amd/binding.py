@@ -30,7 +30,7 @@ EXPORTS = ["bmx_binarize_pack", "bmx_xnor_gemm", "bmx_binary_fc", "bmx_pack_conv
            "bmx_binary_conv2d_bits", "bmx_xnor_gemm_count", "bmx_unpack_pm1", "bmx_widen_words32",
            "bmx_xnor_gemm_w32", "bmx_binary_fc_static", "bmx_last_kernel",
            "bmx_probe_valu", "bmx_w4_quantize", "bmx_w4_dequantize", "bmx_w4_fc", "bmx_kv_write", "bmx_kv_read",
-           "bmx_kv_attention", "bmx_kv_resize", "bmx_rotary", "bmx_kv4_write", "bmx_kv4_read", "bmx_kv4_attention"]
+           "bmx_kv_attention", "bmx_kv_resize", "bmx_kv_resize_most", "bmx_rotary", "bmx_kv4_write", "bmx_kv4_read", "bmx_kv4_attention"]
 
 _i64, _int, _p, _sz = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
 
@@ -110,10 +110,11 @@ def lib():
                                        _p, _p, _sz, _p]
         _kv4 = ctypes.POINTER(Kv4Cache)
         L.bmx_kv_resize.argtypes = [_p, _int, _p, _i64, _int, _p, _p, _int, _p, _p, _p, _i64, _p]
+        L.bmx_kv_resize_most.argtypes = L.bmx_kv_resize.argtypes[:-1] + [_int, _p]
         L.bmx_rotary.argtypes = [_p, _int, _i64, _i64, _int, _int, _i64, _p, _p, _int, _int, ctypes.c_float, _int, _p, _i64, _i64, _p]
         L.bmx_kv4_write.argtypes = L.bmx_kv4_read.argtypes = [_kv4] + L.bmx_kv_write.argtypes[1:]
         L.bmx_kv4_attention.argtypes = [_kv4] + L.bmx_kv_attention.argtypes[1:]
-        for name in EXPORTS[-11:]:
+        for name in EXPORTS[-12:]:
             getattr(L, name).restype = _int
         for name in EXPORTS[:9]:
             getattr(L, name).restype = _int
@@ -347,11 +348,14 @@ def page_pool(num_pages, device="cuda"):
     return pool.to(device)
 
 
-def kv_resize(change, table, lengths, pool, rows, starts=None, positions=None, slots=None, stream=None):
+def kv_resize(change, table, lengths, pool, rows, starts=None, positions=None, slots=None, stream=None, max_new=0):
     """Sequence i has change[i] tokens more from here on (fewer where it is below 0): lengths, table and pool follow, on the GPU.  Returns (starts, positions,
     slots): int32 [sequences + 1], the new tokens' rows as kv_write takes them; int32 [rows] and int64 [rows], each new token's position, and 64 * its page + its
     place there, -1 in rows behind the last.  Where not everything has room (in the table, in the pool, among `rows` rows) nothing changes, pool[1] is the
-    number, from 1 on, of the first sequence that has none (0 otherwise), and starts are zeros, so the calls behind it find no rows."""
+    number, from 1 on, of the first sequence that has none (0 otherwise), and starts are zeros, so the calls behind it find no rows.  max_new: that of the calls behind it, 0
+    where they are given none: a sequence that is to have more new tokens finds no room."""
+    if max_new:
+        return (_native or _host()).kv_resize_most(change, table, lengths, pool, rows, starts, positions, slots, stream, max_new)
     return (_native or _host()).kv_resize(change, table, lengths, pool, rows, starts, positions, slots, stream)
 
 

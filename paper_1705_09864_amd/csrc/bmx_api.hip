@@ -832,14 +832,20 @@ int bmx_fresh_kv_attention(const bmx_kv_cache* cache, const void* q, int type, i
 
 int bmx_kv_resize(const int32_t* change, int sequences, int32_t* table, int64_t table_ld, int table_width, int32_t* lengths, int32_t* pool,
                   int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int64_t rows, void* stream) {
-  if (sequences < 0 || sequences > kMostSequences || table_width < 0 || num_pages < 0 || num_pages > 0x7ffffffd || rows < 0 || rows >= ((int64_t)1 << 31)) return BMX_ERR_SHAPE;
+  return bmx_kv_resize_most(change, sequences, table, table_ld, table_width, lengths, pool, num_pages, starts, positions, slots, rows, 0, stream);
+}
+
+int bmx_kv_resize_most(const int32_t* change, int sequences, int32_t* table, int64_t table_ld, int table_width, int32_t* lengths, int32_t* pool,
+                       int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int64_t rows, int max_new, void* stream) {
+  if (sequences < 0 || sequences > kMostSequences || table_width < 0 || num_pages < 0 || num_pages > 0x7ffffffd || rows < 0 || rows >= ((int64_t)1 << 31) || max_new < 0)
+    return BMX_ERR_SHAPE;
   if (!pool || !starts || (sequences > 0 && (!change || !lengths || (!table && table_width > 0)))) return BMX_ERR_NULL;
   if (table_ld < table_width) return BMX_ERR_LD;
   if (misaligned(change, 4) || misaligned(table, 4) || misaligned(lengths, 4) || misaligned(pool, 4) || misaligned(starts, 4) ||
       misaligned(positions, 4) || misaligned(slots, 8))
     return BMX_ERR_ALIGN;
   return hip_status(bmx::launch_kv_resize(change, sequences, table, table_ld, table_width, lengths, pool, num_pages, starts, positions, slots, (int)rows,
-                                          (hipStream_t)stream));
+                                          (int)new_rows(max_new, rows), (hipStream_t)stream));
 }
 
 int bmx_rotary(const void* x, int type, int64_t x_row, int64_t x_head, int heads, int dim, int64_t rows, const int32_t* positions,

@@ -266,7 +266,7 @@ size_t kv_attention_workspace(int64_t sequences, int64_t table_width, int64_t he
 size_t kv_attention_workspace_of_call(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads, int64_t dim, int64_t max_new);
 // kv_pages.hip: which pages are whose.  rotary.hip: heads rotated by position.
 hipError_t launch_kv_resize(const int32_t* change, int sequences, int32_t* table, int64_t table_ld, int table_width, int32_t* lengths, int32_t* pool,
-                            int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int rows, hipStream_t s);
+                            int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int rows, int most, hipStream_t s);
 hipError_t launch_rotary(const void* x, int type, int64_t x_row, int64_t x_head, int heads, int dim, int rows, const int32_t* positions, const double* freq,
                          int rot, bool interleaved, float factor, bool inverse, void* out, int64_t out_row, int64_t out_head, hipStream_t s);
 // kv4_cache.hip, kv4_attention.hip: the cache of 4 bits and the attention over it, as those of 8.

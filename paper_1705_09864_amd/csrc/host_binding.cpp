@@ -36,6 +36,7 @@
 #pragma weak bmx_kv_attention
 #pragma weak bmx_fresh_kv_attention
 #pragma weak bmx_kv_resize
+#pragma weak bmx_kv_resize_most
 #pragma weak bmx_rotary
 #pragma weak bmx_kv4_write
 #pragma weak bmx_kv4_read
@@ -689,8 +690,8 @@ struct Numbers {
   }
 };
 
-// change, table, lengths, pool, rows, starts, positions, slots, stream -> (starts, positions, slots)
-FUNCTION(kv_resize, 9) {
+// change, table, lengths, pool, rows, starts, positions, slots, stream -> (starts, positions, slots); most: the sequences' bound of new rows, if the call has one
+PyObject* resize(Args a, const int* most) {
   T change = required(a[0], kI32, 1, "kv_resize change", true), table = required(a[1], kI32, 2, "kv_resize table");
   T lengths = required(a[2], kI32, 1, "kv_resize lengths", true), pool = required(a[3], kI32, 1, "kv_resize pool", true);
   const int64_t seqs = lengths->size(0), rows = integer(a[4]);
@@ -701,9 +702,18 @@ FUNCTION(kv_resize, 9) {
   Numbers starts(a[5], kI32, seqs + 1, lengths, "kv_resize starts"), positions(a[6], kI32, rows, lengths, "kv_resize positions");
   Numbers slots(a[7], at::kLong, rows, lengths, "kv_resize slots");
   const hipStream_t s = stream_of(a[8]);
-  call("bmx_kv_resize", bmx_kv_resize, ptr<int32_t>(change), as_int(seqs), ptr<int32_t>(table), ld(table), as_int(table->size(1)), ptr<int32_t>(lengths),
-       ptr<int32_t>(pool), as_int(pool->size(0) - 2), ptr<int32_t>(starts.t), ptr<int32_t>(positions.t), ptr<int64_t>(slots.t), rows, s);
+  const auto make = [&](const char* name, auto f, auto... more) {
+    call(name, f, ptr<int32_t>(change), as_int(seqs), ptr<int32_t>(table), ld(table), as_int(table->size(1)), ptr<int32_t>(lengths), ptr<int32_t>(pool),
+         as_int(pool->size(0) - 2), ptr<int32_t>(starts.t), ptr<int32_t>(positions.t), ptr<int64_t>(slots.t), rows, more..., s);
+  };
+  if (most) make("bmx_kv_resize_most", bmx_kv_resize_most, *most);
+  else make("bmx_kv_resize", bmx_kv_resize);
   return Py_BuildValue("NNN", starts.result(), positions.result(), slots.result());
+}
+FUNCTION(kv_resize, 9) { return resize(a, nullptr); }
+FUNCTION(kv_resize_most, 10) {  // and max_new
+  const int most = small(a[9]);
+  return resize(a, &most);
 }
 
 // x, positions, freq, interleaved, factor, inverse, out, stream -> out
@@ -741,7 +751,7 @@ PyMethodDef methods[] = {ENTRY(binarize_pack), ENTRY(unpack_pm1), ENTRY(xnor_gem
                          ENTRY(pack_conv_weights), ENTRY(binary_conv2d), ENTRY(pack_nchw), ENTRY(binary_conv2d_packed),
                          ENTRY(binary_conv2d_bits), ENTRY(quant_gemm), ENTRY(alpha_mean_abs),
                          ENTRY(w4_quantize), ENTRY(w4_dequantize), ENTRY(w4_fc), ENTRY(kv_write), ENTRY(kv_read),
-                         ENTRY(kv_attention), ENTRY(kv_resize), ENTRY(rotary), ENTRY(kv4_write), ENTRY(kv4_read), ENTRY(kv4_attention),
+                         ENTRY(kv_attention), ENTRY(kv_resize), ENTRY(kv_resize_most), ENTRY(rotary), ENTRY(kv4_write), ENTRY(kv4_read), ENTRY(kv4_attention),
                          {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bmx_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -24,8 +24,16 @@ struct Args {
   int32_t* positions;  // or null, like slots
   int64_t* slots;
   int sequences, table_width, num_pages, rows;
+  int most;  // new rows that a sequence may have
   bool wide;  // positions and slots lie on 16 bytes
 };
+
+// A sequence's change, which also fits only if the calls behind this one take all its rows.
+__device__ inline KvChange change_of(const Args& a, int tokens, int change) {
+  KvChange c = kv_change_of(tokens, change, a.table_width);
+  c.fits = c.fits && c.more <= a.most;
+  return c;
+}
 
 // Sums of numbers that are not negative, 2^32 - 1 where they are more.
 __device__ inline uint32_t plus(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
@@ -82,7 +90,7 @@ __global__ __launch_bounds__(THREADS) void kv_resize_kernel(Args a) {
     c[j].fits = true;
     if (mine + j < n) {
       const int tokens = a.lengths[mine + j];
-      c[j] = kv_change_of(tokens, a.change[mine + j], a.table_width);
+      c[j] = change_of(a, tokens, a.change[mine + j]);
       s.pages_of[mine + j] = c[j].pages, s.first_of[mine + j] = tokens;
     }
     v[0] = plus(v[0], max(c[j].pages - c[j].pages_then, 0)), v[1] = plus(v[1], max(c[j].pages_then - c[j].pages, 0)), v[2] = plus(v[2], c[j].more);
@@ -198,7 +206,7 @@ __global__ __launch_bounds__(THREADS) void kv_resize_many_kernel(Args a) {
     c.fits = true;
     if (i < a.sequences) {
       tokens = a.lengths[i];
-      c = kv_change_of(tokens, a.change[i], a.table_width);
+      c = change_of(a, tokens, a.change[i]);
     }
     v[0] = max(c.pages - c.pages_then, 0), v[1] = max(c.pages_then - c.pages, 0), v[2] = c.more;
 #pragma unroll
@@ -294,8 +302,8 @@ void launch(const Args& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_kv_resize(const int32_t* change, int sequences, int32_t* table, int64_t table_ld, int table_width, int32_t* lengths, int32_t* pool,
-                            int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int rows, hipStream_t s) {
-  const Args a = {change, table, table_ld, lengths, pool, starts, positions, slots, sequences, table_width, num_pages, rows,
+                            int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int rows, int most, hipStream_t s) {
+  const Args a = {change, table, table_ld, lengths, pool, starts, positions, slots, sequences, table_width, num_pages, rows, most,
                   (uintptr_t)positions % 16 == 0 && (uintptr_t)slots % 16 == 0};
   if (sequences <= 256) {
     launch<256, 1>(a, s);

@@ -53,10 +53,10 @@ class DevicePages:
         self.lengths = torch.zeros((sequences,), dtype=torch.int32, device=device)
         self.pool = B.page_pool(num_pages, device)
 
-    def resize(self, change, rows):
-        """change: int32 [sequences], on the GPU: so many tokens more, or fewer.  Returns starts, positions and slots of the new tokens, `rows` of them at most
-        (kv_resize).  Where not everything has room nothing changes, the starts are zeros, and refused() is above 0 from the call on."""
-        return B.kv_resize(change, self.table, self.lengths, self.pool, rows)
+    def resize(self, change, rows, most=0):
+        """change: int32 [sequences], on the GPU: so many tokens more, or fewer.  Returns starts, positions and slots of the new tokens, `rows` of them at most, and `most`
+        of one sequence (0: not known) (kv_resize).  Where not everything has room nothing changes, the starts are zeros, and refused() is above 0 from the call on."""
+        return B.kv_resize(change, self.table, self.lengths, self.pool, rows, max_new=most)
 
     def refused(self):
         """The number, from 1 on, of the first sequence that found no room in the last call, 0 if all did; waits for the GPU."""
@@ -98,8 +98,8 @@ class FewBitAttention:
 
     def step(self, x, where, new, most=0):
         """x [rows, hidden], the sequences' new tokens in their order.  `where`: their Pages, and new[i] more tokens of sequence i, sum(new) rows; or their
-        DevicePages, and `new` an int32 tensor on the GPU, below 0 where a sequence loses tokens, `most` the most of one sequence (0: not known).  Then rows behind the last
-        new token's come back as zeros, and where not everything has room all of them (where.refused()).  Pages that refuse a step are unchanged, and so is the
+        DevicePages, and `new` an int32 tensor on the GPU, below 0 where a sequence loses tokens, `most` the most of one sequence (0: not known; one that is
+        to have more finds no room).  Then rows behind the last new token's come back as zeros, and where not everything has room all of them (where.refused()).  Pages that refuse a step are unchanged, and so is the
         cache.  Steps on DevicePages can be captured into a graph once a step of their sizes has run."""
         on_gpu = isinstance(where, DevicePages)
         if on_gpu:
@@ -110,7 +110,7 @@ class FewBitAttention:
         rows = B.w4_fc(x, *self.qkv, self.n_qkv).view(x.shape[0], self.heads + 2 * self.kv_heads, self.dim)
         if on_gpu:
             sequences = where.lengths.numel()
-            starts, positions, _ = where.resize(new, x.shape[0])
+            starts, positions, _ = where.resize(new, x.shape[0], most)
         else:
             sequences, most = len(new), max(new)
             before = list(where.tokens)
