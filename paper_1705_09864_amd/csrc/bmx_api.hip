@@ -3,6 +3,7 @@
 // ran and no output byte was written.  The contract of each call is in include/bmx.h.
 #include "../../include/bmx.h"
 #include "bmx_internal.h"
+#include "kv_range.h"
 #include "lazy_calls.h"
 
 #include <mutex>
@@ -114,6 +115,10 @@ int kv_check(const Cache* c, int type, int64_t rows, int* max_new) {
     return BMX_ERR_ALIGN;
   return BMX_OK;
 }
+
+// Whether a workgroup of 256 for each page that new rows may lie in is a launch: 2^32 threads along its first dimension would be none.
+template <class Cache>
+bool pages_fit(const Cache& c, int max_new) { return c.sequences * bmx::kv_pages_of(max_new) < ((int64_t)1 << 24); }
 
 // Rows of heads in memory.
 int kv_rows_check(const void* p, int type, int64_t row, int64_t head, int64_t rows, int heads, int dim) {
@@ -802,6 +807,7 @@ int bmx_kv_write(const bmx_kv_cache* cache, const void* k, const void* v, int ty
                  int64_t v_head, int64_t rows, int max_new, void* stream) {
   int st = kv_check(cache, type, rows, &max_new);
   if (st != BMX_OK || rows == 0) return st;
+  if (!pages_fit(*cache, max_new)) return BMX_ERR_SHAPE;
   if ((st = kv_rows_check(k, type, k_row, k_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
   if ((st = kv_rows_check(v, type, v_row, v_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
   return hip_status(bmx::launch_kv_write(*cache, k, v, type, k_row, k_head, v_row, v_head, (int)rows, max_new, (hipStream_t)stream));
@@ -811,6 +817,7 @@ int bmx_kv_read(const bmx_kv_cache* cache, void* k, void* v, int type, int64_t k
                 int64_t rows, int max_new, void* stream) {
   int st = kv_check(cache, type, rows, &max_new);
   if (st != BMX_OK || rows == 0) return st;
+  if (!pages_fit(*cache, max_new)) return BMX_ERR_SHAPE;
   if ((st = kv_rows_check(k, type, k_row, k_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
   if ((st = kv_rows_check(v, type, v_row, v_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
   return hip_status(bmx::launch_kv_read(*cache, k, v, type, k_row, k_head, v_row, v_head, (int)rows, max_new, (hipStream_t)stream));
@@ -868,6 +875,7 @@ int bmx_kv4_write(const bmx_kv4_cache* cache, const void* k, const void* v, int 
                   int64_t v_head, int64_t rows, int max_new, void* stream) {
   int st = kv_check(cache, type, rows, &max_new);
   if (st != BMX_OK || rows == 0) return st;
+  if (!pages_fit(*cache, max_new)) return BMX_ERR_SHAPE;
   if ((st = kv_rows_check(k, type, k_row, k_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
   if ((st = kv_rows_check(v, type, v_row, v_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
   return hip_status(bmx::launch_kv4_write(*cache, k, v, type, k_row, k_head, v_row, v_head, (int)rows, max_new, (hipStream_t)stream));
@@ -877,6 +885,7 @@ int bmx_kv4_read(const bmx_kv4_cache* cache, void* k, void* v, int type, int64_t
                  int64_t rows, int max_new, void* stream) {
   int st = kv_check(cache, type, rows, &max_new);
   if (st != BMX_OK || rows == 0) return st;
+  if (!pages_fit(*cache, max_new)) return BMX_ERR_SHAPE;
   if ((st = kv_rows_check(k, type, k_row, k_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
   if ((st = kv_rows_check(v, type, v_row, v_head, rows, cache->heads, cache->dim)) != BMX_OK) return st;
   return hip_status(bmx::launch_kv4_read(*cache, k, v, type, k_row, k_head, v_row, v_head, (int)rows, max_new, (hipStream_t)stream));
