@@ -96,23 +96,32 @@ class FewBitAttention:
             self.kept.append(self.scratch)
         return self.scratch
 
+    def check(self, rows, sequences, most):
+        """Refuses what a step's later calls would (include/bmx.h), before its first one changes anything."""
+        if most < 0:
+            raise ValueError("most must not be below 0 (got %d)" % most)
+        each = min(most or rows, rows)
+        if each * (self.heads // self.kv_heads) > 65535 * 16 or sequences * ((each + 62) // 64 + 1) >= 1 << 24 or (self.freq is not None and rows > 1 << 23):
+            raise ValueError("%d rows, up to %d for each of %d sequences, are more than a step takes%s" % (rows, each, sequences, "" if most else ": give `most`"))
+
     def step(self, x, where, new, most=0):
         """x [rows, hidden], the sequences' new tokens in their order.  `where`: their Pages, and new[i] more tokens of sequence i, sum(new) rows; or their
-        DevicePages, and `new` an int32 tensor on the GPU, below 0 where a sequence loses tokens, `most` the most of one sequence (0: not known; one that is
-        to have more finds no room).  Then rows behind the last new token's come back as zeros, and where not everything has room all of them (where.refused()).  Pages that refuse a step are unchanged, and so is the
-        cache.  Steps on DevicePages can be captured into a graph once a step of their sizes has run."""
+        DevicePages, and `new` an int32 tensor on the GPU, below 0 where a sequence loses tokens, `most` the most of one sequence: one that is to have more finds no
+        room.  (0: not known; then every sequence is taken to have all rows, so the launches are as large, kernels for prompts do the work of steps, and rows times heads that share
+        one of the cache are 1048560 at most.)  Rows behind the last new token's come back as zeros, and where not everything has room all of them (where.refused()).  Pages
+        that refuse a step are unchanged, and so is the cache.  Steps on DevicePages can be captured into a graph once a step of their sizes has run."""
         on_gpu = isinstance(where, DevicePages)
         if on_gpu:
             if x.dim() != 2 or x.shape[1] != self.hidden:
                 raise ValueError("x: expected the shape [rows, %d], got %r" % (self.hidden, list(x.shape)))
         elif x.dim() != 2 or tuple(x.shape) != (sum(new), self.hidden):
             raise ValueError("x: expected the shape [%d, %d], got %r" % (sum(new), self.hidden, list(x.shape)))
+        sequences, most = where.lengths.numel(), most if on_gpu else max(new, default=0)
+        self.check(x.shape[0], sequences, most)
         rows = B.w4_fc(x, *self.qkv, self.n_qkv).view(x.shape[0], self.heads + 2 * self.kv_heads, self.dim)
         if on_gpu:
-            sequences = where.lengths.numel()
             starts, positions, _ = where.resize(new, x.shape[0], most)
         else:
-            sequences, most = len(new), max(new)
             before = list(where.tokens)
             starts = where.extend(new)
             if self.freq is not None:

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_1705_09864_amd import binding as B
-from paper_1705_09864_amd.decoder_layer import DevicePages, FewBitAttention
+from paper_1705_09864_amd.decoder_layer import DevicePages, FewBitAttention, Pages
 
 
 def make(bits, num_pages=40, **named):
@@ -33,3 +33,31 @@ def test_more_new_tokens_than_said(bits):
         assert all(torch.equal(a, b) for a, b in zip(now, before))
     y = layer.step(x, where, gpu([3, -1, 2]), most=3)
     assert where.refused() == 0 and bool(y.any(1).all()) and where.lengths.tolist() == [73, 0, 7]
+
+
+class Changed(Exception):
+    pass
+
+
+@pytest.mark.parametrize("rows,sequences,most,heads,freq", [(131071, 2, 0, 8, None), (131071, 2, 131071, 8, None), (1048561, 1, 0, 1, None), (2**20, 1024, 0, 1, None),
+                                                            (5, 2, -1, 8, None), ((1 << 23) + 1, 65535, 1, 1, 1)])
+@pytest.mark.parametrize("bits", [8, 4])
+def test_what_later_calls_refuse(monkeypatch, bits, rows, sequences, most, heads, freq):
+    """Refused on the host, while the pages are as they were."""
+    def change(*args, **named):
+        raise Changed
+    monkeypatch.setattr(B, "w4_fc", lambda x, n: torch.zeros(()).expand(x.shape[0], n))
+    monkeypatch.setattr(B, "kv_resize", change)
+    layer = FewBitAttention.__new__(FewBitAttention)
+    layer.__dict__.update(heads=heads, kv_heads=1, dim=8, hidden=1, n_qkv=(heads + 2) * 8, n_out=1, bits=bits, qkv=(), out=(), interleaved=False, scratch=None, kept=[],
+                          freq=freq, pages=torch.zeros((4, 1), dtype=torch.uint8), scales=None)
+    x = torch.zeros(()).expand(rows, 1)
+    where = DevicePages(4, sequences, 3, device="cpu")
+    with pytest.raises(ValueError, match="than a step takes|below 0"):
+        layer.step(x, where, torch.zeros((sequences,), dtype=torch.int32), most=most)
+    if most == 131071:
+        where = Pages(3000, 2, 2500, device="cpu")
+        layer.pages = torch.zeros((3000, 1), dtype=torch.uint8)
+        with pytest.raises(ValueError, match="than a step takes"):
+            layer.step(x, where, [rows, 0])
+        assert where.tokens == [0, 0] and len(where.free) == 3000
