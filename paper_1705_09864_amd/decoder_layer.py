@@ -73,13 +73,18 @@ class FewBitAttention:
     def __init__(self, w_qkv, w_out, heads, kv_heads, dim, num_pages, group=128, block=16, bits=8, freq=None, interleaved=False):
         if bits not in (4, 8):
             raise ValueError("bits must be 4 or 8 (got %r)" % (bits,))
+        if kv_heads <= 0 or heads <= 0 or heads % kv_heads or heads + kv_heads > 65535 or not 0 < dim <= 256:
+            raise ValueError("%d heads, a multiple of the cache's %d, of up to 256 values (got %d): a step would refuse others" % (heads, kv_heads, dim))
         self.heads, self.kv_heads, self.dim, self.bits, self.freq, self.interleaved = heads, kv_heads, dim, bits, freq, interleaved
         self.n_qkv, self.n_out, self.hidden = w_qkv.shape[0], w_out.shape[0], w_qkv.shape[1]
         if self.n_qkv != (heads + 2 * kv_heads) * dim or w_out.shape[1] != heads * dim:
             raise ValueError("w_qkv and w_out do not fit the heads")
+        if freq is not None:
+            if 2 * freq.numel() > dim:
+                raise ValueError("freq: more pairs than a head has")
+            if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.numel() or not freq.is_contiguous() or freq.device != w_qkv.device:
+                raise ValueError("freq: expected angles in float64, one dimension of them, beside the weights (got %s %r on %s)" % (freq.dtype, list(freq.shape), freq.device))
         self.qkv, self.out = B.w4_quantize(w_qkv, group), B.w4_quantize(w_out, group)
-        if freq is not None and 2 * freq.numel() > dim:
-            raise ValueError("freq: more pairs than a head has")
         if bits == 4:
             self.pages, self.scales = B.kv4_cache(num_pages, kv_heads, dim, device=w_qkv.device)
         else:

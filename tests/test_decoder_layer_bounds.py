@@ -61,3 +61,12 @@ def test_what_later_calls_refuse(monkeypatch, bits, rows, sequences, most, heads
         with pytest.raises(ValueError, match="than a step takes"):
             layer.step(x, where, [rows, 0])
         assert where.tokens == [0, 0] and len(where.free) == 3000
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,freq", [(3, 2, 8, None), (2, 0, 8, None), (1, 1, 257, None), (1, 2, 8, None), (65535, 1, 1, None),
+                                                     (2, 1, 8, torch.zeros(4)), (2, 1, 8, torch.zeros((2, 2)).double()), (2, 1, 8, torch.zeros(0).double()),
+                                                     (2, 1, 8, torch.zeros(8).double()[::2]), (2, 1, 8, torch.zeros(4, dtype=torch.float64, device="meta"))])
+def test_layers_whose_steps_would_be_refused(heads, kv_heads, dim, freq):
+    """What each step would refuse behind its first calls is refused when the layer is made."""
+    with pytest.raises(ValueError, match="a step would refuse|freq: expected"):
+        FewBitAttention(torch.zeros(((heads + 2 * kv_heads) * dim, 4)), torch.zeros((4, heads * dim)), heads, kv_heads, dim, 3, freq=freq)
