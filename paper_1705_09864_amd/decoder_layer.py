@@ -14,6 +14,7 @@ class Pages:
     """Which pages of a cache are whose: a table of page numbers, a row for each sequence, and each one's tokens."""
 
     def __init__(self, num_pages, sequences, pages_each, device="cuda"):
+        self.num_pages = num_pages
         self.free = list(range(num_pages - 1, -1, -1))
         self.count = [0] * sequences
         self.tokens = [0] * sequences
@@ -51,6 +52,7 @@ class DevicePages:
     def __init__(self, num_pages, sequences, pages_each, device="cuda"):
         self.table = torch.zeros((sequences, pages_each), dtype=torch.int32, device=device)
         self.lengths = torch.zeros((sequences,), dtype=torch.int32, device=device)
+        self.num_pages = num_pages
         self.pool = B.page_pool(num_pages, device)
 
     def resize(self, change, rows, most=0):
@@ -123,6 +125,8 @@ class FewBitAttention:
             raise ValueError("x: expected the shape [%d, %d], got %r" % (sum(new), self.hidden, list(x.shape)))
         sequences, most = where.lengths.numel(), most if on_gpu else max(new, default=0)
         self.check(x.shape[0], sequences, most)
+        if where.num_pages > self.pages.shape[0]:  # (tokens on a page that the cache does not have would not be there)
+            raise ValueError("the sequences have %d pages, the cache %d" % (where.num_pages, self.pages.shape[0]))
         rows = B.w4_fc(x, *self.qkv, self.n_qkv).view(x.shape[0], self.heads + 2 * self.kv_heads, self.dim)
         if on_gpu:
             starts, positions, _ = where.resize(new, x.shape[0], most)

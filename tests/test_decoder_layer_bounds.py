@@ -70,3 +70,17 @@ def test_layers_whose_steps_would_be_refused(heads, kv_heads, dim, freq):
     """What each step would refuse behind its first calls is refused when the layer is made."""
     with pytest.raises(ValueError, match="a step would refuse|freq: expected"):
         FewBitAttention(torch.zeros(((heads + 2 * kv_heads) * dim, 4)), torch.zeros((4, heads * dim)), heads, kv_heads, dim, 3, freq=freq)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 4])
+def test_more_pages_than_the_cache_has(bits):
+    """Tokens on pages behind the cache's end would be left out of every answer."""
+    layer, g = make(bits, num_pages=2)
+    x = torch.randn((130, 200), device="cuda", generator=g).bfloat16()
+    host, device = Pages(3, 1, 4), DevicePages(3, 1, 4)
+    for where, new in ((host, [130]), (device, gpu([130]))):
+        with pytest.raises(ValueError, match="3 pages, the cache 2"):
+            layer.step(x, where, new)
+    assert host.tokens == [0] and device.lengths.tolist() == [0]
+    assert bool(layer.step(x[:128], DevicePages(2, 1, 4), gpu([128])).any(1).all())
