@@ -95,10 +95,13 @@ class FewBitAttention:
 
     def workspace(self, sequences, width, most):
         """The attention's scratch memory: zeros before its first use, kept from step to step, also where a larger one takes its place (a captured step goes on
-        using it)."""
+        using it).  One that does is enough for any number of new rows: prompts of rising lengths do not leave one for each."""
         op = B.OP_KV4_ATTENTION if self.bits == 4 else B.OP_KV_ATTENTION
-        need = B.workspace_bytes(op, (sequences, width, self.kv_heads, self.heads, self.dim, most))
+        sizes = (sequences, width, self.kv_heads, self.heads, self.dim)
+        need = B.workspace_bytes(op, sizes + (most,))
         if self.scratch is None or self.scratch.numel() < need:
+            if self.scratch is not None:
+                need = B.workspace_bytes(op, sizes + (0,))
             self.scratch = torch.zeros((max(need, 16),), dtype=torch.uint8, device=self.pages.device)
             self.kept.append(self.scratch)
         return self.scratch

@@ -84,3 +84,18 @@ def test_more_pages_than_the_cache_has(bits):
             layer.step(x, where, new)
     assert host.tokens == [0] and device.lengths.tolist() == [0]
     assert bool(layer.step(x[:128], DevicePages(2, 1, 4), gpu([128])).any(1).all())
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("heads,kv_heads,width", [(8, 2, 512), (32, 8, 2048), (1, 1, 10)])
+def test_scratch_memory_of_growing_prompts(bits, heads, kv_heads, width):
+    """Prompts a token longer each: every step has what it needs, and what is held in all is less than two of what any number of rows needs."""
+    layer = FewBitAttention.__new__(FewBitAttention)
+    layer.__dict__.update(heads=heads, kv_heads=kv_heads, dim=128, bits=bits, scratch=None, kept=[], pages=torch.zeros(0))
+    op = B.OP_KV4_ATTENTION if bits == 4 else B.OP_KV_ATTENTION
+    bound = B.workspace_bytes(op, (1, width, kv_heads, heads, 128, 0))
+    for most in [*range(1, 2049), 0]:
+        assert layer.workspace(1, width, most).numel() >= B.workspace_bytes(op, (1, width, kv_heads, heads, 128, most))
+        assert sum(t.numel() for t in layer.kept) <= 2 * max(bound, 16)
+    first = layer.workspace(1, width, 1)
+    assert first is layer.workspace(1, width, 700) is layer.scratch and first is layer.kept[-1] and not bool(first.any())
