@@ -100,6 +100,8 @@ class FewBitAttention:
         sizes = (sequences, width, self.kv_heads, self.heads, self.dim)
         need = B.workspace_bytes(op, sizes + (most,))
         if self.scratch is None or self.scratch.numel() < need:
+            if self.pages.is_cuda and torch.cuda.is_current_stream_capturing():  # (its zeros would be the graph's, and steps beside it would begin with anything)
+                raise ValueError("a step of these sizes has to run before one is captured")
             if self.scratch is not None:
                 need = B.workspace_bytes(op, sizes + (0,))
             self.scratch = torch.zeros((max(need, 16),), dtype=torch.uint8, device=self.pages.device)
@@ -130,6 +132,7 @@ class FewBitAttention:
         self.check(x.shape[0], sequences, most)
         if where.num_pages > self.pages.shape[0]:  # (tokens on a page that the cache does not have would not be there)
             raise ValueError("the sequences have %d pages, the cache %d" % (where.num_pages, self.pages.shape[0]))
+        scratch = self.workspace(sequences, where.table.shape[1], most)
         rows = B.w4_fc(x, *self.qkv, self.n_qkv).view(x.shape[0], self.heads + 2 * self.kv_heads, self.dim)
         if on_gpu:
             starts, positions, _ = where.resize(new, x.shape[0], most)
@@ -147,7 +150,7 @@ class FewBitAttention:
         write(k, v, *cache, starts=starts, max_new=most)
         # (rows of no sequence are not written)
         out = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if on_gpu else None
-        o = attention(q, *cache, starts=starts, max_new=most, out=out, workspace=self.workspace(sequences, where.table.shape[1], most))
+        o = attention(q, *cache, starts=starts, max_new=most, out=out, workspace=scratch)
         return B.w4_fc(o.view(x.shape[0], self.heads * self.dim), *self.out, self.n_out)
 
 

@@ -99,3 +99,26 @@ def test_scratch_memory_of_growing_prompts(bits, heads, kv_heads, width):
         assert sum(t.numel() for t in layer.kept) <= 2 * max(bound, 16)
     first = layer.workspace(1, width, 1)
     assert first is layer.workspace(1, width, 700) is layer.scratch and first is layer.kept[-1] and not bool(first.any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 4])
+def test_captured_before_it_ran(bits):
+    """New scratch memory in a capture would be zeros in the graph's replays alone; the capture is refused, and the layer goes on as before."""
+    layer, g = make(bits)
+    where, x, new = DevicePages(40, 2, 20), torch.randn((2, 200), device="cuda", generator=g).bfloat16(), gpu([1, 1])
+    torch.cuda.synchronize()
+    for _ in range(2):
+        with pytest.raises(ValueError, match="has to run before"):
+            with torch.cuda.graph(torch.cuda.CUDAGraph()):
+                layer.step(x, where, new, most=1)
+    assert layer.scratch is None and where.lengths.tolist() == [0, 0]
+    y = layer.step(x, where, new, most=1)
+    where.resize(-new, 0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        z = layer.step(x, where, new, most=1)
+    for _ in range(3):
+        graph.replay()
+        where.resize(-new, 0)
+        assert torch.equal(y, z) and where.lengths.tolist() == [0, 0]
