@@ -578,46 +578,48 @@ bmx_kv4_cache cache4_of(PyObject* p, PyObject* s, PyObject* t, PyObject* n, PyOb
           as_int(seqs), as_int(table->size(1)), as_int(pages->size(0)), as_int(pages->size(1)), as_int(dim)};
 }
 
-// The calls on either cache; of: what makes its description, name: the call's.
+// The calls on either cache; of: what makes its description, name: the call's, and its arguments'.
+struct WriteNames { const char *call, *k, *v; };
 template <class Of, class F>
-PyObject* write_rows(Args a, Of of, F f, const char* name) {
-  T k = values(a[0], 3, "kv_write k");
+PyObject* write_rows(Args a, Of of, F f, const WriteNames& name) {
+  T k = values(a[0], 3, name.k);
   const at::ScalarType type = k->scalar_type();
-  T v = values(a[1], 3, "kv_write v", &type);
+  T v = values(a[1], 3, name.v, &type);
   const auto c = of(a[2], a[3], a[4], a[5], a[6], k->size(2));
-  shape(k, {k->size(0), c.heads, c.dim}, "kv_write k");
-  shape(v, {k->size(0), c.heads, c.dim}, "kv_write v");
+  shape(k, {k->size(0), c.heads, c.dim}, name.k);
+  shape(v, {k->size(0), c.heads, c.dim}, name.v);
   const int max_new = small(a[7]);
   const hipStream_t s = stream_of(a[8]);
-  call(name, f, &c, k->data_ptr(), v->data_ptr(), type_of(type), k->stride(0), k->stride(1), v->stride(0), v->stride(1), k->size(0), max_new, s);
+  call(name.call, f, &c, k->data_ptr(), v->data_ptr(), type_of(type), k->stride(0), k->stride(1), v->stride(0), v->stride(1), k->size(0), max_new, s);
   Py_RETURN_NONE;
 }
 
 FUNCTION(kv_write, 9) {  // k, v, pages, scales, table, lengths, starts, max_new, stream
-  return write_rows(a, cache_of, bmx_kv_write, "bmx_kv_write");
+  return write_rows(a, cache_of, bmx_kv_write, {"bmx_kv_write", "kv_write k", "kv_write v"});
 }
-FUNCTION(kv4_write, 9) { return write_rows(a, cache4_of, bmx_kv4_write, "bmx_kv4_write"); }
+FUNCTION(kv4_write, 9) { return write_rows(a, cache4_of, bmx_kv4_write, {"bmx_kv4_write", "kv4_write k", "kv4_write v"}); }
 
 // pages, scales, table, lengths, dim, dtype, rows, starts, max_new, out_k, out_v, stream -> (k, v)
+struct ReadNames { const char *call, *dtype, *k, *v; };
 template <class Of, class F>
-PyObject* read_rows(Args a, Of of, F f, const char* name) {
+PyObject* read_rows(Args a, Of of, F f, const ReadNames& name) {
   const auto c = of(a[0], a[1], a[2], a[3], a[7], integer(a[4]));
-  if (!THPDtype_Check(a[5])) raise_value("%s: expected a torch.dtype, got %s", "kv_read dtype", Py_TYPE(a[5])->tp_name);
+  if (!THPDtype_Check(a[5])) raise_value("%s: expected a torch.dtype, got %s", name.dtype, Py_TYPE(a[5])->tp_name);
   const at::ScalarType type = reinterpret_cast<THPDtype*>(a[5])->scalar_type;
-  if (type_of(type) < 0) raise_value("%s: %s, expected Float, Half or BFloat16", "kv_read dtype", c10::toString(type));
+  if (type_of(type) < 0) raise_value("%s: %s, expected Float, Half or BFloat16", name.dtype, c10::toString(type));
   const int64_t rows = integer(a[6]);
-  if (rows < 0) check_status(BMX_ERR_SHAPE, name);
+  if (rows < 0) check_status(BMX_ERR_SHAPE, name.call);
   T pages = &THPVariable_Unpack(a[0]), k, v;
   std::optional<Out> ok, ov;
   if (a[9] == Py_None) k = ok.emplace(Py_None, type, at::IntArrayRef({rows, c.heads, c.dim}), pages, "").t;
-  else k = values(a[9], 3, "kv_read out_k", &type);
+  else k = values(a[9], 3, name.k, &type);
   if (a[10] == Py_None) v = ov.emplace(Py_None, type, at::IntArrayRef({rows, c.heads, c.dim}), pages, "").t;
-  else v = values(a[10], 3, "kv_read out_v", &type);
-  shape(k, {rows, c.heads, c.dim}, "kv_read out_k");
-  shape(v, {rows, c.heads, c.dim}, "kv_read out_v");
+  else v = values(a[10], 3, name.v, &type);
+  shape(k, {rows, c.heads, c.dim}, name.k);
+  shape(v, {rows, c.heads, c.dim}, name.v);
   const int max_new = small(a[8]);
   const hipStream_t s = stream_of(a[11]);
-  call(name, f, &c, k->data_ptr(), v->data_ptr(), type_of(type), k->stride(0), k->stride(1), v->stride(0), v->stride(1),
+  call(name.call, f, &c, k->data_ptr(), v->data_ptr(), type_of(type), k->stride(0), k->stride(1), v->stride(0), v->stride(1),
        rows, max_new, s);
   PyObject* r = PyTuple_New(2);
   if (!r) throw python_error();
@@ -629,13 +631,14 @@ PyObject* read_rows(Args a, Of of, F f, const char* name) {
   }
   return r;
 }
-FUNCTION(kv_read, 12) { return read_rows(a, cache_of, bmx_kv_read, "bmx_kv_read"); }
-FUNCTION(kv4_read, 12) { return read_rows(a, cache4_of, bmx_kv4_read, "bmx_kv4_read"); }
+FUNCTION(kv_read, 12) { return read_rows(a, cache_of, bmx_kv_read, {"bmx_kv_read", "kv_read dtype", "kv_read out_k", "kv_read out_v"}); }
+FUNCTION(kv4_read, 12) { return read_rows(a, cache4_of, bmx_kv4_read, {"bmx_kv4_read", "kv4_read dtype", "kv4_read out_k", "kv4_read out_v"}); }
 
 // q, pages, scales, table, lengths, starts, max_new, scale, causal, window, lse, out, workspace, stream -> out or (out, lse)
+struct AttentionNames { const char *call, *q, *out; };
 template <class Of, class F>
-PyObject* attention(Args a, Of of, F f, F f_fresh, int op, const char* name) {
-  T q = values(a[0], 3, "kv_attention q");
+PyObject* attention(Args a, Of of, F f, F f_fresh, int op, const AttentionNames& name) {
+  T q = values(a[0], 3, name.q);
   const at::ScalarType type = q->scalar_type();
   const auto c = of(a[1], a[2], a[3], a[4], a[5], q->size(2));
   const int64_t rows = q->size(0);
@@ -646,15 +649,15 @@ PyObject* attention(Args a, Of of, F f, F f_fresh, int op, const char* name) {
   std::optional<Out> made, lse;
   T out;
   if (a[11] == Py_None) out = made.emplace(Py_None, type, q->sizes(), q, "").t;
-  else out = values(a[11], 3, "kv_attention out", &type);
-  shape(out, q->sizes(), "kv_attention out");
+  else out = values(a[11], 3, name.out, &type);
+  shape(out, q->sizes(), name.out);
   if (truth(a[10])) lse.emplace(Py_None, kF32, at::IntArrayRef({rows, heads}), q, "");
   const hipStream_t s = stream_of(a[13]);
   const int64_t most = c.starts ? max_new ? std::min<int64_t>(max_new, rows) : rows : rows / std::max(c.sequences, 1);
   Workspace ws;
   const bool fresh = !ws.given(a[12]);
   if (fresh) ws.allocate(op, {c.sequences, c.table_width, c.heads, heads, c.dim, most, rows}, q, s);
-  call(name, fresh ? f_fresh : f, &c, q->data_ptr(), type_of(type), q->stride(0),
+  call(name.call, fresh ? f_fresh : f, &c, q->data_ptr(), type_of(type), q->stride(0),
        q->stride(1), heads, rows, max_new, (float)scale, (int)truth(a[8]), window, out->data_ptr(), out->stride(0), out->stride(1),
        lse ? ptr<float>(lse->t) : nullptr, ws.p, ws.bytes, s);
   PyObject* o;
@@ -662,9 +665,11 @@ PyObject* attention(Args a, Of of, F f, F f_fresh, int op, const char* name) {
   else Py_INCREF(o = a[11]);
   return lse ? Py_BuildValue("NN", o, lse->result()) : o;
 }
-FUNCTION(kv_attention, 14) { return attention(a, cache_of, bmx_kv_attention, bmx_fresh_kv_attention, BMX_OP_KV_ATTENTION, "bmx_kv_attention"); }
+FUNCTION(kv_attention, 14) {
+  return attention(a, cache_of, bmx_kv_attention, bmx_fresh_kv_attention, BMX_OP_KV_ATTENTION, {"bmx_kv_attention", "kv_attention q", "kv_attention out"});
+}
 FUNCTION(kv4_attention, 14) {
-  return attention(a, cache4_of, bmx_kv4_attention, bmx_fresh_kv4_attention, BMX_OP_KV4_ATTENTION, "bmx_kv4_attention");
+  return attention(a, cache4_of, bmx_kv4_attention, bmx_fresh_kv4_attention, BMX_OP_KV4_ATTENTION, {"bmx_kv4_attention", "kv4_attention q", "kv4_attention out"});
 }
 
 // A vector of so many numbers: the caller's, or a new one.
