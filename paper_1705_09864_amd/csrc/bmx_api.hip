@@ -858,6 +858,12 @@ int bmx_kv_resize_most(const int32_t* change, int sequences, int32_t* table, int
 int bmx_rotary(const void* x, int type, int64_t x_row, int64_t x_head, int heads, int dim, int64_t rows, const int32_t* positions,
                const double* freq, int rot, int interleaved, float factor, int inverse, void* out, int64_t out_row, int64_t out_head,
                void* stream) {
+  return bmx_rotary_by(x, type, x_row, x_head, heads, dim, rows, positions, freq, rot, interleaved, factor, inverse, out, out_row, out_head, stream);
+}
+
+int bmx_rotary_by(const void* x, int type, int64_t x_row, int64_t x_head, int heads, int dim, int64_t rows, const int32_t* positions,
+                  const double* freq, int rot, int interleaved, double factor, int inverse, void* out, int64_t out_row, int64_t out_head,
+                  void* stream) {
   if (heads <= 0 || heads > 65535 || dim <= 0 || dim > 256 || rot <= 0 || rot > dim || rot % 2 || rows < 0 || rows > (1 << 23)) return BMX_ERR_SHAPE;
   if (!is_type(type)) return BMX_ERR_UNSUPPORTED;
   if (rows == 0) return BMX_OK;

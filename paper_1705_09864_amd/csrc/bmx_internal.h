@@ -268,7 +268,7 @@ size_t kv_attention_workspace_of_call(int64_t sequences, int64_t table_width, in
 hipError_t launch_kv_resize(const int32_t* change, int sequences, int32_t* table, int64_t table_ld, int table_width, int32_t* lengths, int32_t* pool,
                             int num_pages, int32_t* starts, int32_t* positions, int64_t* slots, int rows, int most, hipStream_t s);
 hipError_t launch_rotary(const void* x, int type, int64_t x_row, int64_t x_head, int heads, int dim, int rows, const int32_t* positions, const double* freq,
-                         int rot, bool interleaved, float factor, bool inverse, void* out, int64_t out_row, int64_t out_head, hipStream_t s);
+                         int rot, bool interleaved, double factor, bool inverse, void* out, int64_t out_row, int64_t out_head, hipStream_t s);
 // kv4_cache.hip, kv4_attention.hip: the cache of 4 bits and the attention over it, as those of 8.
 hipError_t launch_kv4_write(const bmx_kv4_cache& c, const void* k, const void* v, int type, int64_t k_row, int64_t k_head, int64_t v_row,
                             int64_t v_head, int rows, int max_new, hipStream_t s);

@@ -38,6 +38,7 @@
 #pragma weak bmx_kv_resize
 #pragma weak bmx_kv_resize_most
 #pragma weak bmx_rotary
+#pragma weak bmx_rotary_by
 #pragma weak bmx_kv4_write
 #pragma weak bmx_kv4_read
 #pragma weak bmx_kv4_attention
@@ -735,9 +736,12 @@ FUNCTION(rotary, 8) {
   else out = values(a[6], 3, "rotary out", &type);
   shape(out, x->sizes(), "rotary out");
   const hipStream_t s = stream_of(a[7]);
-  call("bmx_rotary", bmx_rotary, x->data_ptr(), type_of(type), x->stride(0), x->stride(1), as_int(x->size(1)), as_int(x->size(2)), x->size(0),
-       ptr<int32_t>(positions), ptr<double>(freq), as_int(2 * freq->size(0)), (int)truth(a[3]), (float)factor, (int)truth(a[5]), out->data_ptr(),
-       out->stride(0), out->stride(1), s);
+  const auto make = [&](auto f, auto by) {
+    call("bmx_rotary", f, x->data_ptr(), type_of(type), x->stride(0), x->stride(1), as_int(x->size(1)), as_int(x->size(2)), x->size(0), ptr<int32_t>(positions),
+         ptr<double>(freq), as_int(2 * freq->size(0)), (int)truth(a[3]), by, (int)truth(a[5]), out->data_ptr(), out->stride(0), out->stride(1), s);
+  };
+  if ((double)(float)factor == factor) make(bmx_rotary, (float)factor);
+  else make(bmx_rotary_by, factor);  // (a Python number has 64 bits, and the sines and cosines are rounded with it)
   if (made) return made->result();
   Py_INCREF(a[6]);
   return a[6];

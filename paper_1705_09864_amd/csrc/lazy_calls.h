@@ -31,4 +31,8 @@ int bmx_fresh_kv_attention(const bmx_kv_cache* cache, const void* q, int type, i
 int bmx_fresh_kv4_attention(const bmx_kv4_cache* cache, const void* q, int type, int64_t q_row, int64_t q_head, int q_heads, int64_t rows,
                             int max_new, float scale, int causal, int window, void* out, int64_t out_row, int64_t out_head, float* lse,
                             void* workspace, size_t workspace_bytes, void* stream);
+// bmx_rotary with a factor of 64 bits.
+int bmx_rotary_by(const void* x, int type, int64_t x_row, int64_t x_head, int heads, int dim, int64_t rows, const int32_t* positions,
+                  const double* freq, int rot, int interleaved, double factor, int inverse, void* out, int64_t out_row, int64_t out_head,
+                  void* stream);
 }

@@ -2,9 +2,9 @@
 //   a' = f (a cos t - b sin t), b' = f (b cos t + a sin t),  t = p freq_j,
 // pairs of neighbours, or of a value and the one half of the rotated part behind it.
 // The angle is taken in 64 bits as a part of a turn, p (freq_j / 2 pi) less the nearest whole number, and then less the nearest quarter: in 32 bits a position of 10^6
-// would leave 4 digits of it.  Sine and cosine of what is left, |t| <= pi / 4, are series in 64 bits too, which end below fp32's last bit with a^9 and a^10, and are rounded
-// to fp32 once, with the factor: 1501 tokens of f32 are 4.0e-8 from 64 bits, where angles rounded to fp32 ahead of the quarters left 5.3e-8, in the same time
-// (4.5 us; an angle is made once a token for all its heads).
+// would leave 4 digits of it.  Sine and cosine of what is left, |t| <= pi / 4, are series in 64 bits too, which end far below fp32's last bit with a^11 and a^10, and are
+// rounded to fp32 once, times the factor: 1501 tokens of f32 are 2.9e-8 from 64 bits, where angles rounded to fp32 ahead of the quarters, and the factor, left 5.3e-8, in the same
+// time (4.5 us; an angle is made once a token for all its heads).
 //
 // Bound by the heads' bytes, in and out once.  A workgroup takes ROWS tokens: a thread makes an angle's sine and cosine, which all heads of the token
 // share, into LDS, while its first values are on their way; then 16 bytes of each side of the pairs a step.  8192 tokens of 40 heads of 128 bf16:
@@ -29,14 +29,14 @@ struct Args {
   const double* freq;
   int heads, dim, half;  // half: pairs
   int rows;
-  float cos_by, sin_by;
+  double cos_by, sin_by;
   bool copy;  // values behind the rotated part go to another place
 };
 
 // Sine and cosine of t turns, |t| <= 1/2.
 __device__ inline void turn(double t, double* s, double* c) {
   const double n = rint(4.0 * t), a = (t - 0.25 * n) * 6.283185307179586477, b = a * a;
-  const double si = a + a * b * (-1.0 / 6 + b * (1.0 / 120 + b * (-1.0 / 5040 + b * (1.0 / 362880))));
+  const double si = a + a * b * (-1.0 / 6 + b * (1.0 / 120 + b * (-1.0 / 5040 + b * (1.0 / 362880 + b * (-1.0 / 39916800)))));
   const double co = 1.0 + b * (-0.5 + b * (1.0 / 24 + b * (-1.0 / 720 + b * (1.0 / 40320 + b * (-1.0 / 3628800)))));
   const int q = (int)n;  // -2 to 2
   const double u = q & 1 ? co : si, v = q & 1 ? si : co;
@@ -168,7 +168,7 @@ void launch(const Args& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_rotary(const void* x, int type, int64_t x_row, int64_t x_head, int heads, int dim, int rows, const int32_t* positions, const double* freq,
-                         int rot, bool interleaved, float factor, bool inverse, void* out, int64_t out_row, int64_t out_head, hipStream_t s) {
+                         int rot, bool interleaved, double factor, bool inverse, void* out, int64_t out_row, int64_t out_head, hipStream_t s) {
   const Args a = {x, x_row, x_head, out, out_row, out_head, positions, freq, heads, dim, rot / 2, rows, factor, inverse ? -factor : factor,
                   out != x && rot < dim};
   const auto f = type == BMX_F32 ? (interleaved ? launch<BMX_F32, true> : launch<BMX_F32, false>)
