@@ -10,7 +10,8 @@
 // Queries go in as parts of 8 bits each that together are all of them: one of bf16, two of f16, three of f32.  Weights p_t c_t go in as two parts, the upper
 // cut off and the lower rounded to nearest, 17 bits (16 + level is up to nine times as large as a value's share of its token's range, and sums of 16 are taken off again:
 // weights of 8 bits alone would cost results of 8 bits two of theirs, and a lower part cut off too would leave a bias that grows with
-// the tokens); for f32 results in three, and the levels less 8.  bf16 has fp32's range: nothing is held relative to a row's largest weight.
+// the tokens).  So a result is off by about 2^-17 of sum p_t (31 c_t + |d_t|) / sum p_t, however small it is itself, and then rounded.  For f32 results in three parts, and the
+// levels less 8.  bf16 has fp32's range: nothing is held relative to a row's largest weight.
 //
 // Bound by the cache's bytes: a wave goes over pages of its own (8.5 KB at 128 values a head) with its queries, running maxima, sums and results in
 // registers, and requests the next page's keys as soon as this one's are used up, its values as soon as these are.  Where rows x heads are few, a sequence's
@@ -677,7 +678,7 @@ __global__ __launch_bounds__(GROUPS * 256, DC <= 4 ? 2 : 1) void kv4_prompt_kern
         pg = next;
         next = fetch(next + 1);
       };
-      __builtin_amdgcn_s_setprio(1);
+      __builtin_amdgcn_s_setprio(1);  // (ahead of the other group's weights: 273.6 us, 276.5 without)
       both(before, buf, slot, other);
       __builtin_amdgcn_s_setprio(0);
       phase();
@@ -819,7 +820,8 @@ Plan plan(int64_t sequences, int64_t table_width, int64_t heads, int64_t q_heads
 // Whether prompts go to workgroups of two groups, one a CU, whose first reads nobody covers: where they have many pages, are alike and fill the rounds of the chip's
 // CUs.  (us in one group, in two, 32 heads on 8 of 128 bf16, sequences x new tokens of all: 2 x 1024 of 2048 103, 90, of 1536 78, 69; 4 x 1024 of 4096 359, 332, of 2048 169,
 // 165, of 1536 120, 123; 16 x 512 of 512 93, 106; 4 x 1024 of 1024 75, 84; 3 x 700 of 2700, a round of 256 and one of 8, 171, 181; 2 x 1600 of 4096 284, 257; 2 x 2048 of 2048 118,
-// 109, but one of these alone, in one round with the short ones, 78, 83; a window of 512 69, 73; 6 ragged ones 124, 129.)
+// 109, but one of these alone, in one round with the short ones, 78, 83; a window of 512 69, 73; 6 ragged ones 124, 129.)  The host knows the table's width alone, and these tables
+// are as wide as their sequences are long: with wider ones short prompts go to two groups too (4 x 1024 of 1024 82 us, 75 in one; 16 x 512 of 512 101, 87).
 bool two_groups(const bmx_kv4_cache& c, const Args& a, const Plan& p) {
   if (p.prompt_splits > 1 || (c.starts && c.sequences > 1)) return false;
   const int64_t tiles = ceil_div(p.prompt_tiles, 2) * c.heads * c.sequences, rounds = ceil_div(tiles, 256);

@@ -286,6 +286,7 @@ __global__ __launch_bounds__(256) void kv_slots_kernel(Args a) {
   put_row(a, r, pos, a.table[i * a.table_ld + (pos >> kLogPage)]);
 }
 
+// (The host knows the rows, not the pages: those given back in a call of few rows are all one workgroup's.  256 sequences of 64 pages that end 51 us, of 512 433, of 2048 1800.)
 template <int THREADS, int SEQS>
 void launch(const Args& a, hipStream_t s) {
   if (a.rows <= kMostInOne * THREADS) {
